@@ -31,7 +31,10 @@
  * momentum optimizer, a general schedule),
  * lact_prologue and lact_rmsnorm_out (and their reverses)
  * (the layer's steps on either side of the path, Alg. 1); per-matrix learning
- * rates through lact_desc.eta_per_matrix.
+ * rates through lact_desc.eta_per_matrix. For the window attention that a
+ * hybrid layer runs beside the path (§3.3): lact_qk_norm_rope and
+ * lact_window_attention (and their reverses), lact_paged_append and
+ * lact_paged_attention.
  *
  * Math layout per instance: W1, W3 are h x d, W2 is d x h, row-major, fp32.
  * The fast weights are the recurrent state; they are read and written in
@@ -511,6 +514,165 @@ int lact_rmsnorm_out_backward(const lact_desc* desc, const void* o, const float*
                               void* d_o, float* dweight, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * ------------------------------------------------------------------------
+ * The attention half of a hybrid layer (§3.3: window attention over the same
+ * projections, beside the fast weights). The conventions above hold: device
+ * pointers, asynchronous on `stream`, no allocation, every error reported
+ * before any HIP call. d is the attention's head dimension, a multiple of 8.
+ *
+ * A lact_view is a tensor [batch][head][token][d] of io_dtype elements with
+ * its strides in elements, so that a part of a fused projection, or heads
+ * behind tokens, is taken as it lies. The d elements of a vector are
+ * consecutive; the data and every stride of an extent over 1 are multiples of
+ * 16 bytes (else LACT_EALIGN), strides are >= 0 and a token's at most 2^22
+ * (else LACT_EINVAL, LACT_EUNSUPPORTED). An input may repeat itself (stride
+ * 0); an output's vectors must not overlap (a stride of 0, or a token stride
+ * below d, over an extent over 1: LACT_EINVAL). Outputs must not alias inputs
+ * or each other. A view of no vectors may have a NULL pointer.
+ */
+typedef struct lact_view {
+  void* data;
+  int64_t batch, head, token;
+} lact_view;
+
+/*
+ * Norm of queries and keys for each head, with the position rotation:
+ *
+ *   y = R(pos) (w o x / sqrt(mean_d(x^2) + eps))
+ *
+ * R turns the pairs of the first `rot` elements by pos * inv_freq[i] radians:
+ * elements (i, i + rot / 2), or (2i, 2i + 1) when `interleaved`:
+ *   y_a = x_a cos - x_b sin,  y_b = x_b cos + x_a sin
+ * Norms and rotations are fp32, angles fp64 (far positions keep their
+ * precision); one rounding at the end.
+ *
+ *   q [B][H][n][d], k [B][Hkv][n][d]       io_dtype views                       in
+ *   wq, wk     fp32 [d], or [H][d] and [Hkv][d] with weight_per_head; each may
+ *              be NULL (no weight)                                              in
+ *   inv_freq   fp64 [rot / 2]; NULL iff rot == 0 (norm only)                    in
+ *   positions  int32 [B][n], or NULL: pos0 + token                              in
+ *   qn, kn     views like q, k                                                  out
+ *
+ * d <= 512; rot <= d, even, and a multiple of 8 unless interleaved (else
+ * LACT_EUNSUPPORTED); eps finite and >= 0.
+ *
+ * lact_qk_norm_rope_backward: from the cotangents dqn, dkn of the outputs,
+ * dq and dk of the inputs and (each may be NULL) dwq, dwk (fp32, like wq, wk;
+ * sums over batch, tokens and, unless weight_per_head, heads, in a fixed
+ * order). A weight's cotangent needs the weight (else LACT_EINVAL).
+ */
+typedef struct lact_rope_desc {
+  int32_t B, H, Hkv, d;
+  int64_t n;                /* tokens of a sequence; B * n < 2^31               */
+  int64_t pos0;             /* |pos0| <= 2^40                                   */
+  int32_t rot;
+  int32_t interleaved;      /* 0 or 1                                           */
+  int32_t weight_per_head;  /* 0 or 1                                           */
+  int32_t io_dtype;
+  float eps;
+  int32_t reserved;         /* must be 0                                        */
+} lact_rope_desc;
+int lact_qk_norm_rope(const lact_rope_desc* desc, const lact_view* q, const lact_view* k, const float* wq,
+                      const float* wk, const double* inv_freq, const int32_t* positions, const lact_view* qn,
+                      const lact_view* kn, void* stream);
+size_t lact_qk_norm_rope_backward_workspace_bytes(const lact_rope_desc* desc, int* err);
+int lact_qk_norm_rope_backward(const lact_rope_desc* desc, const lact_view* q, const lact_view* k, const float* wq,
+                               const float* wk, const double* inv_freq, const int32_t* positions,
+                               const lact_view* dqn, const lact_view* dkn, const lact_view* dq, const lact_view* dk,
+                               float* dwq, float* dwk, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Softmax attention with a sliding window and first tokens that stay visible.
+ * Query i stands at position p = q_start + i and sees key j (at position j)
+ * when
+ *   j <= p + lookahead  and  (j > p - window  or  j < sinks)
+ * and both lie below the sequence's length: j, p < lengths[b] (n_kv when
+ * lengths is NULL; values are clamped to [0, n_kv]). window or lookahead -1:
+ * no bound on that side. So window = W, lookahead = 0 is the causal window of
+ * W tokens, the query's own included.
+ *
+ *   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i . k_j - lse_i)
+ *
+ * Head h uses key head h / (H / Hkv). A query that sees nothing (padding, or
+ * an empty window) has o = 0 and lse = -inf. What stands at a masked place
+ * reaches no output, also infinities and NaN (a masked pair's product is
+ * dropped, not multiplied by zero).
+ *
+ *   q [B][H][n_q][d], k, v [B][Hkv][n_kv][d]   views                            in
+ *   lengths   int32 [B], or NULL                                                in
+ *   o         view like q, every element written                                out
+ *   lse       fp32 [B][H][n_q], or NULL                                         out
+ *
+ * lact_window_attention_backward: from o and lse of the forward and the
+ * cotangent dout of o, the cotangents dq, dk, dv (every element written; zero
+ * at padding). Sums over a group's heads are in a fixed order.
+ *
+ * d <= 256; n_q, n_kv, |q_start| and q_start + n_q <= 2^29; scale finite and
+ * > 0. Weights and their cotangents are rounded to bf16 for the second
+ * products with bf16 I/O; scores, maxima, sums and accumulators are fp32.
+ */
+typedef struct lact_attn_desc {
+  int32_t B, H, Hkv, d;
+  int64_t n_q, n_kv;
+  int64_t q_start;
+  int64_t window, lookahead;  /* -1: unlimited                                  */
+  int64_t sinks;
+  float scale;
+  int32_t io_dtype;
+} lact_attn_desc;
+int lact_window_attention(const lact_attn_desc* desc, const lact_view* q, const lact_view* k, const lact_view* v,
+                          const int32_t* lengths, const lact_view* o, float* lse, void* stream);
+size_t lact_window_attention_backward_workspace_bytes(const lact_attn_desc* desc, int* err);
+int lact_window_attention_backward(const lact_attn_desc* desc, const lact_view* q, const lact_view* k,
+                                   const lact_view* v, const lact_view* o, const float* lse, const lact_view* dout,
+                                   const int32_t* lengths, const lact_view* dq, const lact_view* dk,
+                                   const lact_view* dv, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Serving: attention of new tokens over a cache of pages.
+ *
+ * The cache is `pages` pages of `page` slots; k and v of a slot and key head
+ * are d consecutive elements, at  page * batch + head * head + slot * token
+ * elements by the strides of their view (k_cache and v_cache have the same
+ * strides). Position j of sequence b lies in slot j % page of page
+ * table[b][j / page]. lens[b] counts its tokens, the new ones included; the
+ * new tokens of b are rows cu_new[b] .. cu_new[b + 1] - 1 of q, k, v and o
+ * and stand at its last positions. All three are device data: values out of
+ * range are clamped, never followed; positions whose page is outside
+ * [0, pages) hold nothing (masked; not written by the append).
+ *
+ * lact_paged_append writes the new tokens' keys and values into their slots;
+ * lact_paged_attention attends with the causal window and sinks of
+ * lact_window_attention (lookahead 0). Rows of no sequence (before cu_new[0],
+ * from cu_new[B] on) are left as they were. Pages that several sequences share
+ * are read by all; if an append of one call writes a slot twice, either value
+ * may stay.
+ *
+ *   q, o    [n_new][H][d], k, v [n_new][Hkv][d]   views (batch is not used)
+ *   table   int32 [B][max_pages]; lens int32 [B]; cu_new int32 [B + 1]          in
+ *
+ * d <= 256; n_new * H < 2^31; max_pages * page <= 2^29; scale > 0. For
+ * lact_paged_append H, window, sinks and scale are not used.
+ */
+typedef struct lact_paged_desc {
+  int32_t B, H, Hkv, d;
+  int64_t n_new;
+  int64_t pages;
+  int32_t page, max_pages;
+  int64_t window;             /* -1: unlimited                                  */
+  int64_t sinks;
+  float scale;
+  int32_t io_dtype;
+} lact_paged_desc;
+int lact_paged_append(const lact_paged_desc* desc, const lact_view* k, const lact_view* v, const lact_view* k_cache,
+                      const lact_view* v_cache, const int32_t* table, const int32_t* lens, const int32_t* cu_new,
+                      void* stream);
+size_t lact_paged_attention_workspace_bytes(const lact_paged_desc* desc, int* err);
+int lact_paged_attention(const lact_paged_desc* desc, const lact_view* q, const lact_view* k_cache,
+                         const lact_view* v_cache, const int32_t* table, const int32_t* lens, const int32_t* cu_new,
+                         const lact_view* o, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Kernel timing (instrumentation for benchmarks). While enabled, lact_forward
  * brackets every kernel launch with HIP events on its stream, grouped by
  * kernel class (LACT_KCLASS_*). lact_timing_read synchronises on the recorded
@@ -529,7 +691,10 @@ int lact_rmsnorm_out_backward(const lact_desc* desc, const void* o, const float*
                                /* (lact_backward_linear: its contractions count   */
                                /* as BWD, its row and token steps as UPDATE, its  */
                                /* transposed copies as PREP)                      */
-#define LACT_KCLASS_COUNT 6
+#define LACT_KCLASS_ATTN 6     /* lact_window_attention and its reverse,          */
+                               /* lact_paged_attention (lact_qk_norm_rope, its    */
+                               /* reverse and lact_paged_append count as IO)      */
+#define LACT_KCLASS_COUNT 7
 int lact_timing_enable(int enable);
 int lact_timing_reset(void);
 int lact_timing_read(int kclass, int64_t* launches, double* total_ms, double* flops);

@@ -10,6 +10,7 @@ from .binding import (  # noqa: F401
     forward_schedule, forward_linear, backward, backward_linear, backward_workspace_bytes, backward_momentum,
     backward_momentum_workspace_bytes, backward_schedule, prologue, rmsnorm_out,
     prologue_backward, rmsnorm_out_backward, check_desc,
+    qk_norm_rope, qk_norm_rope_backward, window_attention, window_attention_backward, paged_append, paged_attention,
     timing_enable, timing_reset, timing_read, KCLASS_NAMES,
     APPLY_THEN_UPDATE, UPDATE_THEN_APPLY, IO_BF16, IO_FP32, SEG_MODES, FW_SWIGLU, FW_LINEAR,
 )

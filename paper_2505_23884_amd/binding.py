@@ -9,7 +9,7 @@ LIB_PATH = os.path.join(PKG, "liblact.so")
 
 APPLY_THEN_UPDATE, UPDATE_THEN_APPLY = 0, 1
 IO_BF16, IO_FP32 = 0, 1
-KCLASS_NAMES = ("fwd", "bwd", "update", "ns", "prep", "io")
+KCLASS_NAMES = ("fwd", "bwd", "update", "ns", "prep", "io", "attn")
 
 _ERRORS = {0: "LACT_OK", -1: "LACT_EINVAL", -2: "LACT_EALIGN", -3: "LACT_EWORKSPACE",
            -4: "LACT_EUNSUPPORTED", -5: "LACT_EHIP", -6: "LACT_ESCRATCH"}
@@ -40,6 +40,32 @@ SEG_MODES = {"apply_then_update": 0, "update_then_apply": 1, "update_only": 2, "
 class LactSegment(ctypes.Structure):
     _fields_ = [("mode", ctypes.c_int32), ("reserved", ctypes.c_int32), ("begin", ctypes.c_int64),
                 ("end", ctypes.c_int64)]
+
+
+class LactView(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("head", ctypes.c_int64),
+                ("token", ctypes.c_int64)]
+
+
+class LactRopeDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("n", ctypes.c_int64), ("pos0", ctypes.c_int64), ("rot", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("weight_per_head", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class LactAttnDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("n_q", ctypes.c_int64), ("n_kv", ctypes.c_int64), ("q_start", ctypes.c_int64),
+                ("window", ctypes.c_int64), ("lookahead", ctypes.c_int64), ("sinks", ctypes.c_int64),
+                ("scale", ctypes.c_float), ("io_dtype", ctypes.c_int32)]
+
+
+class LactPagedDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("n_new", ctypes.c_int64), ("pages", ctypes.c_int64), ("page", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("window", ctypes.c_int64), ("sinks", ctypes.c_int64),
+                ("scale", ctypes.c_float), ("io_dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -94,6 +120,22 @@ def load_library(path: str | None = None):
     L.lact_rmsnorm_out_backward.argtypes = [dp, vp, vp, f32, vp, vp, vp, vp, sz, vp]
     L.lact_rmsnorm_out_backward.restype = i32
     L.lact_rmsnorm_out.restype = i32
+    vw, ip = ctypes.POINTER(LactView), ctypes.POINTER(i32)
+    rp, ap, pp = ctypes.POINTER(LactRopeDesc), ctypes.POINTER(LactAttnDesc), ctypes.POINTER(LactPagedDesc)
+    L.lact_qk_norm_rope.argtypes = [rp, vw, vw, vp, vp, vp, vp, vw, vw, vp]
+    L.lact_qk_norm_rope_backward.argtypes = [rp, vw, vw, vp, vp, vp, vp, vw, vw, vw, vw, vp, vp, vp, sz, vp]
+    L.lact_window_attention.argtypes = [ap, vw, vw, vw, vp, vw, vp, vp]
+    L.lact_window_attention_backward.argtypes = [ap, vw, vw, vw, vw, vp, vw, vp, vw, vw, vw, vp, sz, vp]
+    L.lact_paged_append.argtypes = [pp, vw, vw, vw, vw, vp, vp, vp, vp]
+    L.lact_paged_attention.argtypes = [pp, vw, vw, vw, vp, vp, vp, vw, vp, sz, vp]
+    for f in ("lact_qk_norm_rope", "lact_qk_norm_rope_backward", "lact_window_attention",
+              "lact_window_attention_backward", "lact_paged_append", "lact_paged_attention"):
+        getattr(L, f).restype = i32
+    for f, desc in (("lact_qk_norm_rope_backward_workspace_bytes", rp),
+                    ("lact_window_attention_backward_workspace_bytes", ap),
+                    ("lact_paged_attention_workspace_bytes", pp)):
+        getattr(L, f).argtypes = [desc, ip]
+        getattr(L, f).restype = sz
     L.lact_timing_enable.argtypes = [i32]
     L.lact_timing_enable.restype = i32
     L.lact_timing_reset.argtypes = []
@@ -726,6 +768,256 @@ def rmsnorm_out_backward(o, dy, weight=None, eps=1e-6, with_dweight=True, out=No
     if rc:
         _raise(rc)
     return d_o, dw
+
+
+# ---- the attention half of a hybrid layer (strided tensors are taken as they lie)
+
+def _io(t, name):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return IO_BF16
+    if t.dtype == torch.float32:
+        return IO_FP32
+    raise LactError(-1, f"unsupported {name} dtype {t.dtype}")
+
+
+def _view(t, batch=0, head=1, token=2):
+    """LactView of a tensor whose last dimension is a vector; batch None: no batch dimension."""
+    return LactView(t.data_ptr(), 0 if batch is None else t.stride(batch), t.stride(head), t.stride(token))
+
+
+def _check(t, name, shape, like):
+    """A tensor of `shape`, of like's type and on its device, vectors consecutive."""
+    if tuple(t.shape) != tuple(shape):
+        raise LactError(-1, f"{name} must be {list(shape)}, not {list(t.shape)}")
+    if t.dtype != like.dtype:
+        raise LactError(-1, f"{name} must be {like.dtype}, not {t.dtype}")
+    if t.device != like.device or not t.is_cuda:
+        raise LactError(-1, f"{name} must be a device tensor on {like.device}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise LactError(-1, f"{name}'s last dimension must be contiguous")
+
+
+def _check_aux(t, name, shape, dtype, like):
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous() or t.device != like.device:
+        raise LactError(-1, f"{name} must be a contiguous {dtype} tensor {list(shape)} on {like.device}")
+
+
+def _call(fn, like, stream, *args):
+    """fn(*args, stream) on like's device and its current stream (or `stream`)."""
+    import torch
+    i = like.device.index
+    if torch.cuda.current_device() == i:
+        rc = fn(*args, torch.cuda.current_stream(i).cuda_stream if stream is None else stream)
+    else:
+        with torch.cuda.device(i):
+            rc = fn(*args, torch.cuda.current_stream(i).cuda_stream if stream is None else stream)
+    if rc:
+        _raise(rc)
+
+
+def _workspace(fn, desc, workspace, like):
+    import torch
+    err = ctypes.c_int(0)
+    n = int(fn(ctypes.byref(desc), ctypes.byref(err)))
+    if err.value:
+        _raise(err.value)
+    if workspace is None:
+        return (torch.empty(n, dtype=torch.uint8, device=like.device) if n else None), n
+    if workspace.device != like.device or not workspace.is_contiguous():
+        raise LactError(-1, f"workspace must be a contiguous tensor on {like.device}")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _p(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rope_desc(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved):
+    import torch
+    if q.dim() != 4 or k.dim() != 4:
+        raise LactError(-1, "q must be [B, n, H, d] and k [B, n, Hkv, d]")
+    B, n, H, d = q.shape
+    Hkv = k.shape[2]
+    _check(q, "q", (B, n, H, d), q)
+    _check(k, "k", (B, n, Hkv, d), q)
+    per_head = any(w is not None and w.dim() == 2 for w in (wq, wk))
+    _check_aux(wq, "wq", (H, d) if per_head else (d,), torch.float32, q)
+    _check_aux(wk, "wk", (Hkv, d) if per_head else (d,), torch.float32, q)
+    if inv_freq is not None and inv_freq.dim() != 1:
+        raise LactError(-1, "inv_freq must be [rot / 2]")
+    rot = 0 if inv_freq is None else 2 * inv_freq.shape[0]
+    if rot:
+        _check_aux(inv_freq, "inv_freq", (rot // 2,), torch.float64, q)
+    _check_aux(positions, "positions", (B, n), torch.int32, q)
+    return LactRopeDesc(B, H, Hkv, d, n, int(pos0), rot, int(bool(interleaved)), int(per_head), _io(q, "q"), float(eps), 0)
+
+
+def qk_norm_rope(q, k, wq=None, wk=None, inv_freq=None, *, positions=None, pos0=0, eps=1e-6, interleaved=False,
+                 out=None, stream=None):
+    """RMS norm of queries and keys for each head with the position rotation
+    (lact_qk_norm_rope): q [B, n, H, d], k [B, n, Hkv, d] (bf16 or fp32; any
+    strides with contiguous vectors, such as parts of a fused projection); wq,
+    wk fp32 [d], or [H, d] and [Hkv, d], or None; inv_freq fp64 [rot / 2]
+    radians a position, or None (norm only); positions int32 [B, n], or None
+    (pos0 + token). Returns (qn [B, H, n, d], kn [B, Hkv, n, d]), into ``out``
+    (two tensors of those shapes, any strides) when it is given."""
+    import torch
+    desc = _rope_desc(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved)
+    B, n, H, d = q.shape
+    if out is None:
+        out = (torch.empty(B, H, n, d, dtype=q.dtype, device=q.device),
+               torch.empty(B, k.shape[2], n, d, dtype=q.dtype, device=q.device))
+    qn, kn = out
+    _check(qn, "qn", (B, H, n, d), q)
+    _check(kn, "kn", (B, k.shape[2], n, d), q)
+    _call(lib().lact_qk_norm_rope, q, stream, desc, _view(q, 0, 2, 1), _view(k, 0, 2, 1), _p(wq), _p(wk),
+          _p(inv_freq) if desc.rot else None, _p(positions), _view(qn), _view(kn))
+    return qn, kn
+
+
+def qk_norm_rope_backward(q, k, dqn, dkn, wq=None, wk=None, inv_freq=None, *, positions=None, pos0=0, eps=1e-6,
+                          interleaved=False, with_dweight=True, out=None, workspace=None, stream=None):
+    """Reverse of qk_norm_rope() (lact_qk_norm_rope_backward): from the
+    cotangents dqn [B, H, n, d], dkn [B, Hkv, n, d], returns (dq [B, n, H, d],
+    dk [B, n, Hkv, d], dwq, dwk); the weights' cotangents are None without a
+    weight or with_dweight. ``out`` may hold that tuple."""
+    import torch
+    desc = _rope_desc(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved)
+    B, n, H, d = q.shape
+    Hkv = k.shape[2]
+    _check(dqn, "dqn", (B, H, n, d), q)
+    _check(dkn, "dkn", (B, Hkv, n, d), q)
+    if out is None:
+        dw = [torch.empty_like(w) if w is not None and with_dweight else None for w in (wq, wk)]
+        out = (torch.empty(B, n, H, d, dtype=q.dtype, device=q.device),
+               torch.empty(B, n, Hkv, d, dtype=q.dtype, device=q.device), *dw)
+    dq, dk, dwq, dwk = out
+    _check(dq, "dq", (B, n, H, d), q)
+    _check(dk, "dk", (B, n, Hkv, d), q)
+    for t, w, name in ((dwq, wq, "dwq"), (dwk, wk, "dwk")):
+        if t is not None and w is None:
+            raise LactError(-1, f"{name} needs its weight")
+        if t is not None:
+            _check_aux(t, name, w.shape, torch.float32, q)
+    nb = 0
+    if dwq is not None or dwk is not None:
+        workspace, nb = _workspace(lib().lact_qk_norm_rope_backward_workspace_bytes, desc, workspace, q)
+    _call(lib().lact_qk_norm_rope_backward, q, stream, desc, _view(q, 0, 2, 1), _view(k, 0, 2, 1), _p(wq), _p(wk),
+          _p(inv_freq) if desc.rot else None, _p(positions), _view(dqn), _view(dkn), _view(dq, 0, 2, 1),
+          _view(dk, 0, 2, 1), _p(dwq), _p(dwk), _p(workspace), nb)
+    return dq, dk, dwq, dwk
+
+
+def _attn_desc(q, k, v, window, sinks, lookahead, lengths, scale, q_start):
+    import torch
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise LactError(-1, "q must be [B, H, n_q, d], k and v [B, Hkv, n_kv, d]")
+    B, H, n_q, d = q.shape
+    Hkv, n_kv = k.shape[1], k.shape[2]
+    _check(q, "q", (B, H, n_q, d), q)
+    _check(k, "k", (B, Hkv, n_kv, d), q)
+    _check(v, "v", (B, Hkv, n_kv, d), q)
+    _check_aux(lengths, "lengths", (B,), torch.int32, q)
+    return LactAttnDesc(B, H, Hkv, d, n_q, n_kv, n_kv - n_q if q_start is None else int(q_start),
+                        -1 if window is None else int(window), -1 if lookahead is None else int(lookahead), int(sinks),
+                        d ** -0.5 if scale is None else float(scale), _io(q, "q"))
+
+
+def window_attention(q, k, v, *, window=None, sinks=0, lookahead=0, lengths=None, scale=None, q_start=None,
+                     with_lse=False, out=None, stream=None):
+    """Softmax attention with a sliding window and first tokens that stay
+    visible (lact_window_attention): q [B, H, n_q, d], k, v [B, Hkv, n_kv, d]
+    (bf16 or fp32, any strides with contiguous vectors). Query i stands at
+    position p = q_start + i (q_start: n_kv - n_q) and sees key j when
+    j <= p + lookahead and (j > p - window or j < sinks), both below
+    lengths[b] (int32 [B], or None: n_kv). None for window or lookahead: no
+    bound. scale: d ** -0.5. A query that sees nothing gives 0 (lse -inf).
+    Returns o like q, or (o, lse fp32 [B, H, n_q]) with_lse; ``out`` may hold o,
+    or that pair."""
+    import torch
+    desc = _attn_desc(q, k, v, window, sinks, lookahead, lengths, scale, q_start)
+    B, H, n_q, _ = q.shape
+    if out is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty(B, H, n_q, dtype=torch.float32, device=q.device) if with_lse else None
+    else:
+        o, lse = out if with_lse else (out, None)
+    _check(o, "o", q.shape, q)
+    _check_aux(lse, "lse", (B, H, n_q), torch.float32, q)
+    _call(lib().lact_window_attention, q, stream, desc, _view(q), _view(k), _view(v), _p(lengths), _view(o), _p(lse))
+    return (o, lse) if with_lse else o
+
+
+def window_attention_backward(q, k, v, o, lse, dout, *, window=None, sinks=0, lookahead=0, lengths=None, scale=None,
+                              q_start=None, out=None, workspace=None, stream=None):
+    """Reverse of window_attention() (lact_window_attention_backward): from its
+    o and lse and the cotangent dout of o, returns (dq, dk, dv), written into
+    ``out`` (that tuple) when it is given."""
+    import torch
+    desc = _attn_desc(q, k, v, window, sinks, lookahead, lengths, scale, q_start)
+    _check(o, "o", q.shape, q)
+    _check(dout, "dout", q.shape, q)
+    if lse is None:
+        raise LactError(-1, "lse of the forward is needed")
+    _check_aux(lse, "lse", q.shape[:3], torch.float32, q)
+    if out is None:
+        out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dq, dk, dv = out
+    for t, ref, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
+        _check(t, name, ref.shape, q)
+    workspace, nb = _workspace(lib().lact_window_attention_backward_workspace_bytes, desc, workspace, q)
+    _call(lib().lact_window_attention_backward, q, stream, desc, _view(q), _view(k), _view(v), _view(o), _p(lse),
+          _view(dout), _p(lengths), _view(dq), _view(dk), _view(dv), _p(workspace), nb)
+    return dq, dk, dv
+
+
+def _paged_desc(x, H, k_cache, v_cache, table, lens, cu_new, window, sinks, scale):
+    import torch
+    if x.dim() != 3 or k_cache.dim() != 4 or table.dim() != 2:
+        raise LactError(-1, "new tokens are [n_new, heads, d], caches [pages, page, Hkv, d], table [B, max_pages]")
+    pages, page, Hkv, d = k_cache.shape
+    B, max_pages = table.shape
+    _check(x, "the new tokens", (x.shape[0], x.shape[1], d), x)
+    _check(k_cache, "k_cache", k_cache.shape, x)
+    _check(v_cache, "v_cache", k_cache.shape, x)
+    _check_aux(table, "table", (B, max_pages), torch.int32, x)
+    _check_aux(lens, "lens", (B,), torch.int32, x)
+    _check_aux(cu_new, "cu_new", (B + 1,), torch.int32, x)
+    return LactPagedDesc(B, H, Hkv, d, x.shape[0], pages, page, max_pages, -1 if window is None else int(window),
+                         int(sinks), d ** -0.5 if scale is None else float(scale), _io(x, "new tokens"))
+
+
+def paged_append(k, v, k_cache, v_cache, table, lens, cu_new, *, stream=None):
+    """Writes new keys and values k, v [n_new, Hkv, d] into the pages of a
+    cache (lact_paged_append): k_cache, v_cache [pages, page, Hkv, d] (in
+    place), table int32 [B, max_pages], lens int32 [B] (tokens of a sequence,
+    the new ones included), cu_new int32 [B + 1] (rows of a sequence's new
+    tokens, which are its last positions)."""
+    desc = _paged_desc(k, k.shape[1], k_cache, v_cache, table, lens, cu_new, None, 0, 1.0)
+    if k.shape[1] != desc.Hkv:
+        raise LactError(-1, "k must be [n_new, Hkv, d]")
+    _check(v, "v", k.shape, k)
+    _call(lib().lact_paged_append, k, stream, desc, _view(k, None, 1, 0), _view(v, None, 1, 0), _view(k_cache, 0, 2, 1),
+          _view(v_cache, 0, 2, 1), _p(table), _p(lens), _p(cu_new))
+
+
+def paged_attention(q, k_cache, v_cache, table, lens, cu_new, *, window=None, sinks=0, scale=None, out=None,
+                    workspace=None, stream=None):
+    """Causal attention of new tokens q [n_new, H, d] over a cache of pages
+    (lact_paged_attention): the cache, table, lens and cu_new of
+    paged_append(), window and sinks of window_attention(). Returns o like q
+    (rows of no sequence are left as they were), into ``out`` when given."""
+    import torch
+    desc = _paged_desc(q, q.shape[1] if q.dim() == 3 else 0, k_cache, v_cache, table, lens, cu_new, window, sinks, scale)
+    o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    _check(o, "o", q.shape, q)
+    workspace, nb = _workspace(lib().lact_paged_attention_workspace_bytes, desc, workspace, q)
+    _call(lib().lact_paged_attention, q, stream, desc, _view(q, None, 1, 0), _view(k_cache, 0, 2, 1),
+          _view(v_cache, 0, 2, 1), _p(table), _p(lens), _p(cu_new), _view(o, None, 1, 0), _p(workspace), nb)
+    return o
 
 
 def timing_enable(on: bool = True):

@@ -4,15 +4,18 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liblact.so")
-SOURCES = ["lact_api.hip", "lact_kernels.hip", "lact_io.hip"]
+SOURCES = ["lact_api.hip", "lact_kernels.hip", "lact_io.hip", "lact_attn_api.hip", "lact_window.hip", "lact_paged.hip",
+           "lact_rope.hip"]
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed fp32 VALU ops stay off: plain fp32 math only
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument",
@@ -27,16 +30,25 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source into liblact.so next to this file; returns its path."""
+    """Compile every HIP source (side by side) and link liblact.so next to this file; returns its path."""
     tmp = LIB + ".tmp"
-    cmd = [hipcc(), *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError(f"hipcc failed ({res.returncode}) building {LIB}")
+    with tempfile.TemporaryDirectory() as objs, ThreadPoolExecutor(max_workers=4) as pool:
+        def run(cmd):
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            res = subprocess.run(cmd, capture_output=True, text=True)
+            if res.returncode != 0:
+                sys.stderr.write(res.stdout + res.stderr)
+                raise RuntimeError(f"hipcc failed ({res.returncode}) building {LIB}")
+
+        def compile_one(src):
+            obj = os.path.join(objs, src + ".o")
+            run([hipcc(), *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", os.path.join(CSRC, src),
+                 "-o", obj])
+            return obj
+
+        objects = list(pool.map(compile_one, SOURCES))
+        run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", *objects, "-o", tmp])
     os.replace(tmp, LIB)
     return LIB
 

@@ -362,6 +362,14 @@ int timed(int kclass, double flops, hipStream_t s, F&& launch) {
   return rc;
 }
 
+}  // namespace
+
+int timed_launch(int kclass, double flops, hipStream_t s, hipError_t (*launch)(void*), void* ctx) {
+  return timed(kclass, flops, s, [&] { return launch(ctx); });
+}
+
+namespace {
+
 // ---------------------------------------------------------------- schedule
 struct Ctx {
   const lact_desc* dsc;

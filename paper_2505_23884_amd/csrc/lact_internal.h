@@ -512,4 +512,98 @@ hipError_t launch_zero_rows(void* out, int BH, int64_t row_bytes, int64_t rows, 
 hipError_t launch_zero_f32(float* x, int BH, int64_t inst, int64_t off, int64_t count, hipStream_t s);
 constexpr int kNsBlockElems = 4096;
 
+// ---- attention half of the layer (lact_window.hip, lact_paged.hip, lact_rope.hip)
+// [batch, head, token] of rows of d elements; strides in elements.
+struct AttnView {
+  void* p;
+  int64_t sb, sh, st;
+};
+constexpr int64_t kAttnTokens = (int64_t)1 << 29;   // tokens, positions, windows: int32 sums of two stay in range
+
+// Query i stands at position p = q_start + i and sees key j when
+// j <= p + look, j > p - win or j < sinks, and both are below the length.
+struct WindowArgs {
+  AttnView q, k, v, o;
+  float* lse;            // [B * H][n_q], or nullptr
+  const int32_t* len;    // [B], or nullptr (n_kv)
+  int B, H, Hkv, G, d;   // G = H / Hkv
+  int n_q, n_kv, q_start, win, look, sinks;
+  float scale;
+};
+hipError_t launch_window_fwd(const WindowArgs& a, bool bf16, hipStream_t s);
+
+// Jobs of the key-stationary half of the backward: a job is one tile of `kb`
+// keys of one (batch, key head) with a part of the queries that see it. Tiles
+// below `st` hold sinks and are cut into np_s parts of ch_s queries, the
+// others into np_a of ch_a; and the heads of a group into gs parts. A tile of
+// more than one part leaves fp32 partial sums, one slot a part.
+struct DkvPlan {
+  int kb, ntile, st, np_s, np_a, ch_s, ch_a, gs;
+  __host__ __device__ int jobs() const { return (st * np_s + (ntile - st) * np_a) * gs; }
+  __host__ __device__ int slots() const {
+    return (np_s * gs > 1 ? st * np_s * gs : 0) + (np_a * gs > 1 ? (ntile - st) * np_a * gs : 0);
+  }
+};
+DkvPlan window_dkv_plan(const WindowArgs& a, bool bf16);
+
+struct WindowBwdArgs {
+  WindowArgs f;          // f.lse: read; f.o: the forward's output, read
+  AttnView dout, dq, dk, dv;
+  float* lse2;           // [B * H][n_q]: lse log2(e), +inf where it is -inf
+  float* delta;          // [B * H][n_q]: sum_d dout o
+  float* part;           // [B * Hkv][slots][2][kb][d]: dK and dV partial sums
+  DkvPlan plan;
+};
+hipError_t launch_window_bwd(const WindowBwdArgs& a, bool bf16, hipStream_t s);
+
+// Attention of T new tokens, those of sequence b at rows cu[b] .. cu[b + 1] - 1
+// and at its last positions, over a cache of `pages` pages of `page` slots.
+struct PagedArgs {
+  AttnView q, o;         // [token][head] rows (sb unused)
+  const void *kc, *vc;   // element (page, head, slot) at page c.sb + head c.sh + slot c.st (k and v alike)
+  AttnView c;            // strides of the cache (p unused)
+  const int32_t *table, *len, *cu;
+  int B, H, Hkv, G, d, T, page, max_pages, pages, win, look, sinks;
+  uint32_t mul, shift;   // x / page = (mulhi(x, mul) + x) >> shift
+  float scale;
+  int splits;            // parts of the keys; more than one: sums to `part`, joined by a second launch
+  bool wide;             // 128 rows (token, head of the group) a workgroup, else 32
+  float* part;           // [splits][T * H][d], then [splits][T * H][2]: maximum and sum
+};
+void paged_plan(PagedArgs& a, bool bf16);   // splits and wide, from the sizes
+hipError_t launch_paged(const PagedArgs& a, bool bf16, hipStream_t s);
+
+struct AppendArgs {
+  AttnView k, v;         // [token][head] rows
+  void *kc, *vc;
+  AttnView c;
+  const int32_t *table, *len, *cu;
+  int B, Hkv, d, T, page, max_pages, pages;
+  uint32_t mul, shift;
+};
+hipError_t launch_append(const AppendArgs& a, bool bf16, hipStream_t s);
+
+// Norm and rotation of q and k (lact_rope.hip). The reverse reads dy in y's
+// place and writes dx.
+struct RopeArgs {
+  AttnView x[2], y[2], dx[2];   // q, k
+  const float* w[2];            // [d] or [heads][d], or nullptr
+  const double* freq;           // [rot / 2] radians a position, or nullptr (rot 0)
+  const int32_t* pos;           // [B][n], or nullptr: pos0 + token
+  int64_t pos0, n;
+  int B, H[2], d, rot;
+  bool interleaved, per_head;
+  float eps;
+  float* dw[2];                 // reverse: [d] or [heads][d], or nullptr
+  float* part;                  // reverse: partial sums of dw
+  int tb, hs, nblk;             // tokens a step, head parts (forward), workgroups
+};
+void rope_plan(RopeArgs& a, bool bf16, bool bwd);
+size_t rope_part_floats(const RopeArgs& a);
+hipError_t launch_rope(const RopeArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_rope_bwd(const RopeArgs& a, bool bf16, hipStream_t s);
+
+// timed() of lact_api.hip for the entry points of other files.
+int timed_launch(int kclass, double flops, hipStream_t s, hipError_t (*launch)(void*), void* ctx);
+
 }  // namespace lact

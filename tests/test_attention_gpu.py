@@ -1,0 +1,206 @@
+"""The attention entry points on the GPU against plain 64-bit forms, with
+bounds derived from the arithmetic (attention_reference.py)."""
+import math
+
+import pytest
+import torch
+
+import paper_2505_23884_amd as P
+from attention_reference import HALF, attention, check, norm_rope
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def rnd(seed, *shape, dtype=torch.bfloat16, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(dtype)
+
+
+def strided(x):
+    """The same [B, H, n, d] values with heads behind tokens and a gap after each token."""
+    B, H, n, d = x.shape
+    big = torch.full((B, n, H + 1, d), float("nan"), dtype=x.dtype, device=x.device)
+    big[:, :, :H] = x.transpose(1, 2)
+    return big[:, :, :H].transpose(1, 2)
+
+
+BF, F32 = torch.bfloat16, torch.float32
+# B, H, Hkv, n_q, n_kv, d, options
+WINDOW = [
+    (1, 1, 1, 1, 1, 64, {}),
+    (2, 2, 1, 33, 33, 64, {}),
+    (1, 4, 2, 130, 130, 128, {}),
+    (1, 2, 2, 300, 300, 128, dict(window=1)),
+    (1, 2, 1, 257, 257, 128, dict(window=64, sinks=4)),
+    (1, 6, 2, 200, 200, 80, dict(window=50, sinks=70)),
+    (2, 5, 1, 190, 190, 96, dict(window=17, lookahead=9)),
+    (1, 2, 2, 140, 140, 64, dict(window=None, lookahead=None)),
+    (1, 2, 1, 150, 150, 256, dict(window=40, sinks=2)),
+    (1, 1, 1, 70, 70, 200, dict(lookahead=None)),
+    (2, 2, 2, 7, 150, 64, dict(window=100)),              # queries at the end of longer keys
+    (1, 2, 1, 150, 20, 64, {}),                           # more queries than keys: the first see nothing
+    (1, 2, 2, 100, 100, 64, dict(window=0)),              # empty windows
+    (1, 2, 2, 100, 100, 64, dict(window=0, sinks=3)),
+    (1, 2, 1, 100, 300, 8, dict(q_start=50, window=60, lookahead=20)),
+    (1, 1, 1, 90, 64, 64, dict(q_start=-30, window=10, lookahead=4)),
+    (3, 2, 1, 210, 210, 64, dict(window=64, sinks=1, lengths=[0, 1, 131])),
+    (4, 2, 2, 140, 140, 128, dict(window=None, lookahead=None, lengths=[140, 64, 128, -5])),
+    (2, 8, 1, 65, 65, 24, dict(scale=0.5)),
+    (1, 2, 1, 1000, 1000, 64, dict(window=100, sinks=130)),
+    (1, 2, 1, 5, 0, 64, {}),                              # no keys
+    (1, 2, 1, 0, 5, 64, {}),                              # no queries
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("i", range(len(WINDOW)))
+def test_window_attention_matches_the_formula(i, dtype):
+    B, H, Hkv, n_q, n_kv, d, opt = WINDOW[i]
+    opt = dict(opt)
+    q, k, v, do = (rnd(10 * i + x, B, h, n, d, dtype=dtype) for x, h, n in
+                   ((0, H, n_q), (1, Hkv, n_kv), (2, Hkv, n_kv), (3, H, n_q)))
+    want, tol = attention(q, k, v, do=do, **opt)
+    if "lengths" in opt:
+        opt["lengths"] = torch.tensor(opt["lengths"], dtype=torch.int32, device=DEV)
+    q, k, v, do = (x.to(DEV) for x in (q, k, v, do))
+    if i % 2:
+        q, k, v, do = (strided(x) for x in (q, k, v, do))
+    print(f"[gpu] window {WINDOW[i]} {dtype}", flush=True)
+    o, lse = P.window_attention(q, k, v, with_lse=True, **opt)
+    torch.cuda.synchronize()
+    check("o", o, want["o"], tol["o"])
+    check("lse", lse, want["lse"], tol["lse"])
+    dq, dk, dv = P.window_attention_backward(q, k, v, o, lse, do, **opt)
+    torch.cuda.synchronize()
+    for name, got in (("dq", dq), ("dk", dk), ("dv", dv)):
+        check(name, got, want[name], tol[name])
+
+
+ROPE = [
+    # B, n, H, Hkv, d, rot, interleaved, per_head, far
+    (1, 1, 1, 1, 8, 8, False, False, 0),
+    (2, 5, 3, 1, 64, 64, False, False, 0),
+    (1, 40, 4, 2, 128, 128, False, False, 100000),
+    (3, 17, 2, 2, 128, 64, False, True, 0),
+    (1, 33, 5, 1, 80, 40, False, False, 7),
+    (2, 9, 2, 1, 96, 96, True, False, 1000000),
+    (1, 21, 2, 1, 64, 6, True, True, 3),
+    (2, 3, 2, 2, 256, 0, False, False, 0),
+    (1, 70, 1, 1, 512, 512, False, False, 0),
+    (1, 2100, 2, 1, 72, 16, False, False, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("i", range(len(ROPE)))
+def test_qk_norm_rope_matches_the_formula(i, dtype):
+    B, n, H, Hkv, d, rot, inter, per_head, far = ROPE[i]
+    fused = rnd(i, B, n, H + 2 * Hkv, d, dtype=dtype).to(DEV)
+    q, k = fused[:, :, :H], fused[:, :, H:H + Hkv]
+    wq, wk = ((torch.rand(*((h, d) if per_head else (d,)), generator=torch.Generator().manual_seed(i + 50)) + 0.5).to(DEV)
+              for h in (H, Hkv))
+    if i == 0:
+        wk = None
+    inv = (10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)).to(DEV) if rot else None
+    pos = torch.arange(n, dtype=torch.int32).repeat(B, 1) * (1 if i % 3 else -1) + far
+    kw = dict(eps=1e-5, interleaved=inter)
+    if i % 2:
+        kw["positions"] = pos.to(DEV)
+    else:
+        kw["pos0"] = far
+        pos = torch.arange(n, dtype=torch.int32).repeat(B, 1) + far
+    dqn, dkn = rnd(i + 7, B, H, n, d, dtype=dtype).to(DEV), rnd(i + 8, B, Hkv, n, d, dtype=dtype).to(DEV)
+    print(f"[gpu] rope {ROPE[i]} {dtype}", flush=True)
+    qn, kn = P.qk_norm_rope(q, k, wq, wk, inv, **kw)
+    dq, dk, dwq, dwk = P.qk_norm_rope_backward(q, k, dqn, dkn, wq, wk, inv, **kw)
+    torch.cuda.synchronize()
+    h, u = HALF[dtype], 2.0 ** -24
+    for x, w, y, dy, dx, dw, name in ((q, wq, qn, dqn, dq, dwq, "q"), (k, wk, kn, dkn, dk, dwk, "k")):
+        ry, rdx, rdw, mag, wmag = norm_rope(x, w, inv, pos, 1e-5, inter, dy)
+        # norm and products: d + 16 roundings; the angle's sine and cosine: a step each of 2 pi 2^-24
+        e = (d + 32) * u
+        amp = (x.double().abs().cpu() * (1.0 if w is None else w.double().cpu().abs())).amax(-1).transpose(1, 2)[..., None]
+        r = (1.0 / torch.sqrt(x.double().cpu().square().mean(-1) + 1e-5)).transpose(1, 2)[..., None]
+        check(name + "n", y, ry, ry.abs() * h + amp * r * e)
+        check("d" + name, dx, rdx, rdx.abs() * h + mag.amax(-1, keepdim=True) * e * 2)
+        if w is None:
+            assert dw is None
+        else:
+            if not per_head:
+                rdw, wmag = rdw.sum(0), wmag.sum(0)
+            check("dw" + name, dw, rdw, wmag.max() * (e + B * n * H * u) + rdw.abs() * u)
+
+
+def paged_setup(lens, new, H, Hkv, d, page, dtype, seed=0, extra=2):
+    B = len(lens)
+    width = max(1, max(-(-x // page) for x in lens)) + 1
+    pages = B * width + extra
+    perm = torch.randperm(pages, generator=torch.Generator().manual_seed(seed))[:B * width].view(B, width)
+    cu = [0]
+    for x in new:
+        cu.append(cu[-1] + x)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    kc, vc = (torch.full((pages, page, Hkv, d), float("nan"), dtype=dtype) for _ in range(2))
+    K = [rnd(seed + 3 * b + 1, 1, Hkv, lens[b], d, dtype=dtype) for b in range(B)]
+    V = [rnd(seed + 3 * b + 2, 1, Hkv, lens[b], d, dtype=dtype) for b in range(B)]
+    for b in range(B):
+        for p in range(lens[b]):
+            kc[perm[b, p // page], p % page] = K[b][0, :, p]
+            vc[perm[b, p // page], p % page] = V[b][0, :, p]
+    q = rnd(seed + 99, cu[-1] + extra, H, d, dtype=dtype)
+    return q.to(DEV), kc.to(DEV), vc.to(DEV), i32(perm.tolist()), i32(lens), i32(cu), K, V, cu
+
+
+PAGED = [
+    # lens, new, H, Hkv, d, page, options
+    ([1], [1], 1, 1, 64, 16, {}),
+    ([40, 1, 300], [1, 1, 1], 4, 1, 128, 16, {}),
+    ([130, 7, 65, 257], [1, 1, 1, 1], 8, 2, 64, 24, dict(window=50, sinks=3)),
+    ([600], [1], 16, 2, 128, 1, dict(window=64, sinks=1)),
+    ([70, 200, 5], [70, 33, 5], 4, 2, 128, 7, {}),
+    ([300, 90], [200, 1], 6, 2, 80, 16, dict(window=40, sinks=70)),
+    ([64, 0, 128], [3, 0, 128], 5, 1, 96, 32, {}),
+    ([100, 31], [4, 31], 2, 2, 256, 64, dict(window=20)),
+    ([3, 10], [5, 2], 2, 1, 64, 4, {}),                  # more new tokens than the sequence holds
+    ([1500], [1], 4, 4, 64, 128, dict(scale=0.2)),
+    ([50, 60], [1, 1], 2, 1, 64, 16, dict(window=0)),
+    ([900, 2000], [130, 257], 8, 4, 64, 128, dict(window=300, sinks=5)),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("i", range(len(PAGED)))
+def test_paged_attention_matches_the_formula(i, dtype):
+    lens, new, H, Hkv, d, page, opt = PAGED[i]
+    q, kc, vc, table, ln, cu_new, K, V, cu = paged_setup(lens, new, H, Hkv, d, page, dtype, seed=100 * i)
+    out = torch.full_like(q, 7.0)
+    print(f"[gpu] paged {PAGED[i]} {dtype}", flush=True)
+    P.paged_attention(q, kc, vc, table, ln, cu_new, out=out, **opt)
+    torch.cuda.synchronize()
+    for b in range(len(lens)):
+        if not new[b]:
+            continue
+        qb = q[cu[b]:cu[b + 1]].transpose(0, 1)[None].cpu()
+        want, tol = attention(qb, K[b], V[b], q_start=lens[b] - new[b], **opt)
+        check(f"sequence {b}", out[cu[b]:cu[b + 1]].transpose(0, 1)[None], want["o"], tol["o"])
+    assert bool((out[cu[-1]:] == 7.0).all())               # rows of no sequence
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("lens,new,Hkv,d,page", [([1], [1], 1, 8, 1), ([40, 17, 64], [1, 17, 30], 2, 128, 16),
+                                                 ([5, 9], [0, 9], 3, 80, 7), ([3], [6], 1, 64, 4)])
+def test_paged_append_writes_the_slots_and_nothing_else(lens, new, Hkv, d, page, dtype):
+    q, kc, vc, table, ln, cu_new, _, _, cu = paged_setup(lens, new, Hkv, Hkv, d, page, dtype, seed=5)
+    k, v = rnd(1, cu[-1] + 2, Hkv, d, dtype=dtype).to(DEV), rnd(2, cu[-1] + 2, Hkv, d, dtype=dtype).to(DEV)
+    kw, vw = torch.nan_to_num(kc, nan=3.0), torch.nan_to_num(vc, nan=3.0)
+    kc, vc = kw.clone(), vw.clone()
+    for b in range(len(lens)):
+        for x in range(new[b]):
+            p = lens[b] - new[b] + x
+            if p >= 0:
+                kw[table[b, p // page].item(), p % page] = k[cu[b] + x]
+                vw[table[b, p // page].item(), p % page] = v[cu[b] + x]
+    P.paged_append(k, v, kc, vc, table, ln, cu_new)
+    torch.cuda.synchronize()
+    assert torch.equal(kc, kw) and torch.equal(vc, vw)
