@@ -33,7 +33,6 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kTiny = 1.17549435e-38f;       // least normal fp32 (and bf16)
 constexpr uint32_t kBufOOB = 0x80000000u;      // a raw buffer offset past every range: loads zeros
 constexpr int kBufFlags = 0x00020000;
 
@@ -109,116 +108,166 @@ template <> struct RowsB<float> {
   __device__ __forceinline__ explicit RowsB(const f32x16& s) : v(s) {}
 };
 
-// The two 16-bit halves of a dword: whether they are infinite or NaN, +inf or
-// NaN (`sign` 0), -inf or NaN (`sign` 0x8000), as 0 / 1.0 in bf16.
-__device__ __forceinline__ uint32_t bf16_nonfinite(uint32_t x) {
-  return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-}
-__device__ __forceinline__ uint32_t bf16_finite_or_zero(uint32_t x) {
-  const uint32_t lo = (x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu;
-  const uint32_t hi = (x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u;
-  return lo | hi;
-}
-__device__ __forceinline__ uint32_t bf16_one_if(uint32_t x, uint32_t sign) {
-  uint32_t r = 0;
-#pragma unroll
-  for (int s = 0; s < 32; s += 16) {
-    const uint32_t h = (x >> s) & 0xffffu, mag = h & 0x7fffu;
-    if (mag > 0x7f80u || (mag == 0x7f80u && (h & 0x8000u) == sign)) r |= 0x3f80u << s;
-  }
-  return r;
-}
-__device__ __forceinline__ uint32_t bf16_one_if_nonzero(uint32_t x) {
-  return ((x & 0x7fffu) ? 0x3f80u : 0u) | ((x & 0x7fff0000u) ? 0x3f800000u : 0u);
-}
+// What stands at a masked place must not reach an output, but zero times an
+// infinity or NaN is NaN, and a weight of zero is how a masked pair enters the
+// second products. Such values are rare: tiles at the edge of some query's
+// view are looked through once they are in LDS, and one that holds any is
+// scrubbed there (infinities and NaN become zeros); what they amount to is
+// then given to the pairs that are visible.
 
-// Infinities that the products of one block are known to hold.
-__device__ __forceinline__ void add_infinities(f32x16& acc, const f32x16& plus, const f32x16& minus) {
+// A chunk of 16 bytes of T: whether it holds an infinity or NaN, and the
+// chunk without them.
+template <typename T>
+__device__ __forceinline__ bool nonfinite(const u32x4& x) {
+  uint32_t bad = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    if (plus[i] > 0.0f) acc[i] += __builtin_inff();
-    if (minus[i] > 0.0f) acc[i] += neg_inf();
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) bad |= (x[i] & 0x7f807f80u) + 0x00800080u;   // carries into the sign bits
+    else bad |= (x[i] & 0x7f800000u) + 0x00800000u;
   }
+  return bad & (sizeof(T) == 2 ? 0x80008000u : 0x80000000u);
 }
-
-// acc (32 columns d x 32 columns of b) += (rows rb .. rb + 31, columns
-// 32 db ..  of the tile)^T x b.
-//
-// MASKED (b has weights that are zero because their pair is masked): a zero
-// weight drops its product, so an infinity or NaN that stands in a masked
-// place reaches no output; products with a non-zero weight are as in IEEE
-// arithmetic (an infinity stays one, NaN stays NaN). Such values are rare:
-// they are looked for, and only then the slower form runs, which multiplies
-// them as zeros and then adds what they amount to (+inf, -inf, or both for
-// NaN) wherever a non-zero weight meets them.
-template <typename T, int DP, bool MASKED>
-__device__ __forceinline__ void mma_rows(f32x16& acc, const RowsB<T>& b, const uint8_t* tile, int rb, int db) {
-  using L = Tile<T, DP>;
-  const int lane = threadIdx.x & 63, half = lane >> 5;
+template <typename T>
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t x) {
   if constexpr (sizeof(T) == 2) {
-    const int g = (lane >> 4) & 1, sl = lane & 15;
-    const int chunk = 4 * db + 2 * g + ((sl >> 1) & 1);
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int r0 = rb + 16 * s + 4 * half + (sl >> 2), r1 = r0 + 8;
-      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                     (lds_s16x4*)(tile + L::off(r0, chunk) + ((sl & 1) << 3))));
-      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                     (lds_s16x4*)(tile + L::off(r1, chunk) + ((sl & 1) << 3))));
-      u32x4 a = {lo[0], lo[1], hi[0], hi[1]};
-      if constexpr (MASKED) {
-        const uint32_t bad =
-            bf16_nonfinite(a[0]) | bf16_nonfinite(a[1]) | bf16_nonfinite(a[2]) | bf16_nonfinite(a[3]);
-        if (__builtin_expect(__any(bad != 0), 0)) {
-          u32x4 w, ap, am;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            w[i] = bf16_one_if_nonzero(b.v[s][i]);
-            ap[i] = bf16_one_if(a[i], 0u);
-            am[i] = bf16_one_if(a[i], 0x8000u);
-            a[i] = bf16_finite_or_zero(a[i]);
-          }
-          f32x16 plus = {}, minus = {};
-          mma_chunk<T>(plus, ap, w);
-          mma_chunk<T>(minus, am, w);
-          add_infinities(acc, plus, minus);
-        }
-      }
-      mma_chunk<T>(acc, a, b.v[s]);
-    }
+    const uint32_t lo = (x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu;
+    const uint32_t hi = (x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u;
+    return lo | hi;
   } else {
-    const int col = 32 * db + (lane & 31);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int row = rb + 8 * (i >> 2) + 4 * half + (i & 3);
-      float a = *reinterpret_cast<const float*>(tile + L::off(row, col >> 2) + ((col & 3) << 2));
-      if constexpr (MASKED) {
-        const bool bad = !(fabsf(a) < __builtin_inff());
-        if (__builtin_expect(__any(bad), 0)) {
-          const float w = b.v[i] != 0.0f ? 1.0f : 0.0f, inf = __builtin_inff();
-          f32x16 plus = {}, minus = {};
-          plus = __builtin_amdgcn_mfma_f32_32x32x2f32(bad && a != -inf ? 1.0f : 0.0f, w, plus, 0, 0, 0);
-          minus = __builtin_amdgcn_mfma_f32_32x32x2f32(bad && a != inf ? 1.0f : 0.0f, w, minus, 0, 0, 0);
-          add_infinities(acc, plus, minus);
-          if (bad) a = 0.0f;
-        }
-      }
-      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a, b.v[i], acc, 0, 0, 0);
-    }
+    return (x & 0x7f800000u) == 0x7f800000u ? 0u : x;
   }
 }
 
-// acc (32 rows of the tile from rb x 32 columns of b) = rows . b over d; b
+// LDS fragments of 16-bit tiles are read in batches, each with its wait in the
+// same asm statement: the compiler would drain the copies in flight to the
+// other stage before every read that it can see, since it cannot tell the
+// stages apart. The waves of a SIMD cover each other's waits.
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  typedef __attribute__((address_space(3))) const void lds_cvoid;
+  return (uint32_t)(uintptr_t)(lds_cvoid*)p;
+}
+template <int OFF>
+__device__ __forceinline__ void read_rows4(u32x4 (&r)[4], const uint32_t (&a)[4]) {
+  asm volatile(
+      "ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%8\n\t"
+      "ds_read_b128 %2, %6 offset:%8\n\tds_read_b128 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+      : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(OFF)
+      : "memory");
+}
+template <int OFF>
+__device__ __forceinline__ void read_rows8(u32x4 (&r)[8], const uint32_t (&a)[8]) {
+  asm volatile(
+      "ds_read_b128 %0, %8 offset:%16\n\tds_read_b128 %1, %9 offset:%16\n\t"
+      "ds_read_b128 %2, %10 offset:%16\n\tds_read_b128 %3, %11 offset:%16\n\t"
+      "ds_read_b128 %4, %12 offset:%16\n\tds_read_b128 %5, %13 offset:%16\n\t"
+      "ds_read_b128 %6, %14 offset:%16\n\tds_read_b128 %7, %15 offset:%16\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+      : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(a[4]), "v"(a[5]), "v"(a[6]), "v"(a[7]), "n"(OFF)
+      : "memory");
+}
+// Column fragments of two 32-column blocks and both 16-row steps: r[4 b + 2 s]
+// rows 16 s + 4 half + 0..3, r[4 b + 2 s + 1] the rows 8 further (lo, hi: the
+// lane's addresses of the two in each block).
+template <int OFF, int STEP>
+__device__ __forceinline__ void read_cols2(u32x2 (&r)[8], const uint32_t (&lo)[2], const uint32_t (&hi)[2]) {
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %9 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %2, %8 offset:%13\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+      "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %11 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %6, %10 offset:%13\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+      : "v"(lo[0]), "v"(hi[0]), "v"(lo[1]), "v"(hi[1]), "n"(OFF), "n"(OFF + STEP)
+      : "memory");
+}
+
+// acc (32 rows of the tile from RB x 32 columns of b) = rows . b over d; b
 // holds a lane's column as Tile::KS chunks.
-template <typename T, int DP>
-__device__ __forceinline__ void mma_dot(f32x16& acc, const uint8_t* tile, int rb, const u32x4 (&b)[(Tile<T, DP>::KS)]) {
+template <typename T, int DP, int RB>
+__device__ __forceinline__ void mma_dot(f32x16& acc, const uint8_t* tile, const u32x4 (&b)[(Tile<T, DP>::KS)]) {
   using L = Tile<T, DP>;
   const int lane = threadIdx.x & 63;
   acc = f32x16{};
+  if constexpr (sizeof(T) == 2) {
+    constexpr int N = L::KS < 8 ? 4 : 8;
+    // chunk 2c + half of the row: the lane's first address with bits 5 and up of c flipped in
+    const uint32_t a0 = lds_addr(tile) + L::off(lane & 31, lane >> 5);
 #pragma unroll
-  for (int c = 0; c < L::KS; ++c)
-    mma_chunk<T>(acc, L::row_chunk(tile, rb + (lane & 31), 2 * c + (lane >> 5)), b[c]);
+    for (int c = 0; c < L::KS; c += N) {
+      uint32_t a[N];
+      u32x4 r[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) a[i] = a0 ^ (uint32_t)((c + i) << 5);
+      if constexpr (N == 4) read_rows4<RB * L::PITCH>(r, a);
+      else read_rows8<RB * L::PITCH>(r, a);
+#pragma unroll
+      for (int i = 0; i < N; ++i) mma_chunk<T>(acc, r[i], b[c + i]);
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < L::KS; ++c)
+      mma_chunk<T>(acc, L::row_chunk(tile, RB + (lane & 31), 2 * c + (lane >> 5)), b[c]);
+  }
+}
+
+// acc[0 .. NB) (32-column blocks db0 .. of d x 32 columns of b) += (rows RB ..
+// RB + 31 of the tile)^T x b.
+template <typename T, int DP, int NB, int RB>
+__device__ __forceinline__ void mma_rows(f32x16 (&acc)[NB], const RowsB<T>& b, const uint8_t* tile, int db0) {
+  using L = Tile<T, DP>;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  if constexpr (sizeof(T) == 2) {
+    static_assert(NB % 2 == 0, "column blocks are read in pairs");
+    const int g = (lane >> 4) & 1, sl = lane & 15, row = 4 * half + (sl >> 2), chunk = 2 * g + ((sl >> 1) & 1);
+    const uint32_t base = lds_addr(tile) + ((sl & 1) << 3);
+    const uint32_t a0 = base + L::off(row, chunk), a1 = base + L::off(row + 8, chunk);
+#pragma unroll
+    for (int x = 0; x < NB; x += 2) {
+      uint32_t lo[2], hi[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        lo[y] = a0 ^ (uint32_t)((db0 + x + y) << 6);
+        hi[y] = a1 ^ (uint32_t)((db0 + x + y) << 6);
+      }
+      u32x2 r[8];
+      read_cols2<RB * L::PITCH, 16 * L::PITCH>(r, lo, hi);
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const u32x2 p = r[4 * y + 2 * s], q = r[4 * y + 2 * s + 1];
+          mma_chunk<T>(acc[x + y], u32x4{p[0], p[1], q[0], q[1]}, b.v[s]);
+        }
+    }
+  } else {
+#pragma unroll
+    for (int x = 0; x < NB; ++x) {
+      const int col = 32 * (db0 + x) + (lane & 31);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int row = RB + 8 * (i >> 2) + 4 * half + (i & 3);
+        const float a = *reinterpret_cast<const float*>(tile + L::off(row, col >> 2) + ((col & 3) << 2));
+        acc[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, b.v[i], acc[x], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// The infinities and NaN of a scrubbed row (d elements in memory), added to
+// the lane's column of acc where its query (or key) sees the row: the product
+// with any weight above zero.
+template <typename T, int NB>
+__device__ __forceinline__ void add_nonfinite(f32x16 (&acc)[NB], const T* row, bool see, int d0, int d) {
+  const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int db = 0; db < NB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int e = d0 + 32 * db + 8 * (i >> 2) + 4 * half + (i & 3);
+      if (!see || e >= d) continue;
+      const float x = (float)row[e];
+      if (!(fabsf(x) < __builtin_inff())) acc[db][i] += x;
+    }
 }
 
 // One lane's row (16-byte chunks 2c + lane / 32) of a matrix in memory, zeros
@@ -234,32 +283,65 @@ __device__ __forceinline__ void load_row(u32x4 (&r)[(Tile<T, DP>::KS)], const T*
   }
 }
 
-// A tile of R rows on its way from memory to LDS through the registers of NT
-// threads, 16 bytes a time along the rows: the loads of the next tile are
-// issued before the products of the present one and stored after them.
+// A tile of R rows copied from memory to LDS by the NT threads of a
+// workgroup, 16 bytes a lane and without registers between (each wave
+// instruction fills 1 KiB in order; the swizzle is in the source addresses).
+// The copies are done when vmcnt is 0 (a __syncthreads waits for it).
 template <typename T, int DP, int R, int NT>
-struct Stage {
+struct Copy {
   using L = Tile<T, DP>;
   static constexpr int N = R * L::CPR / NT;     // chunks per thread
   static constexpr int STEP = NT / L::CPR;      // rows between them
   static_assert(N >= 1 && R * L::CPR % NT == 0 && NT % L::CPR == 0, "tile split");
-  u32x4 r[N];
+  typedef __attribute__((address_space(3))) void lds_void;
 
   // rows of `ld` bytes from `base` (the same in all threads), `rows` of them
   // (<= 0: none); the rest, and columns past d, are zeros
-  __device__ __forceinline__ void load(const T* base, int ld, int64_t rows, int d) {
-    const int row = threadIdx.x % NT / L::CPR, c = threadIdx.x % L::CPR;
-    const int n = (int)(rows < R ? rows : R);
+  static __device__ __forceinline__ void rows(uint8_t* tile, const T* base, int ld, int64_t rows, int d) {
+    const int tid = threadIdx.x, n = (int)(rows < R ? rows : R);
     const int span = n > 0 ? (n - 1) * ld + d * (int)sizeof(T) : 0;
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, span, kBufFlags);
-    const uint32_t o = c * L::E < d ? (uint32_t)(row * ld + c * 16) : kBufOOB;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
-    for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, o + (uint32_t)(i * STEP * ld), 0, 0);
+    for (int i = 0; i < N; ++i) {
+      const int row = tid / L::CPR + i * STEP, c = (tid % L::CPR) ^ L::swz(row);
+      const uint32_t o = c * L::E < d ? (uint32_t)(row * ld + c * 16) : kBufOOB;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (i * NT + wave * 64) * 16), 16, o, 0, 0, 0);
+    }
   }
-  __device__ __forceinline__ void store(uint8_t* tile) const {
-    const int row = threadIdx.x % NT / L::CPR, c = threadIdx.x % L::CPR;
+  // this thread's part of a tile in LDS: whether it holds an infinity or NaN, and without them
+  static __device__ __forceinline__ bool any_nonfinite(const uint8_t* tile) {
+    bool bad = false;
 #pragma unroll
-    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(tile + L::off(row + i * STEP, c)) = r[i];
+    for (int i = 0; i < N; ++i) bad |= nonfinite<T>(*reinterpret_cast<const u32x4*>(tile + (i * NT + threadIdx.x) * 16));
+    return bad;
+  }
+  // whether tile x holds an infinity or NaN, by the whole workgroup with a
+  // barrier; `found`: a word of LDS, -1 at first
+  static __device__ __forceinline__ bool holds_nonfinite(const uint8_t* tile, int x, int* found) {
+    if (any_nonfinite(tile)) *found = x;
+    __syncthreads();
+    return *found == x;
+  }
+  // scrubs the tile; the rows that held one, a bit each (`mask`: two words of
+  // LDS). By the whole workgroup, with barriers before and after.
+  static __device__ __forceinline__ uint64_t scrub(uint8_t* tile, uint32_t* mask) {
+    if (threadIdx.x < 2) mask[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+      const int at = i * NT + threadIdx.x, row = at / L::CPR;
+      u32x4 x = *reinterpret_cast<const u32x4*>(tile + at * 16);
+      if (!nonfinite<T>(x)) continue;
+      atomicOr(&mask[row >> 5], 1u << (row & 31));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = finite_or_zero<T>(x[k]);
+      *reinterpret_cast<u32x4*>(tile + at * 16) = x;
+    }
+    __syncthreads();
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(mask[0]), hi = __builtin_amdgcn_readfirstlane(mask[1]);
+    __syncthreads();
+    return ((uint64_t)hi << 32) | lo;
   }
 };
 
@@ -314,10 +396,10 @@ struct Softmax {
     l = 0.0f;
   }
   __device__ __forceinline__ void grow(float mx) {
-    if (!__any(mx > m + 8.0f)) return;
-    const float mn = fmaxf(m, mx);
-    const float f = mn == m ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-    m = mn;
+    const bool up = mx > m + 8.0f;   // by lane: a row's result does not depend on its neighbours'
+    if (!__any(up)) return;
+    const float f = up ? __builtin_amdgcn_exp2f(m - mx) : 1.0f;
+    m = up ? mx : m;
     l *= f;
 #pragma unroll
     for (int i = 0; i < NB; ++i)
@@ -326,45 +408,49 @@ struct Softmax {
   }
 };
 
-// One tile of KT keys: scores, weights, and their products with the values.
-// see(j) says whether the lane's query sees key j of the tile (MASKED).
-template <typename T, int DP, int KT, bool MASKED, class See>
-__device__ __forceinline__ void softmax_tile(Softmax<DP / 32>& st, const u32x4 (&q)[(Tile<T, DP>::KS)], const uint8_t* kt,
-                                             const uint8_t* vt, float c, See&& see) {
-  constexpr int MB = KT / 32;
-  const int half = (threadIdx.x >> 5) & 1;
-  f32x16 s[MB];
+// What a lane's query sees of a tile: rows r with r - lo <= span (unsigned) or
+// r < sink, r counted from the tile's first key plus 4 (lane / 32).
+struct Sight {
+  int lo, sink;
+  uint32_t span;
+  bool sinks;    // whether the tile holds sinks (the same in all lanes)
+  template <class Args>
+  __device__ __forceinline__ Sight(const Args& a, int p, int jhi, int k0) {
+    const int at = k0 + 4 * (int)((threadIdx.x >> 5) & 1), jlo = p - a.win + 1;
+    lo = jhi < jlo ? (1 << 30) : jlo - at;
+    span = (uint32_t)max(jhi - jlo, 0);
+    sinks = k0 < a.sinks;
+    sink = min(a.sinks, jhi + 1) - at;
+  }
+  __device__ __forceinline__ bool see(int r) const { return (uint32_t)(r - lo) <= span || (sinks && r < sink); }
+};
+
+// The 32 keys of a tile from row RB: scores, weights, and their products with
+// the values. see(r) says whether the lane's query sees row r + 4 (lane / 32)
+// (`masked`, the same in all lanes; else it sees all of them).
+template <typename T, int DP, int RB, class See>
+__device__ __forceinline__ void softmax_step(Softmax<DP / 32>& st, const u32x4 (&q)[(Tile<T, DP>::KS)],
+                                             const uint8_t* kt, const uint8_t* vt, float c, bool masked, See&& see) {
+  f32x16 s;
+  mma_dot<T, DP, RB>(s, kt, q);
+  if (masked) {
 #pragma unroll
-  for (int b = 0; b < MB; ++b) mma_dot<T, DP>(s[b], kt, 32 * b, q);
+    for (int i = 0; i < 16; ++i)
+      if (!see(RB + 8 * (i >> 2) + (i & 3))) s[i] = neg_inf();
+  }
   float mx = neg_inf();
 #pragma unroll
-  for (int b = 0; b < MB; ++b)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if constexpr (MASKED)
-        if (!see(32 * b + 8 * (i >> 2) + 4 * half + (i & 3))) s[b][i] = neg_inf();
-      mx = fmaxf(mx, s[b][i]);
-    }
+  for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i]);
   st.grow(half_max(mx) * c);
   const float m = st.m == neg_inf() ? 0.0f : st.m;   // a query that has seen nothing: weights of 0, not NaN
   float sum = 0.0f;
 #pragma unroll
-  for (int b = 0; b < MB; ++b)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -m));
-      // a visible weight stays above zero, which is what marks a masked one
-      if constexpr (MASKED) p = p < kTiny && s[b][i] != neg_inf() ? kTiny : p;
-      s[b][i] = p;
-      sum += p;
-    }
-  st.l += sum;
-#pragma unroll
-  for (int b = 0; b < MB; ++b) {
-    const RowsB<T> w(s[b]);
-#pragma unroll
-    for (int db = 0; db < DP / 32; ++db) mma_rows<T, DP, MASKED>(st.o[db], w, vt, 32 * b, db);
+  for (int i = 0; i < 16; ++i) {
+    s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -m));
+    sum += s[i];
   }
+  st.l += sum;
+  mma_rows<T, DP, DP / 32, RB>(st.o, RowsB<T>(s), vt, 0);
 }
 
 // The band of an attention is args.win, .look and .sinks: position p sees key j

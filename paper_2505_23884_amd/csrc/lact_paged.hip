@@ -101,6 +101,19 @@ struct PagedStage {
       v[i] = ok ? *reinterpret_cast<const u32x4*>(vb + o + e) : u32x4{};
     }
   }
+  // an infinity or NaN among the values; the values without them
+  __device__ __forceinline__ bool any_nonfinite() const {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) bad |= nonfinite<T>(v[i]);
+    return bad;
+  }
+  __device__ __forceinline__ void scrub() {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) v[i][x] = finite_or_zero<T>(v[i][x]);
+  }
   __device__ __forceinline__ void store(uint8_t* kt, uint8_t* vt) const {
     const int row = threadIdx.x % NT / L::CPR, c = threadIdx.x % L::CPR;
 #pragma unroll
@@ -114,6 +127,17 @@ struct PagedStage {
 __device__ __forceinline__ void wave_fence() {   // LDS of one wave: its instructions run in order
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
+}
+
+// The infinities and NaN of a scrubbed tile (offsets `at` of its keys, a lane
+// each) to the rows that see them.
+template <typename T, int DP, class See>
+__device__ __forceinline__ void restore_nonfinite(Softmax<DP / 32>& st, const T* vb, int64_t at, int d, See&& see) {
+#pragma unroll 1
+  for (int j = 0; j < kKT; ++j) {
+    const int64_t o = shfl64(at, j);
+    if (o >= 0) add_nonfinite<T, DP / 32>(st.o, vb + o, see(j - 4 * (int)((threadIdx.x >> 5) & 1)), 0, d);
+  }
 }
 
 // What a workgroup and its lane work on.
@@ -169,38 +193,50 @@ __global__ __launch_bounds__(64 * kWaves) void k_paged_wide(const PagedArgs a) {
   Softmax<DP / 32> st;
   st.init();
   const float c = a.scale * kLog2e;
-  const int jlo = row.p - a.win + 1, jhi = row.ok ? row.p : -1;
+  const int jhi = row.ok ? row.p : -1;
   PagedStage<T, DP, NT> sg;
   // slots run two tiles ahead of the products, the loads one
-  auto slot = [&](int x) { return x < x1 && lane < kKT ? slot_of(a, table, kt.tile(x) * kKT + lane, s.len) : -1; };
-  int64_t at = slot(x0);
-  uint32_t there = (uint32_t)__ballot(at >= 0), there_next = 0;
+  auto slot = [&](int x) __attribute__((always_inline)) { return x < x1 && lane < kKT ? slot_of(a, table, kt.tile(x) * kKT + lane, s.len) : -1; };
+  const int pa = s.p0 + r0 / a.G, pb = s.p0 + rl / a.G;
+  bool scrubbed = false;
+  // the tile that was loaded into LDS for all waves
+  auto store = [&](int x, uint8_t* to, uint32_t whole) __attribute__((always_inline)) {
+    const bool edge = whole != 0xffffffffu || sees(a, s.len, pa, pb, kt.tile(x) * kKT, kKT) != 2;
+    const bool bad = edge && sg.any_nonfinite();
+    if (__builtin_expect(bad, 0)) sg.scrub();
+    sg.store(to, to + BYTES);
+    if (edge) {
+      scrubbed = __syncthreads_or(bad);
+    } else {
+      scrubbed = false;
+      __syncthreads();
+    }
+  };
+  int64_t at = slot(x0), here = at;
+  uint32_t there = (uint32_t)__ballot(at >= 0);
   if (x0 < x1) {
     sg.load(kb, vb, at, a.d);
     at = slot(x0 + 1);
-    sg.store(smem, smem + BYTES);
+    store(x0, smem, there);
   }
-  __syncthreads();
   for (int x = x0; x < x1; ++x) {
-    uint8_t* ks = smem + ((x - x0) & 1) * 2 * BYTES;
-    uint8_t* kn = smem + ((x - x0 + 1) & 1) * 2 * BYTES;
-    there_next = (uint32_t)__ballot(at >= 0);
+    const uint8_t* ks = smem + ((x - x0) & 1) * 2 * BYTES;
+    const uint32_t there_next = (uint32_t)__ballot(at >= 0);
+    const int64_t next = at;
     if (x + 1 < x1) {
       sg.load(kb, vb, at, a.d);
       at = slot(x + 2);
     }
     const int k0 = kt.tile(x) * kKT;
     const int what = sees(a, s.len, wa, wb, k0, kKT);
-    if (what == 2 && there == 0xffffffffu)
-      softmax_tile<T, DP, kKT, false>(st, q, ks, ks + BYTES, c, [](int) { return true; });
-    else if (what)
-      softmax_tile<T, DP, kKT, true>(st, q, ks, ks + BYTES, c, [&](int j) {
-        const int key = k0 + j;
-        return key <= jhi && (key >= jlo || key < a.sinks) && ((there >> j) & 1);
-      });
-    if (x + 1 < x1) sg.store(kn, kn + BYTES);
+    const Sight sight(a, row.p, jhi, k0);
+    const uint32_t mine = there >> (4 * (lane >> 5));
+    auto see = [&](int r) __attribute__((always_inline)) { return sight.see(r) && (mine >> r & 1); };
+    if (what) softmax_step<T, DP, 0>(st, q, ks, ks + BYTES, c, what == 1 || there != 0xffffffffu, see);
+    if (__builtin_expect(scrubbed, 0)) restore_nonfinite<T, DP>(st, vb, here, a.d, see);
+    if (x + 1 < x1) store(x + 1, smem + ((x - x0 + 1) & 1) * 2 * BYTES, there_next);
     there = there_next;
-    __syncthreads();
+    here = next;
   }
   finish<T, DP>(a, row, split, st);
 }
@@ -209,7 +245,7 @@ template <typename T, int DP>
 __global__ __launch_bounds__(64 * kWaves) void k_paged_narrow(const PagedArgs a) {
   using L = Tile<T, DP>;
   constexpr int BYTES = kKT * L::PITCH, JOIN = 32 * (DP + 2) * 4;   // a wave's sums, when they are joined
-  constexpr int WAVE = 2 * BYTES > JOIN ? 2 * BYTES : JOIN;
+  constexpr int WAVE = ((2 * BYTES > JOIN ? 2 * BYTES : JOIN) + 1023) / 1024 * 1024;   // tiles start at multiples of their pitch
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kWaves * WAVE];
   Seq s;
   int r0;
@@ -229,34 +265,30 @@ __global__ __launch_bounds__(64 * kWaves) void k_paged_narrow(const PagedArgs a)
   Softmax<DP / 32> st;
   st.init();
   const float c = a.scale * kLog2e;
-  const int jlo = row.p - a.win + 1, jhi = row.ok ? row.p : -1;
+  const int jhi = row.ok ? row.p : -1;
   uint8_t* ks = smem + wave * WAVE;
   PagedStage<T, DP, 64> sg;
-  auto slot = [&](int x) { return x < x1 && lane < kKT ? slot_of(a, table, kt.tile(x) * kKT + lane, s.len) : -1; };
+  auto slot = [&](int x) __attribute__((always_inline)) { return x < x1 && lane < kKT ? slot_of(a, table, kt.tile(x) * kKT + lane, s.len) : -1; };
   int x = x0 + wave;
   int64_t at = slot(x);
-  uint32_t there = (uint32_t)__ballot(at >= 0);
   if (x < x1) sg.load(kb, vb, at, a.d);
-  at = slot(x + kWaves);
   for (; x < x1; x += kWaves) {
+    const int64_t here = at;
+    const uint32_t there = (uint32_t)__ballot(here >= 0);
+    at = slot(x + kWaves);
+    const int k0 = kt.tile(x) * kKT;
+    const int what = there == 0xffffffffu ? sees(a, s.len, wa, wb, k0, kKT) : 1;
+    const bool scrubbed = what == 1 && __any(sg.any_nonfinite());
+    if (__builtin_expect(scrubbed, 0)) sg.scrub();
     wave_fence();
     sg.store(ks, ks + BYTES);
     wave_fence();
-    const uint32_t here = there;
-    there = (uint32_t)__ballot(at >= 0);
-    if (x + kWaves < x1) {
-      sg.load(kb, vb, at, a.d);
-      at = slot(x + 2 * kWaves);
-    }
-    const int k0 = kt.tile(x) * kKT;
-    const int what = sees(a, s.len, wa, wb, k0, kKT);
-    if (what == 2 && here == 0xffffffffu)
-      softmax_tile<T, DP, kKT, false>(st, q, ks, ks + BYTES, c, [](int) { return true; });
-    else if (what)
-      softmax_tile<T, DP, kKT, true>(st, q, ks, ks + BYTES, c, [&](int j) {
-        const int key = k0 + j;
-        return key <= jhi && (key >= jlo || key < a.sinks) && ((here >> j) & 1);
-      });
+    if (x + kWaves < x1) sg.load(kb, vb, at, a.d);
+    const Sight sight(a, row.p, jhi, k0);
+    const uint32_t mine = there >> (4 * (lane >> 5));
+    auto see = [&](int r) __attribute__((always_inline)) { return sight.see(r) && (mine >> r & 1); };
+    if (what) softmax_step<T, DP, 0>(st, q, ks, ks + BYTES, c, what == 1, see);
+    if (__builtin_expect(scrubbed, 0)) restore_nonfinite<T, DP>(st, vb, here, a.d, see);
   }
   // the waves' sums: each lane's [32][DP] and (m, l), added by all threads
   __syncthreads();

@@ -50,6 +50,8 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_fwd(const WindowArgs a)
   using L = Tile<T, DP>;
   constexpr int BYTES = KT * L::PITCH;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BYTES];
+  __shared__ uint32_t mask[2];
+  __shared__ int found;
   const int ntile = (a.n_q + QB - 1) / QB;
   const int w = xcd_order(blockIdx.x, gridDim.x);
   const int bh = w / ntile, qt = ntile - 1 - w % ntile;   // the longest rows of a causal head first
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_fwd(const WindowArgs a)
   const bool live = i <= last;
   const KeyTiles kt(a, len, a.q_start + r0, a.q_start + min(r0 + QB - 1, last), KT);
   const int wa = a.q_start + r0 + 32 * wave, wb = a.q_start + min(r0 + 32 * wave + 31, last);
-  const int jlo = p - a.win + 1, jhi = live ? min(p + a.look, len - 1) : -1;
+  const int jhi = live ? min(p + a.look, len - 1) : -1;
 
   u32x4 q[L::KS];
   load_row<T, DP>(q, row_of<T>(a.q, b, h, min(i, a.n_q - 1)), live, a.d);
@@ -71,34 +73,37 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_fwd(const WindowArgs a)
   const float c = a.scale * kLog2e;
   const int n = kt.count();
   const int ldk = (int)(a.k.st * sizeof(T)), ldv = (int)(a.v.st * sizeof(T));
-  Stage<T, DP, KT, NT> sk, sv;
-  auto load = [&](int x) {
+  using Cp = Copy<T, DP, KT, NT>;
+  auto copy = [&](int x) __attribute__((always_inline)) {
     const int k0 = kt.tile(x) * KT;
-    sk.load(row_of<T>(a.k, b, hk, k0), ldk, len - k0, a.d);
-    sv.load(row_of<T>(a.v, b, hk, k0), ldv, len - k0, a.d);
+    uint8_t* to = smem + (x & 1) * 2 * BYTES;
+    Cp::rows(to, row_of<T>(a.k, b, hk, k0), ldk, len - k0, a.d);
+    Cp::rows(to + BYTES, row_of<T>(a.v, b, hk, k0), ldv, len - k0, a.d);
   };
-  auto store = [&](int stage) {
-    sk.store(smem + stage * 2 * BYTES);
-    sv.store(smem + stage * 2 * BYTES + BYTES);
-  };
-  if (n > 0) {
-    load(0);
-    store(0);
-  }
+  const int pa = a.q_start + r0, pb = a.q_start + min(r0 + QB - 1, last);
+  if (threadIdx.x == 0) found = -1;
+  if (n > 0) copy(0);
   __syncthreads();
   for (int x = 0; x < n; ++x) {
-    const uint8_t* ks = smem + (x & 1) * 2 * BYTES;
-    if (x + 1 < n) load(x + 1);
+    uint8_t* ks = smem + (x & 1) * 2 * BYTES;
     const int k0 = kt.tile(x) * KT;
-    const int what = sees(a, len, wa, wb, k0, KT);
-    if (what == 2)
-      softmax_tile<T, DP, KT, false>(st, q, ks, ks + BYTES, c, [](int) { return true; });
-    else if (what == 1)
-      softmax_tile<T, DP, KT, true>(st, q, ks, ks + BYTES, c, [&](int j) {
-        const int key = k0 + j;
-        return key <= jhi && (key >= jlo || key < a.sinks);
-      });
-    if (x + 1 < n) store((x + 1) & 1);
+    uint64_t bad = 0;   // keys whose values were scrubbed
+    if (sees(a, len, pa, pb, k0, KT) != 2 && __builtin_expect(Cp::holds_nonfinite(ks + BYTES, x, &found), 0))
+      bad = Cp::scrub(ks + BYTES, mask);
+    if (x + 1 < n) copy(x + 1);
+    const Sight sight(a, p, jhi, k0);
+    auto step = [&](auto rb) __attribute__((always_inline)) {
+      constexpr int RB = decltype(rb)::value;
+      const int what = sees(a, len, wa, wb, k0 + RB, 32);
+      if (what) softmax_step<T, DP, RB>(st, q, ks, ks + BYTES, c, what == 1, [&](int r) { return sight.see(r); });
+    };
+    step(std::integral_constant<int, 0>{});
+    if constexpr (KT == 64) step(std::integral_constant<int, 32>{});
+#pragma unroll 1
+    for (; __builtin_expect(bad != 0, 0); bad &= bad - 1) {
+      const int j = __builtin_ctzll(bad);
+      add_nonfinite<T, DP / 32>(st.o, row_of<T>(a.v, b, hk, k0 + j), sight.see(j - 4 * (lane >> 5)), 0, a.d);
+    }
     __syncthreads();
   }
   const float l = half_sum(st.l);
@@ -152,6 +157,8 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
   using L = Tile<T, DP>;
   constexpr int BYTES = KT * L::PITCH;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BYTES];
+  __shared__ uint32_t mask[2];
+  __shared__ int found;
   const int ntile = (a.n_q + QB - 1) / QB;
   const int w = xcd_order(blockIdx.x, gridDim.x);
   const int bh = w / ntile, qt = ntile - 1 - w % ntile;
@@ -164,7 +171,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
   const bool live = i <= last;
   const KeyTiles kt(a, len, a.q_start + r0, a.q_start + min(r0 + QB - 1, last), KT);
   const int wa = a.q_start + r0 + 32 * wave, wb = a.q_start + min(r0 + 32 * wave + 31, last);
-  const int jlo = p - a.win + 1, jhi = live ? min(p + a.look, len - 1) : -1;
+  const int jhi = live ? min(p + a.look, len - 1) : -1;
 
   u32x4 q[L::KS], go[L::KS];
   load_row<T, DP>(q, row_of<T>(a.q, b, h, ic), live, a.d);
@@ -177,53 +184,48 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
   const float c = a.scale * kLog2e;
   const int n = kt.count();
   const int ldk = (int)(a.k.st * sizeof(T)), ldv = (int)(a.v.st * sizeof(T));
-  Stage<T, DP, KT, NT> sk, sv;
-  auto load = [&](int x) {
+  using Cp = Copy<T, DP, KT, NT>;
+  auto copy = [&](int x) __attribute__((always_inline)) {
     const int k0 = kt.tile(x) * KT;
-    sk.load(row_of<T>(a.k, b, hk, k0), ldk, len - k0, a.d);
-    sv.load(row_of<T>(a.v, b, hk, k0), ldv, len - k0, a.d);
+    uint8_t* to = smem + (x & 1) * 2 * BYTES;
+    Cp::rows(to, row_of<T>(a.k, b, hk, k0), ldk, len - k0, a.d);
+    Cp::rows(to + BYTES, row_of<T>(a.v, b, hk, k0), ldv, len - k0, a.d);
   };
-  auto store = [&](int stage) {
-    sk.store(smem + stage * 2 * BYTES);
-    sv.store(smem + stage * 2 * BYTES + BYTES);
-  };
-  auto step = [&](const uint8_t* ks, int k0, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
+  const int pa = a.q_start + r0, pb = a.q_start + min(r0 + QB - 1, last);
+  auto step = [&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad) __attribute__((always_inline)) {
+    constexpr int RB = decltype(rb)::value;
+    f32x16 s, dp;
+    mma_dot<T, DP, RB>(s, ks, q);
+    mma_dot<T, DP, RB>(dp, ks + BYTES, go);
 #pragma unroll
-    for (int mb = 0; mb < KT / 32; ++mb) {
-      f32x16 s, dp;
-      mma_dot<T, DP>(s, ks, 32 * mb, q);
-      mma_dot<T, DP>(dp, ks + BYTES, 32 * mb, go);
+    for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse2)) * (dp[e] - delta);
+    if (masked) {
+      if (__builtin_expect(bad != 0, 0))   // keys that held an infinity or NaN
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float ds = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse2)) * (dp[e] - delta);
-        if constexpr (MASKED) {
-          const int key = k0 + 32 * mb + 8 * (e >> 2) + 4 * half + (e & 3);
-          s[e] = key <= jhi && (key >= jlo || key < a.sinks) ? ds : 0.0f;
-        } else {
-          s[e] = ds;
-        }
-      }
-      const RowsB<T> wb(s);
+        for (int e = 0; e < 16; ++e)
+          if (bad >> (RB + 8 * (e >> 2) + 4 * half + (e & 3)) & 1) s[e] = __builtin_nanf("");
+      const Sight sight(a, p, jhi, k0);
 #pragma unroll
-      for (int db = 0; db < DP / 32; ++db) mma_rows<T, DP, MASKED>(dq[db], wb, ks, 32 * mb, db);
+      for (int e = 0; e < 16; ++e) s[e] = sight.see(RB + 8 * (e >> 2) + (e & 3)) ? s[e] : 0.0f;
     }
+    mma_rows<T, DP, DP / 32, RB>(dq, RowsB<T>(s), ks, 0);
   };
-  using Yes = std::true_type;
-  using No = std::false_type;
-  if (n > 0) {
-    load(0);
-    store(0);
-  }
+  if (threadIdx.x == 0) found = -1;
+  if (n > 0) copy(0);
   __syncthreads();
   for (int x = 0; x < n; ++x) {
-    const uint8_t* ks = smem + (x & 1) * 2 * BYTES;
-    if (x + 1 < n) load(x + 1);
+    uint8_t* ks = smem + (x & 1) * 2 * BYTES;
     const int k0 = kt.tile(x) * KT;
-    const int what = sees(a, len, wa, wb, k0, KT);
-    if (what == 2) step(ks, k0, No{});
-    else if (what == 1) step(ks, k0, Yes{});
-    if (x + 1 < n) store((x + 1) & 1);
+    uint64_t bad = 0;
+    if (sees(a, len, pa, pb, k0, KT) != 2 && __builtin_expect(Cp::holds_nonfinite(ks, x, &found), 0))
+      bad = Cp::scrub(ks, mask);
+    if (x + 1 < n) copy(x + 1);
+    auto part = [&](auto rb) __attribute__((always_inline)) {
+      const int what = sees(a, len, wa, wb, k0 + rb, 32);
+      if (what) step(ks, k0, rb, what == 1 || bad != 0, bad);
+    };
+    part(std::integral_constant<int, 0>{});
+    if constexpr (KT == 64) part(std::integral_constant<int, 32>{});
     __syncthreads();
   }
   store_row<T, DP / 32>(row_of<T>(g.dq, b, h, ic), dq, a.scale, 0, a.d, i < a.n_q, !live);
@@ -263,8 +265,11 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
   const WindowArgs& a = g.f;
   constexpr int KB = 32 * NW, NT = 64 * NW, NB = DO / 32;
   using L = Tile<T, DP>;
-  constexpr int BYTES = QT * L::PITCH, STAGE = 2 * BYTES + 2 * QT * 4;
+  constexpr int BYTES = QT * L::PITCH, STAGE = 2 * BYTES + 1024;   // tiles start at multiples of their pitch
+  static_assert(2 * QT * 4 <= 1024, "lse2 and delta of a step");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE];
+  __shared__ uint32_t mask[2];
+  __shared__ int found;
   const int jobs = g.plan.jobs(), ND = DP / DO;
   const int w = xcd_order(blockIdx.x, gridDim.x);
   const int dsel = w % ND, bk = (w / ND) / jobs, b = bk / a.Hkv, hk = bk % a.Hkv;
@@ -273,9 +278,10 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
   const int kw = job.tile * KB + 32 * wave, j = kw + (lane & 31), jc = min(j, a.n_kv - 1);
   const bool live = j < len;
-  // positions that see key j
-  const int plo = j - a.look, phi = !live ? -1 : (j < a.sinks ? len - 1 : min(len - 1, j + a.win - 1));
   const int iend = min(a.n_q, len - a.q_start);   // queries past it are padding
+  // the queries of the job that see key j
+  const int ilo = max(j - a.look - a.q_start, 0);
+  const int ihi = !live ? -1 : min(job.qb - 1, j < a.sinks ? iend - 1 : min(iend - 1, j + a.win - 1 - a.q_start));
 
   u32x4 kf[L::KS], vf[L::KS];
   load_row<T, DP>(kf, row_of<T>(a.k, b, hk, jc), live, a.d);
@@ -287,84 +293,98 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
   const int steps = job.qb > job.qa ? (job.qb - job.qa + QT - 1) / QT : 0;
   const int gh = a.G / g.plan.gs, n = steps * gh;
   const int ldq = (int)(a.q.st * sizeof(T)), ldo = (int)(g.dout.st * sizeof(T));
-  Stage<T, DP, QT, NT> sq, so;
-  float s_lse = 0.0f, s_delta = 0.0f;
-  auto load = [&](int x) {
+  using Cp = Copy<T, DP, QT, NT>;
+  using Cp2 = Copy<T, DP, 2 * QT, NT>;   // queries and cotangents as one tile
+  typedef __attribute__((address_space(3))) void lds_void;
+  auto copy = [&](int x) __attribute__((always_inline)) {
     const int h = hk * a.G + job.head_part * gh + x / steps, i0 = job.qa + (x % steps) * QT;
-    sq.load(row_of<T>(a.q, b, h, i0), ldq, job.qb - i0, a.d);
-    so.load(row_of<T>(g.dout, b, h, i0), ldo, job.qb - i0, a.d);
-    if ((int)threadIdx.x < QT) {
-      const int i = i0 + threadIdx.x;
-      const int64_t at = ((int64_t)b * a.H + h) * a.n_q + i;
-      s_lse = i < job.qb ? g.lse2[at] : __builtin_inff();
-      s_delta = i < job.qb ? g.delta[at] : 0.0f;
+    uint8_t* to = smem + (x & 1) * STAGE;
+    Cp::rows(to, row_of<T>(a.q, b, h, i0), ldq, job.qb - i0, a.d);
+    Cp::rows(to + BYTES, row_of<T>(g.dout, b, h, i0), ldo, job.qb - i0, a.d);
+    if (wave < 2) {   // lse2 and delta of the queries; past the last one zeros (masked)
+      const float* from = (wave ? g.delta : g.lse2) + ((int64_t)b * a.H + h) * a.n_q + i0;
+      const __amdgpu_buffer_rsrc_t rsrc =
+          __builtin_amdgcn_make_buffer_rsrc((void*)from, (short)0, min(QT, job.qb - i0) * 4, kBufFlags);
+      if (lane < QT)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + 2 * BYTES + wave * QT * 4), 4, lane * 4, 0, 0, 0);
     }
   };
-  auto store = [&](int stage) {
-    uint8_t* s = smem + stage * STAGE;
-    sq.store(s);
-    so.store(s + BYTES);
-    if ((int)threadIdx.x < QT) {
-      reinterpret_cast<float*>(s + 2 * BYTES)[threadIdx.x] = s_lse;
-      reinterpret_cast<float*>(s + 2 * BYTES)[QT + threadIdx.x] = s_delta;
-    }
+  const int kb0 = job.tile * KB, kb1 = kb0 + KB - 1;
+  // queries i0 .. against the keys k0 .. k1: nothing (0), something (1) or all (2)
+  auto seen = [&](int i0, int count, int k0, int k1) __attribute__((always_inline)) {
+    const int pa = a.q_start + i0, pe = a.q_start + min(i0 + count, min(job.qb, iend)) - 1;
+    if (pa > pe || k0 >= len || k0 > pe + a.look || (k0 >= a.sinks && k1 <= pa - a.win)) return 0;
+    return pe - pa == count - 1 && k1 < len && k1 <= pa + a.look && (k0 > pe - a.win || k1 < a.sinks) ? 2 : 1;
   };
-  auto step = [&](const uint8_t* qs, int i0, int rb, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
+  auto step = [&](const uint8_t* qs, int i0, auto rb, bool masked, uint64_t badq, uint64_t bado)
+      __attribute__((always_inline)) {
+    constexpr int RB = decltype(rb)::value;
     const uint8_t* os = qs + BYTES;
-    const float* rows = reinterpret_cast<const float*>(qs + 2 * BYTES) + rb;
     f32x16 s, dp;
-    mma_dot<T, DP>(s, qs, rb, kf);
-    mma_dot<T, DP>(dp, os, rb, vf);
+    mma_dot<T, DP, RB>(s, qs, kf);
+    mma_dot<T, DP, RB>(dp, os, vf);
+    // lse2 and delta of rows 8e + 4 half ..
+    u32x4 rows[8];
+    {
+      const uint32_t at = lds_addr(qs + 2 * BYTES) + RB * 4 + 16 * half;
+      const uint32_t ad[8] = {at, at + 32, at + 64, at + 96, at + 4 * QT, at + 4 * QT + 32, at + 4 * QT + 64, at + 4 * QT + 96};
+      read_rows8<0>(rows, ad);
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const f32x4 ls = *reinterpret_cast<const f32x4*>(rows + 8 * e + 4 * half);
-      const f32x4 dl = *reinterpret_cast<const f32x4*>(rows + QT + 8 * e + 4 * half);
+      const f32x4 ls = __builtin_bit_cast(f32x4, rows[e]), dl = __builtin_bit_cast(f32x4, rows[4 + e]);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int r = 4 * e + u;
-        float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ls[u]));
-        float ds = pr * (dp[r] - dl[u]);
-        if constexpr (MASKED) {
-          const int i = i0 + rb + 8 * e + 4 * half + u, p = a.q_start + i;
-          const bool see = i < job.qb && p >= plo && p <= phi;
-          pr = !see ? 0.0f : pr < kTiny ? kTiny : pr;   // a visible weight stays above zero (mma_rows)
-          ds = see ? ds : 0.0f;
-        }
-        s[r] = pr;
-        dp[r] = ds;
+        s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ls[u]));
+        dp[r] = s[r] * (dp[r] - dl[u]);
       }
     }
-    const RowsB<T> wp(s), wd(dp);
+    if (masked) {
+      if (__builtin_expect((badq | bado) != 0, 0))   // queries, or cotangents, that held an infinity or NaN
 #pragma unroll
-    for (int x = 0; x < NB; ++x) {
-      mma_rows<T, DP, MASKED>(dv[x], wp, os, rb, dsel * NB + x);
-      mma_rows<T, DP, MASKED>(dk[x], wd, qs, rb, dsel * NB + x);
+        for (int e = 0; e < 16; ++e) {
+          const int r = RB + 8 * (e >> 2) + 4 * half + (e & 3);
+          if (badq >> r & 1) s[e] = __builtin_nanf("");
+          if ((badq | bado) >> r & 1) dp[e] = __builtin_nanf("");
+        }
+      // the queries ilo .. ihi see the lane's key
+      const int at = i0 + RB + 4 * half, lo = ihi < ilo ? (1 << 30) : ilo - at;
+      const uint32_t span = (uint32_t)max(ihi - ilo, 0);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const bool see = (uint32_t)(8 * (e >> 2) + (e & 3) - lo) <= span;
+        s[e] = see ? s[e] : 0.0f;
+        dp[e] = see ? dp[e] : 0.0f;
+      }
     }
+    mma_rows<T, DP, NB, RB>(dv, RowsB<T>(s), os, dsel * NB);
+    mma_rows<T, DP, NB, RB>(dk, RowsB<T>(dp), qs, dsel * NB);
   };
-  using Yes = std::true_type;
-  using No = std::false_type;
-  const int kw1 = kw + 31;
-  if (n > 0) {
-    load(0);
-    store(0);
-  }
+  if (threadIdx.x == 0) found = -1;
+  if (n > 0) copy(0);
   __syncthreads();
   for (int x = 0; x < n; ++x) {
-    const uint8_t* qs = smem + (x & 1) * STAGE;
-    if (x + 1 < n) load(x + 1);
+    uint8_t* qs = smem + (x & 1) * STAGE;
     const int i0 = job.qa + (x % steps) * QT;
-#pragma unroll
-    for (int rb = 0; rb < QT; rb += 32) {
-      // the 32 queries against the wave's 32 keys: nothing, something or all
-      const int pa = a.q_start + i0 + rb, pe = a.q_start + min(i0 + rb + 32, min(job.qb, iend)) - 1;
-      const bool none = pa > pe || kw >= len || kw > pe + a.look || (kw >= a.sinks && kw1 <= pa - a.win);
-      const bool all = pe - pa == 31 && kw1 < len && kw1 <= pa + a.look && (kw > pe - a.win || kw1 < a.sinks);
-      if (none) continue;
-      if (all) step(qs, i0, rb, No{});
-      else step(qs, i0, rb, Yes{});
+    uint64_t badq = 0, bado = 0;
+    if (seen(i0, QT, kb0, kb1) != 2 &&
+        __builtin_expect(Cp2::holds_nonfinite(qs, x, &found), 0)) {
+      badq = Cp::scrub(qs, mask);
+      bado = Cp::scrub(qs + BYTES, mask);
     }
-    if (x + 1 < n) store((x + 1) & 1);
+    if (x + 1 < n) copy(x + 1);
+    auto part = [&](auto rb) __attribute__((always_inline)) {
+      const int what = seen(i0 + rb, 32, kw, kw + 31);
+      if (what) step(qs, i0, rb, what == 1 || (badq | bado) != 0, badq, bado);
+    };
+    part(std::integral_constant<int, 0>{});
+    if constexpr (QT == 64) part(std::integral_constant<int, 32>{});
+#pragma unroll 1
+    for (; __builtin_expect(bado != 0, 0); bado &= bado - 1) {   // dv takes the cotangents' infinities and NaN
+      const int i = i0 + __builtin_ctzll(bado), h = hk * a.G + job.head_part * gh + x / steps;
+      add_nonfinite<T, NB>(dv, row_of<T>(g.dout, b, h, i), i >= ilo && i <= ihi, dsel * DO, a.d);
+    }
     __syncthreads();
   }
   if (job.slot < 0) {
@@ -416,7 +436,7 @@ int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 template <typename T, int DP>
 hipError_t fwd(const WindowArgs& a, hipStream_t s) {
-  constexpr int OCC = sizeof(T) == 2 && DP <= 128 ? 2 : 1;
+  constexpr int OCC = sizeof(T) == 4 || DP > 128 ? 1 : DP > 64 ? 2 : 4;
   const int64_t bh = (int64_t)a.B * a.H;
   k_window_fwd<T, DP, 4, OCC><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(a);
   return hipGetLastError();
@@ -432,7 +452,7 @@ hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
     int G = 1;
     while (G < 64 && G * (16 / (int)sizeof(T)) < a.d) G *= 2;
     k_window_delta<T><<<(unsigned)((bh * a.n_q + 256 / G - 1) / (256 / G)), 256, 0, s>>>(g, G);
-    k_window_dq<T, DP, 4, 1><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(g);
+    k_window_dq<T, DP, 4, (H16 && DP <= 128 ? 2 : 1)><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(g);
   }
   if (a.n_kv > 0) {
     k_window_dkv<T, DP, DO, QT, 4><<<(unsigned)(bk * g.plan.jobs() * (DP / DO)), 256, 0, s>>>(g);
@@ -449,14 +469,40 @@ hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
 
 }  // namespace
 
+// Tiles of sinks are seen by every later query, the others by a window of
+// them: the former are cut into parts of about the latter's work, and all of
+// them, by heads first, where the tiles alone would leave CUs idle.
 DkvPlan window_dkv_plan(const WindowArgs& a, bool bf16) {
+  (void)bf16;
   DkvPlan p{};
   p.kb = 128;
   p.ntile = cdiv(a.n_kv, p.kb);
-  p.st = 0;
+  const int n_q = std::max(a.n_q, 1);
+  const int reach = (int)std::min<int64_t>(n_q, (int64_t)a.win + a.look + p.kb);   // queries that see a tile
+  auto parts = [&](int ch, int* np, int* out) {   // parts of about `ch` queries, at most 64
+    *np = std::min(cdiv(n_q, std::max(ch, 1)), 64);
+    *out = cdiv(cdiv(n_q, *np), 64) * 64;
+  };
   p.np_s = p.np_a = p.gs = 1;
-  p.ch_s = p.ch_a = std::max(a.n_q, 1);
-  (void)bf16;
+  p.ch_s = p.ch_a = cdiv(n_q, 64) * 64;
+  const int64_t tiles = (int64_t)a.B * a.Hkv * p.ntile;
+  if (reach < n_q) {
+    p.st = cdiv(std::min(a.sinks, a.n_kv), p.kb);
+    parts(cdiv(reach, 64) * 64, &p.np_s, &p.ch_s);
+  }
+  while (tiles * p.gs < 256 && p.gs < a.G) {
+    int f = 2;
+    while (a.G / p.gs % f) ++f;   // the least factor of what is left of the group
+    p.gs *= f;
+  }
+  if (tiles * p.gs < 128 && reach > 512) {
+    const int want = (int)std::min<int64_t>(256 / (tiles * p.gs), reach / 256);
+    if (want > 1) {
+      p.np_a = want;
+      p.ch_a = cdiv(cdiv(reach, want), 64) * 64;
+      if (p.st) parts(p.ch_a, &p.np_s, &p.ch_s);
+    }
+  }
   return p;
 }
 

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2505_23884_amd as P
-from attention_reference import HALF, attention, check, norm_rope
+from attention_reference import HALF, attention, check, norm_rope, visible
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -75,6 +75,64 @@ def test_window_attention_matches_the_formula(i, dtype):
     torch.cuda.synchronize()
     for name, got in (("dq", dq), ("dk", dk), ("dv", dv)):
         check(name, got, want[name], tol[name])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("n,d,opt", [(150, 64, dict(window=20, sinks=2)), (200, 128, dict(window=70)), (90, 256, {}),
+                                     (130, 64, dict(window=10, lookahead=10)),
+                                     (140, 128, dict(lookahead=None, lengths=[100]))])
+def test_infinities_and_nan_reach_only_what_sees_them(n, d, opt, value, dtype):
+    opt = dict(opt)
+    H, Hkv, at = 2, 1, 75
+    L = opt["lengths"][0] if "lengths" in opt else n
+    q, k, v, do = (rnd(x, 1, h, n, d, dtype=dtype).to(DEV) for x, h in ((0, H), (1, Hkv), (2, Hkv), (3, H)))
+    if "lengths" in opt:
+        opt["lengths"] = torch.tensor(opt["lengths"], dtype=torch.int32, device=DEV)
+    see = visible(n, n, L, 0, opt.get("window"), opt.get("sinks", 0), opt.get("lookahead", 0))
+    o0, lse0 = P.window_attention(q, k, v, with_lse=True, **opt)
+    g0 = P.window_attention_backward(q, k, v, o0, lse0, do, **opt)
+
+    def spoil(x, rows):
+        x = x.clone()
+        x[:, :, rows, 5] = value
+        return x
+
+    def same(name, got, want, rows):      # rows that cannot be reached: bitwise as before
+        assert torch.equal(got[:, :, rows.to(DEV)], want[:, :, rows.to(DEV)]), name
+
+    for rows in ([at], [n - 1] if L < n else [at, 3]):
+        hit_q = see[:, rows].any(1)                 # queries that see such a key
+        hit_k = see[rows].any(0)                    # keys that such a query sees
+        print(f"[gpu] nonfinite n={n} d={d} {opt} {value} rows {rows} {dtype}", flush=True)
+        o, lse = P.window_attention(q, k, spoil(v, rows), with_lse=True, **opt)
+        same("o", o, o0, ~hit_q)
+        assert torch.equal(lse, lse0)
+        assert bool((~torch.isfinite(o[:, :, hit_q.to(DEV), 5].float())).all())
+        if math.isinf(value):
+            assert bool((o[:, :, hit_q.to(DEV), 5] == value).all())
+        o, lse = P.window_attention(q, spoil(k, rows), v, with_lse=True, **opt)
+        same("o of k", o, o0, ~hit_q)
+        dq, dk, dv = P.window_attention_backward(q, spoil(k, rows), v, o, lse, do, **opt)
+        same("dq of k", dq, g0[0], ~hit_q)
+        far = ~see[hit_q].any(0)                    # keys that no such query sees
+        same("dk of k", dk, g0[1], far)
+        same("dv of k", dv, g0[2], far)
+        do2 = spoil(do, rows)
+        dq, dk, dv = P.window_attention_backward(q, k, v, o0, lse0, do2, **opt)
+        rest = torch.ones(n, dtype=torch.bool)
+        rest[rows] = False
+        same("dq of do", dq, g0[0], rest)
+        same("dk of do", dk, g0[1], ~hit_k)
+        same("dv of do", dv, g0[2], ~hit_k)
+        assert bool((~torch.isfinite(dv[:, :, hit_k.to(DEV), 5].float())).all())
+        q2 = spoil(q, rows)
+        o, lse = P.window_attention(q2, k, v, with_lse=True, **opt)
+        same("o of q", o, o0, rest)
+        dq, dk, dv = P.window_attention_backward(q2, k, v, o, lse, do, **opt)
+        same("dq of q", dq, g0[0], rest)
+        same("dk of q", dk, g0[1], ~hit_k)
+        same("dv of q", dv, g0[2], ~hit_k)
 
 
 ROPE = [
