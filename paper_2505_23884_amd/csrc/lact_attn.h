@@ -96,6 +96,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 template <typename T> struct RowsB;
 template <> struct RowsB<__bf16> {
   u32x4 v[2];
+  __device__ __forceinline__ RowsB() {}
   __device__ __forceinline__ explicit RowsB(const f32x16& s) {
 #pragma unroll
     for (int g = 0; g < 2; ++g)
@@ -344,6 +345,81 @@ struct Copy {
     return ((uint64_t)hi << 32) | lo;
   }
 };
+
+// The same through registers: the loads of the next tile are issued before
+// the products of the present one and stored after them. For kernels with
+// registers to spare: plain LDS reads then do not wait for copies in flight.
+template <typename T, int DP, int R, int NT>
+struct Stage {
+  using L = Tile<T, DP>;
+  static constexpr int N = R * L::CPR / NT, STEP = NT / L::CPR;
+  static_assert(N >= 1 && R * L::CPR % NT == 0 && NT % L::CPR == 0, "tile split");
+  u32x4 r[N];
+  __device__ __forceinline__ void load(const T* base, int ld, int64_t rows, int d) {
+    const int row = threadIdx.x / L::CPR, c = threadIdx.x % L::CPR;
+    const int n = (int)(rows < R ? rows : R);
+    const int span = n > 0 ? (n - 1) * ld + d * (int)sizeof(T) : 0;
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, span, kBufFlags);
+    const uint32_t o = c * L::E < d ? (uint32_t)(row * ld + c * 16) : kBufOOB;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, o + (uint32_t)(i * STEP * ld), 0, 0);
+  }
+  __device__ __forceinline__ void store(uint8_t* tile) const {
+    const int row = threadIdx.x / L::CPR, c = threadIdx.x % L::CPR;
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(tile + L::off(row + i * STEP, c)) = r[i];
+  }
+};
+
+// Plain fragment reads of a 16-bit tile: a lane's row (chunks 2c + lane / 32)
+// of rows RB .., and its columns of 32-column blocks (c[2 x + s]: block x,
+// rows 16 s ..).
+template <int DP>
+struct Frags16 {
+  using L = Tile<__bf16, DP>;
+  int ro[L::KS], lo[L::DB], hi[L::DB];   // the lane's offsets in a tile
+  __device__ __forceinline__ Frags16() {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    const int a = L::off(lane & 31, half);
+#pragma unroll
+    for (int c = 0; c < L::KS; ++c) ro[c] = a ^ (c << 5);
+    const int g = (lane >> 4) & 1, sl = lane & 15, row = 4 * half + (sl >> 2), chunk = 2 * g + ((sl >> 1) & 1);
+    const int l = L::off(row, chunk) + ((sl & 1) << 3), h = L::off(row + 8, chunk) + ((sl & 1) << 3);
+#pragma unroll
+    for (int x = 0; x < L::DB; ++x) {
+      lo[x] = l ^ (x << 6);
+      hi[x] = h ^ (x << 6);
+    }
+  }
+  template <int RB>
+  __device__ __forceinline__ void rows(u32x4 (&r)[L::KS], const uint8_t* tile) const {
+#pragma unroll
+    for (int c = 0; c < L::KS; ++c) r[c] = *reinterpret_cast<const u32x4*>(tile + RB * L::PITCH + ro[c]);
+  }
+  template <int RB>
+  __device__ __forceinline__ void cols(u32x4 (&r)[2 * L::DB], const uint8_t* tile) const {
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+#pragma unroll
+    for (int x = 0; x < L::DB; ++x)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const uint8_t* t = tile + (RB + 16 * s) * L::PITCH;
+        const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(t + lo[x])));
+        const u32x2 q = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(t + hi[x])));
+        r[2 * x + s] = u32x4{p[0], p[1], q[0], q[1]};
+      }
+  }
+};
+
+// x is computed here, neither later (sunk to its use past a branch) nor, for a
+// value from memory, waited for later (inside a loop, together with what the
+// loop has loaded since).
+__device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
+template <int N>
+__device__ __forceinline__ void pin(u32x4 (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
 
 // acc (columns d in rows, this lane's row in its column) * f to the lane's
 // row of d elements at `out`, 16 bytes a store.

@@ -107,6 +107,7 @@ int check_attn(const lact_attn_desc* s) {
   LACT_TRY(check_heads(s->B, s->H, s->Hkv, s->d, s->io_dtype, 256));
   if (s->n_q < 0 || s->n_kv < 0 || s->window < -1 || s->lookahead < -1 || s->sinks < 0) return LACT_EINVAL;
   if (!(s->scale > 0.0f) || !finite(s->scale)) return LACT_EINVAL;
+  if (s->scale < 1e-12f || s->scale > 1e12f) return LACT_EUNSUPPORTED;   // lse / scale stays far from overflow
   if (s->n_q > kAttnTokens || s->n_kv > kAttnTokens || s->q_start > kAttnTokens || s->q_start < -kAttnTokens ||
       s->q_start + s->n_q > kAttnTokens)
     return LACT_EUNSUPPORTED;
@@ -135,12 +136,12 @@ WindowArgs window_args(const lact_attn_desc* s) {
 }
 
 struct WindowLayout {
-  size_t lse2, delta, part, total;
+  size_t nlse, ndelta, part, total;
 };
 WindowLayout window_layout(const WindowArgs& a, const DkvPlan& p) {
   WindowLayout l{};
   const size_t rows = ws_round((size_t)a.B * a.H * a.n_q * 4);
-  l.delta = rows;
+  l.ndelta = rows;
   l.part = 2 * rows;
   l.total = l.part + ws_round((size_t)a.B * a.Hkv * p.slots() * 2 * p.kb * a.d * 4);
   return l;
@@ -358,8 +359,8 @@ int lact_window_attention_backward(const lact_attn_desc* desc, const lact_view* 
   g.dk = take(dk, s.B, s.Hkv, s.n_kv);
   g.dv = take(dv, s.B, s.Hkv, s.n_kv);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  g.lse2 = reinterpret_cast<float*>(ws + l.lse2);
-  g.delta = reinterpret_cast<float*>(ws + l.delta);
+  g.nlse = reinterpret_cast<float*>(ws + l.nlse);
+  g.ndelta = reinterpret_cast<float*>(ws + l.ndelta);
   g.part = reinterpret_cast<float*>(ws + l.part);
   return go<WindowBwdArgs, launch_window_bwd>(LACT_KCLASS_ATTN, g, bf16, stream);
 }

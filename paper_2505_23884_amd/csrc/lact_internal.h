@@ -549,8 +549,8 @@ DkvPlan window_dkv_plan(const WindowArgs& a, bool bf16);
 struct WindowBwdArgs {
   WindowArgs f;          // f.lse: read; f.o: the forward's output, read
   AttnView dout, dq, dk, dv;
-  float* lse2;           // [B * H][n_q]: lse log2(e), +inf where it is -inf
-  float* delta;          // [B * H][n_q]: sum_d dout o
+  float* nlse;           // [B * H][n_q]: -lse / scale, -inf where lse is
+  float* ndelta;         // [B * H][n_q]: -sum_d dout o
   float* part;           // [B * Hkv][slots][2][kb][d]: dK and dV partial sums
   DkvPlan plan;
 };

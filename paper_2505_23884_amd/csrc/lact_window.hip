@@ -29,6 +29,17 @@ __device__ __forceinline__ int xcd_order(int b, int n) {
   return x * per + (x < extra ? x : extra) + (b >> 3);
 }
 
+// Item p of a list of n in which each eighth, and so each XCD's share of a
+// head, holds items from all along it: every eighth one, then the next ones.
+// Work that shrinks towards the end of a sequence spreads over the XCDs, and
+// each share ends with its shortest items.
+__device__ __forceinline__ int spread(int p, int n) {
+  const int full = n >> 3, extra = n & 7;   // residues below `extra` have full + 1 items
+  if (p < extra * (full + 1)) return p / (full + 1) + 8 * (p % (full + 1));
+  p -= extra * (full + 1);
+  return extra + p / max(full, 1) + 8 * (p % max(full, 1));
+}
+
 template <typename T>
 __device__ __forceinline__ T* row_of(const AttnView& v, int b, int h, int64_t t) {
   return reinterpret_cast<T*>(v.p) + b * v.sb + h * v.sh + t * v.st;
@@ -116,7 +127,8 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_fwd(const WindowArgs a)
 }
 
 // ------------------------------------------------------------------ reverse
-// lse2 and delta, once per query: G lanes a row.
+// -lse / scale and -delta, once per query: the accumulators of the scores and
+// of do . v start from them. G lanes a row.
 template <typename T>
 __global__ __launch_bounds__(256) void k_window_delta(const WindowBwdArgs g, int G) {
   const WindowArgs& a = g.f;
@@ -143,8 +155,8 @@ __global__ __launch_bounds__(256) void k_window_delta(const WindowBwdArgs g, int
   for (int o = G >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   if (lg == 0) {
     const float l = a.lse[r];
-    g.lse2[r] = l == neg_inf() ? __builtin_inff() : l * kLog2e;   // weights of an empty row: exp2(-inf) = 0
-    g.delta[r] = sum;
+    g.nlse[r] = l == neg_inf() ? neg_inf() : -l / a.scale;   // an empty row's too: weights exp2(-inf) = 0
+    g.ndelta[r] = -sum;
   }
 }
 
@@ -176,8 +188,8 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
   u32x4 q[L::KS], go[L::KS];
   load_row<T, DP>(q, row_of<T>(a.q, b, h, ic), live, a.d);
   load_row<T, DP>(go, row_of<T>(g.dout, b, h, ic), live, a.d);
-  const float lse2 = live ? g.lse2[(int64_t)bh * a.n_q + ic] : __builtin_inff();
-  const float delta = live ? g.delta[(int64_t)bh * a.n_q + ic] : 0.0f;
+  const float nlse2 = (live ? g.nlse[(int64_t)bh * a.n_q + ic] : neg_inf()) * a.scale * kLog2e;
+  const float ndelta = live ? g.ndelta[(int64_t)bh * a.n_q + ic] : 0.0f;
   f32x16 dq[DP / 32];
 #pragma unroll
   for (int x = 0; x < DP / 32; ++x) dq[x] = f32x16{};
@@ -198,7 +210,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
     mma_dot<T, DP, RB>(s, ks, q);
     mma_dot<T, DP, RB>(dp, ks + BYTES, go);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse2)) * (dp[e] - delta);
+    for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, nlse2)) * (dp[e] + ndelta);
     if (masked) {
       if (__builtin_expect(bad != 0, 0))   // keys that held an infinity or NaN
 #pragma unroll
@@ -231,24 +243,34 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
   store_row<T, DP / 32>(row_of<T>(g.dq, b, h, ic), dq, a.scale, 0, a.d, i < a.n_q, !live);
 }
 
-// The job of a workgroup of k_window_dkv.
+// The job of workgroup `id` of `n`: first the tiles without sinks of every
+// (batch, key head), then the parts of the others, which are short and fill
+// the gaps that the former leave.
 struct DkvJob {
-  int tile, part, head_part, slot;   // slot < 0: the sums go to dk and dv
-  int qa, qb;                        // queries [qa, qb)
-  __device__ __forceinline__ DkvJob(const WindowArgs& a, const DkvPlan& pl, int len, int x) {
+  int bk, tile, part, head_part, slot;   // slot < 0: the sums go to dk and dv
+  int qa, qb;                            // queries [qa, qb)
+  __device__ __forceinline__ DkvJob(const WindowArgs& a, const DkvPlan& pl, int id, int n) {
+    const int plain = (pl.ntile - pl.st) * pl.np_a * pl.gs, sinks = pl.st * pl.np_s * pl.gs;
+    const int n1 = n / (plain + sinks) * plain;
+    const bool sink = id >= n1;
+    const int per = sink ? sinks : plain, w = sink ? xcd_order(id - n1, n - n1) : xcd_order(id, n1);
+    bk = w / per;
+    int x = spread(w % per, per);
     head_part = x % pl.gs;
     x /= pl.gs;
-    const bool sink = x < pl.st * pl.np_s;
-    const int np = sink ? pl.np_s : pl.np_a, ch = sink ? pl.ch_s : pl.ch_a;
-    if (!sink) x -= pl.st * pl.np_s;
+    const int np = sink ? pl.np_s : pl.np_a;
     tile = x / np + (sink ? 0 : pl.st);
     part = x % np;
-    const int before = sink || pl.np_s * pl.gs <= 1 ? 0 : pl.st * pl.np_s * pl.gs;
+    const int before = sink || pl.np_s * pl.gs <= 1 ? 0 : sinks;
     slot = np * pl.gs > 1 ? before + (((sink ? tile : tile - pl.st) * np) + part) * pl.gs + head_part : -1;
+  }
+  __device__ __forceinline__ void queries(const WindowArgs& a, const DkvPlan& pl, int len) {
+    const bool sink = tile < pl.st;
+    const int np = sink ? pl.np_s : pl.np_a, ch = sink ? pl.ch_s : pl.ch_a;
     const int k0 = tile * pl.kb, k1 = min(k0 + pl.kb, len) - 1;   // keys k0 .. k1
     const int last = min(a.n_q, len - a.q_start);                  // queries of the sequence
     // j <= p + look and (p < j + win or j < sinks), p = q_start + i
-    int ia = max(0, k0 - a.look - a.q_start);
+    const int ia = max(0, k0 - a.look - a.q_start);
     int ib = k0 < a.sinks ? last : min(last, k1 + a.win - a.q_start);
     if (k0 > k1) ib = ia;
     qa = ia + part * ch;
@@ -270,11 +292,12 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE];
   __shared__ uint32_t mask[2];
   __shared__ int found;
-  const int jobs = g.plan.jobs(), ND = DP / DO;
-  const int w = xcd_order(blockIdx.x, gridDim.x);
-  const int dsel = w % ND, bk = (w / ND) / jobs, b = bk / a.Hkv, hk = bk % a.Hkv;
+  constexpr int ND = DP / DO;
+  const int dsel = blockIdx.x % ND;
+  DkvJob job(a, g.plan, blockIdx.x / ND, gridDim.x / ND);
+  const int bk = job.bk, b = bk / a.Hkv, hk = bk % a.Hkv;
   const int len = length_of(a, b);
-  const DkvJob job(a, g.plan, len, (w / ND) % jobs);
+  job.queries(a, g.plan, len);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
   const int kw = job.tile * KB + 32 * wave, j = kw + (lane & 31), jc = min(j, a.n_kv - 1);
   const bool live = j < len;
@@ -301,8 +324,8 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
     uint8_t* to = smem + (x & 1) * STAGE;
     Cp::rows(to, row_of<T>(a.q, b, h, i0), ldq, job.qb - i0, a.d);
     Cp::rows(to + BYTES, row_of<T>(g.dout, b, h, i0), ldo, job.qb - i0, a.d);
-    if (wave < 2) {   // lse2 and delta of the queries; past the last one zeros (masked)
-      const float* from = (wave ? g.delta : g.lse2) + ((int64_t)b * a.H + h) * a.n_q + i0;
+    if (wave < 2) {   // nlse and ndelta of the queries; past the last one zeros (masked)
+      const float* from = (wave ? g.ndelta : g.nlse) + ((int64_t)b * a.H + h) * a.n_q + i0;
       const __amdgpu_buffer_rsrc_t rsrc =
           __builtin_amdgcn_make_buffer_rsrc((void*)from, (short)0, min(QT, job.qb - i0) * 4, kBufFlags);
       if (lane < QT)
@@ -323,7 +346,7 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
     f32x16 s, dp;
     mma_dot<T, DP, RB>(s, qs, kf);
     mma_dot<T, DP, RB>(dp, os, vf);
-    // lse2 and delta of rows 8e + 4 half ..
+    // nlse and ndelta of rows 8e + 4 half ..
     u32x4 rows[8];
     {
       const uint32_t at = lds_addr(qs + 2 * BYTES) + RB * 4 + 16 * half;
@@ -331,14 +354,9 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
       read_rows8<0>(rows, ad);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const f32x4 ls = __builtin_bit_cast(f32x4, rows[e]), dl = __builtin_bit_cast(f32x4, rows[4 + e]);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int r = 4 * e + u;
-        s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ls[u]));
-        dp[r] = s[r] * (dp[r] - dl[u]);
-      }
+    for (int e = 0; e < 16; ++e) {
+      s[e] = __builtin_amdgcn_exp2f((s[e] + __uint_as_float(rows[e >> 2][e & 3])) * c);
+      dp[e] = s[e] * (dp[e] + __uint_as_float(rows[4 + (e >> 2)][e & 3]));
     }
     if (masked) {
       if (__builtin_expect((badq | bado) != 0, 0))   // queries, or cotangents, that held an infinity or NaN
@@ -397,6 +415,208 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
   }
 }
 
+// The same for 16-bit I/O and DP <= 128, one wave a SIMD with registers to
+// spare: a step is 64 queries in two halves A and B, in four phases of matrix
+// products that the vector work of the other half runs beside:
+//   S and dP of A | S and dP of B, weights of A | dV and dK of A, weights of B
+//   | dV and dK of B
+// Each phase's fragments are read from LDS in the phase before it.
+template <int DP, int NW>
+__global__ __launch_bounds__(64 * NW, DP <= 64 ? 2 : 1) void k_window_dkv16(const WindowBwdArgs g) {
+  typedef __bf16 T;
+  const WindowArgs& a = g.f;
+  constexpr int KB = 32 * NW, NT = 64 * NW, QT = 64, NB = DP / 32;
+  using L = Tile<T, DP>;
+  constexpr int BYTES = QT * L::PITCH, STAGE = 2 * BYTES + 1024;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE];
+  __shared__ uint32_t mask[2];
+  __shared__ int found;
+  DkvJob job(a, g.plan, blockIdx.x, gridDim.x);
+  const int bk = job.bk, b = bk / a.Hkv, hk = bk % a.Hkv;
+  const int len = length_of(a, b);
+  job.queries(a, g.plan, len);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const int kw = job.tile * KB + 32 * wave, j = kw + (lane & 31), jc = min(j, a.n_kv - 1);
+  const bool live = j < len;
+  const int iend = min(a.n_q, len - a.q_start);   // queries past it are padding
+  const int ilo = max(j - a.look - a.q_start, 0);  // the queries of the job that see key j: ilo .. ihi
+  const int ihi = !live ? -1 : min(job.qb - 1, j < a.sinks ? iend - 1 : min(iend - 1, j + a.win - 1 - a.q_start));
+  const uint32_t span = (uint32_t)max(ihi - ilo, 0);
+  const int first = ihi < ilo ? (1 << 30) : ilo - 4 * half;
+
+  u32x4 kf[L::KS], vf[L::KS];
+  load_row<T, DP>(kf, row_of<T>(a.k, b, hk, jc), live, a.d);
+  load_row<T, DP>(vf, row_of<T>(a.v, b, hk, jc), live, a.d);
+  f32x16 dk[NB], dv[NB];
+#pragma unroll
+  for (int x = 0; x < NB; ++x) dk[x] = dv[x] = f32x16{};
+  const float c = a.scale * kLog2e;
+  const int steps = job.qb > job.qa ? (job.qb - job.qa + QT - 1) / QT : 0;
+  const int gh = a.G / g.plan.gs, n = steps * gh;
+  const int ldq = (int)(a.q.st * sizeof(T)), ldo = (int)(g.dout.st * sizeof(T));
+  Stage<T, DP, QT, NT> sq, so;
+  const Frags16<DP> fr;
+  float s_row = 0.0f;
+  const int h0 = hk * a.G + job.head_part * gh;
+  auto load = [&](int x) __attribute__((always_inline)) {
+    const int h = h0 + x / steps, i0 = job.qa + (x % steps) * QT;
+    sq.load(row_of<T>(a.q, b, h, i0), ldq, job.qb - i0, a.d);
+    so.load(row_of<T>(g.dout, b, h, i0), ldo, job.qb - i0, a.d);
+    if (threadIdx.x < 2 * QT) {   // nlse, then ndelta; past the last query zeros (masked)
+      const int i = i0 + threadIdx.x % QT;
+      const float* from = (int)threadIdx.x < QT ? g.nlse : g.ndelta;
+      s_row = i < job.qb ? from[((int64_t)b * a.H + h) * a.n_q + i] : 0.0f;
+    }
+  };
+  auto store = [&](uint8_t* to) __attribute__((always_inline)) {
+    sq.store(to);
+    so.store(to + BYTES);
+    if (threadIdx.x < 2 * QT) reinterpret_cast<float*>(to + 2 * BYTES)[threadIdx.x] = s_row;
+  };
+  using Cp = Copy<T, DP, QT, NT>;
+  auto body = [&](auto stage, int x) __attribute__((always_inline)) {
+    uint8_t* qs = smem + decltype(stage)::value * STAGE;
+    uint8_t* os = qs + BYTES;
+    float* rows = reinterpret_cast<float*>(qs + 2 * BYTES);
+    const int i0 = job.qa + (x % steps) * QT;
+    // the step against the workgroup's and the wave's keys: nothing, something or all
+    auto seen = [&](int k0, int k1) __attribute__((always_inline)) {
+      const int pa = a.q_start + i0, pe = a.q_start + min(i0 + QT, min(job.qb, iend)) - 1;
+      if (pa > pe || k0 >= len || k0 > pe + a.look || (k0 >= a.sinks && k1 <= pa - a.win)) return 0;
+      return pe - pa == QT - 1 && k1 < len && k1 <= pa + a.look && (k0 > pe - a.win || k1 < a.sinks) ? 2 : 1;
+    };
+    uint64_t bado = 0;
+    if (seen(job.tile * KB, job.tile * KB + KB - 1) != 2 &&
+        __builtin_expect((Copy<T, DP, 2 * QT, NT>::holds_nonfinite(qs, x, &found)), 0)) {
+      const uint64_t badq = Cp::scrub(qs, mask);
+      bado = Cp::scrub(os, mask);
+      // a query's infinity or NaN makes its weights NaN, a cotangent's their cotangents
+      if (threadIdx.x < QT) {
+        if (badq >> threadIdx.x & 1) rows[threadIdx.x] = __builtin_nanf("");
+        if (bado >> threadIdx.x & 1) rows[QT + threadIdx.x] = __builtin_nanf("");
+      }
+      __syncthreads();
+    }
+    if (x + 1 < n) load(x + 1);
+    const int what = seen(kw, kw + 31);
+    if (what) {
+      u32x4 f0[L::KS], f1[L::KS], f2[L::KS], f3[L::KS];
+      f32x16 sa, da, sb, db;
+      RowsB<T> pa, da16, pb, db16;
+      const int lo = first - i0;
+      // the accumulators' first values: rows 8e + 4 half .. of half RB
+      auto start = [&](auto rb, f32x16& s, f32x16& d) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(rows + decltype(rb)::value + 8 * e + 4 * half);
+          const f32x4 y = *reinterpret_cast<const f32x4*>(rows + QT + decltype(rb)::value + 8 * e + 4 * half);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            s[4 * e + u] = x[u];
+            d[4 * e + u] = y[u];
+          }
+        }
+      };
+      auto hide = [&](auto rb, f32x16& s, f32x16& d) __attribute__((always_inline)) {
+        if (what == 2) return;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const bool see = (uint32_t)(decltype(rb)::value + 8 * (r >> 2) + (r & 3) - lo) <= span;
+          s[r] = see ? s[r] : neg_inf();
+          d[r] = see ? d[r] : 0.0f;
+        }
+      };
+      // weights and their cotangents of elements e, e + 1
+      auto weigh = [&](int e, const f32x16& s, const f32x16& d, RowsB<T>& p16, RowsB<T>& d16)
+          __attribute__((always_inline)) {
+        const float p0 = __builtin_amdgcn_exp2f(s[e] * c), p1 = __builtin_amdgcn_exp2f(s[e + 1] * c);
+        uint32_t x = pack_bf16(p0, p1), y = pack_bf16(p0 * d[e], p1 * d[e + 1]);
+        pin(x);
+        pin(y);
+        p16.v[e >> 3][(e & 7) >> 1] = x;
+        d16.v[e >> 3][(e & 7) >> 1] = y;
+      };
+      const std::integral_constant<int, 0> A;
+      const std::integral_constant<int, 32> B;
+      start(A, sa, da);
+      fr.template rows<0>(f0, qs);
+      fr.template rows<0>(f1, os);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (DP > 64) {
+        fr.template rows<32>(f2, qs);
+        fr.template rows<32>(f3, os);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = 0; i < L::KS; ++i) {
+        mma_chunk<T>(sa, f0[i], kf[i]);
+        mma_chunk<T>(da, f1[i], vf[i]);
+      }
+      hide(A, sa, da);
+      start(B, sb, db);
+      if constexpr (DP == 64) {
+        fr.template rows<32>(f2, qs);
+        fr.template rows<32>(f3, os);
+      }
+      fr.template cols<0>(f0, os);
+      fr.template cols<0>(f1, qs);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < L::KS; ++i) {
+        mma_chunk<T>(sb, f2[i], kf[i]);
+        mma_chunk<T>(db, f3[i], vf[i]);
+#pragma unroll
+        for (int e = 0; e < 16 / L::KS; e += 2) weigh(16 / L::KS * i + e, sa, da, pa, da16);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      hide(B, sb, db);
+      fr.template cols<32>(f2, os);
+      fr.template cols<32>(f3, qs);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) {
+        mma_chunk<T>(dv[i >> 1], f0[i], pa.v[i & 1]);
+        mma_chunk<T>(dk[i >> 1], f1[i], da16.v[i & 1]);
+#pragma unroll
+        for (int e = 0; e < 8 / NB; e += 2) weigh(8 / NB * i + e, sb, db, pb, db16);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) {
+        mma_chunk<T>(dv[i >> 1], f2[i], pb.v[i & 1]);
+        mma_chunk<T>(dk[i >> 1], f3[i], db16.v[i & 1]);
+      }
+    }
+#pragma unroll 1
+    for (; __builtin_expect(bado != 0, 0); bado &= bado - 1) {   // dv takes the cotangents' infinities and NaN
+      const int i = i0 + __builtin_ctzll(bado);
+      add_nonfinite<T, NB>(dv, row_of<T>(g.dout, b, h0 + x / steps, i), i >= ilo && i <= ihi, 0, a.d);
+    }
+    if (x + 1 < n) store(smem + (1 - decltype(stage)::value) * STAGE);
+    __syncthreads();
+  };
+  if (threadIdx.x == 0) found = -1;
+  pin(kf);
+  pin(vf);
+  if (n > 0) {
+    load(0);
+    store(smem);
+  }
+  __syncthreads();
+  for (int x = 0; x < n; x += 2) {
+    body(std::integral_constant<int, 0>{}, x);
+    if (x + 1 < n) body(std::integral_constant<int, 1>{}, x + 1);
+  }
+  if (job.slot < 0) {
+    store_row<T, NB>(row_of<T>(g.dk, b, hk, jc), dk, a.scale, 0, a.d, j < a.n_kv, !live);
+    store_row<T, NB>(row_of<T>(g.dv, b, hk, jc), dv, 1.0f, 0, a.d, j < a.n_kv, !live);
+  } else {
+    float* part = g.part + ((int64_t)bk * g.plan.slots() + job.slot) * 2 * KB * a.d + (int64_t)(32 * wave + (lane & 31)) * a.d;
+    store_row<float, NB>(part, dk, a.scale, 0, a.d, true, !live);
+    store_row<float, NB>(part + (int64_t)KB * a.d, dv, 1.0f, 0, a.d, true, !live);
+  }
+}
+
 // dk and dv of the tiles whose sums came in parts, in the order of the parts:
 // four elements a thread.
 template <typename T>
@@ -446,7 +666,7 @@ template <typename T, int DP>
 hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
   const WindowArgs& a = g.f;
   constexpr bool H16 = sizeof(T) == 2;
-  constexpr int DO = DP <= 128 ? DP : H16 ? 128 : 64, QT = H16 && DP <= 128 ? 64 : 32;
+  constexpr int DO = DP <= 128 ? DP : H16 ? 128 : 64, QT = 32;
   const int64_t bh = (int64_t)a.B * a.H, bk = (int64_t)a.B * a.Hkv;
   if (a.n_q > 0) {
     int G = 1;
@@ -455,7 +675,10 @@ hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
     k_window_dq<T, DP, 4, (H16 && DP <= 128 ? 2 : 1)><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(g);
   }
   if (a.n_kv > 0) {
-    k_window_dkv<T, DP, DO, QT, 4><<<(unsigned)(bk * g.plan.jobs() * (DP / DO)), 256, 0, s>>>(g);
+    if constexpr (H16 && DP <= 128)
+      k_window_dkv16<DP, 4><<<(unsigned)(bk * g.plan.jobs()), 256, 0, s>>>(g);
+    else
+      k_window_dkv<T, DP, DO, QT, 4><<<(unsigned)(bk * g.plan.jobs() * (DP / DO)), 256, 0, s>>>(g);
     const DkvPlan& pl = g.plan;
     const bool ps = pl.np_s * pl.gs > 1 && pl.st > 0, pa = pl.np_a * pl.gs > 1;
     const int t0 = pl.np_s * pl.gs > 1 ? 0 : pl.st, t1 = pa ? pl.ntile : pl.st;
@@ -470,8 +693,10 @@ hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
 }  // namespace
 
 // Tiles of sinks are seen by every later query, the others by a window of
-// them: the former are cut into parts of about the latter's work, and all of
-// them, by heads first, where the tiles alone would leave CUs idle.
+// them: the former are cut into parts of a quarter of the latter's queries
+// ([1, 16 / 4, 8192, 128], window 2048, sinks 4: 12 jobs of a whole window's
+// size beside 256 others take another round, 720 us; without sinks 400), and
+// all of them, by heads first, where the tiles alone would leave CUs idle.
 DkvPlan window_dkv_plan(const WindowArgs& a, bool bf16) {
   (void)bf16;
   DkvPlan p{};
@@ -488,7 +713,7 @@ DkvPlan window_dkv_plan(const WindowArgs& a, bool bf16) {
   const int64_t tiles = (int64_t)a.B * a.Hkv * p.ntile;
   if (reach < n_q) {
     p.st = cdiv(std::min(a.sinks, a.n_kv), p.kb);
-    parts(cdiv(reach, 64) * 64, &p.np_s, &p.ch_s);
+    parts(std::max(256, cdiv(reach, 256) * 64), &p.np_s, &p.ch_s);
   }
   while (tiles * p.gs < 256 && p.gs < a.G) {
     int f = 2;
