@@ -36,6 +36,21 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr uint32_t kBufOOB = 0x80000000u;      // a raw buffer offset past every range: loads zeros
 constexpr int kBufFlags = 0x00020000;
 
+// At most N of this wave's loads and copies still in flight (those that were
+// issued last).
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// A barrier that waits for nothing else: reads of LDS before it are complete
+// (their results are in use), copies behind it go on.
+__device__ __forceinline__ void barrier_only() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 
 // Lane of the other half of the wave: max / sum of x over lanes l and l ^ 32.
@@ -96,7 +111,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 template <typename T> struct RowsB;
 template <> struct RowsB<__bf16> {
   u32x4 v[2];
-  __device__ __forceinline__ RowsB() {}
   __device__ __forceinline__ explicit RowsB(const f32x16& s) {
 #pragma unroll
     for (int g = 0; g < 2; ++g)
@@ -182,15 +196,32 @@ __device__ __forceinline__ void read_cols2(u32x2 (&r)[8], const uint32_t (&lo)[2
       : "memory");
 }
 
-// acc (32 rows of the tile from RB x 32 columns of b) = rows . b over d; b
-// holds a lane's column as Tile::KS chunks.
-template <typename T, int DP, int RB>
-__device__ __forceinline__ void mma_dot(f32x16& acc, const uint8_t* tile, const u32x4 (&b)[(Tile<T, DP>::KS)]) {
+// The same of four blocks in one batch.
+template <int OFF, int STEP>
+__device__ __forceinline__ void read_cols4(u32x2 (&r)[16], const uint32_t (&lo)[4], const uint32_t (&hi)[4]) {
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %16 offset:%24\n\tds_read_b64_tr_b16 %1, %17 offset:%24\n\t"
+      "ds_read_b64_tr_b16 %2, %16 offset:%25\n\tds_read_b64_tr_b16 %3, %17 offset:%25\n\t"
+      "ds_read_b64_tr_b16 %4, %18 offset:%24\n\tds_read_b64_tr_b16 %5, %19 offset:%24\n\t"
+      "ds_read_b64_tr_b16 %6, %18 offset:%25\n\tds_read_b64_tr_b16 %7, %19 offset:%25\n\t"
+      "ds_read_b64_tr_b16 %8, %20 offset:%24\n\tds_read_b64_tr_b16 %9, %21 offset:%24\n\t"
+      "ds_read_b64_tr_b16 %10, %20 offset:%25\n\tds_read_b64_tr_b16 %11, %21 offset:%25\n\t"
+      "ds_read_b64_tr_b16 %12, %22 offset:%24\n\tds_read_b64_tr_b16 %13, %23 offset:%24\n\t"
+      "ds_read_b64_tr_b16 %14, %22 offset:%25\n\tds_read_b64_tr_b16 %15, %23 offset:%25\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7]),
+        "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]), "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15])
+      : "v"(lo[0]), "v"(hi[0]), "v"(lo[1]), "v"(hi[1]), "v"(lo[2]), "v"(hi[2]), "v"(lo[3]), "v"(hi[3]), "n"(OFF),
+        "n"(OFF + STEP)
+      : "memory");
+}
+
+// acc (32 rows of the tile from RB x 32 columns of b) += rows . b over d; b
+// holds a lane's column as Tile::KS chunks. N chunks a batch of reads.
+template <typename T, int DP, int RB, int N = (Tile<T, DP>::KS < 8 ? 4 : 8)>
+__device__ __forceinline__ void mma_dot_add(f32x16& acc, const uint8_t* tile, const u32x4 (&b)[(Tile<T, DP>::KS)]) {
   using L = Tile<T, DP>;
   const int lane = threadIdx.x & 63;
-  acc = f32x16{};
   if constexpr (sizeof(T) == 2) {
-    constexpr int N = L::KS < 8 ? 4 : 8;
     // chunk 2c + half of the row: the lane's first address with bits 5 and up of c flipped in
     const uint32_t a0 = lds_addr(tile) + L::off(lane & 31, lane >> 5);
 #pragma unroll
@@ -210,6 +241,31 @@ __device__ __forceinline__ void mma_dot(f32x16& acc, const uint8_t* tile, const 
       mma_chunk<T>(acc, L::row_chunk(tile, RB + (lane & 31), 2 * c + (lane >> 5)), b[c]);
   }
 }
+template <typename T, int DP, int RB>
+__device__ __forceinline__ void mma_dot(f32x16& acc, const uint8_t* tile, const u32x4 (&b)[(Tile<T, DP>::KS)]) {
+  acc = f32x16{};
+  mma_dot_add<T, DP, RB>(acc, tile, b);
+}
+// The same with b's columns as rows of another tile in LDS (16-bit).
+template <int DP>
+__device__ __forceinline__ void mma_dot_lds(f32x16& acc, const uint8_t* tile, const uint8_t* bt) {
+  using L = Tile<__bf16, DP>;
+  const int lane = threadIdx.x & 63, o = L::off(lane & 31, lane >> 5);
+  const uint32_t a0 = lds_addr(tile) + o, b0 = lds_addr(bt) + o;
+#pragma unroll
+  for (int c = 0; c < L::KS; c += 4) {
+    uint32_t ad[8];
+    u32x4 r[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      ad[i] = a0 ^ (uint32_t)((c + i) << 5);
+      ad[4 + i] = b0 ^ (uint32_t)((c + i) << 5);
+    }
+    read_rows8<0>(r, ad);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mma_chunk<__bf16>(acc, r[i], r[4 + i]);
+  }
+}
 
 // acc[0 .. NB) (32-column blocks db0 .. of d x 32 columns of b) += (rows RB ..
 // RB + 31 of the tile)^T x b.
@@ -218,24 +274,26 @@ __device__ __forceinline__ void mma_rows(f32x16 (&acc)[NB], const RowsB<T>& b, c
   using L = Tile<T, DP>;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   if constexpr (sizeof(T) == 2) {
-    static_assert(NB % 2 == 0, "column blocks are read in pairs");
+    constexpr int M = NB % 4 ? 2 : 4;   // column blocks a batch
+    static_assert(NB % M == 0, "column blocks are read in pairs");
     const int g = (lane >> 4) & 1, sl = lane & 15, row = 4 * half + (sl >> 2), chunk = 2 * g + ((sl >> 1) & 1);
     const uint32_t base = lds_addr(tile) + ((sl & 1) << 3);
     const uint32_t a0 = base + L::off(row, chunk), a1 = base + L::off(row + 8, chunk);
 #pragma unroll
-    for (int x = 0; x < NB; x += 2) {
-      uint32_t lo[2], hi[2];
+    for (int x = 0; x < NB; x += M) {
+      uint32_t lo[M], hi[M];
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
+      for (int y = 0; y < M; ++y) {
         lo[y] = a0 ^ (uint32_t)((db0 + x + y) << 6);
         hi[y] = a1 ^ (uint32_t)((db0 + x + y) << 6);
       }
-      u32x2 r[8];
-      read_cols2<RB * L::PITCH, 16 * L::PITCH>(r, lo, hi);
+      u32x2 r[4 * M];
+      if constexpr (M == 4) read_cols4<RB * L::PITCH, 16 * L::PITCH>(r, lo, hi);
+      else read_cols2<RB * L::PITCH, 16 * L::PITCH>(r, lo, hi);
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int y = 0; y < M; ++y) {
           const u32x2 p = r[4 * y + 2 * s], q = r[4 * y + 2 * s + 1];
           mma_chunk<T>(acc[x + y], u32x4{p[0], p[1], q[0], q[1]}, b.v[s]);
         }
@@ -259,7 +317,8 @@ __device__ __forceinline__ void mma_rows(f32x16 (&acc)[NB], const RowsB<T>& b, c
 // with any weight above zero.
 template <typename T, int NB>
 __device__ __forceinline__ void add_nonfinite(f32x16 (&acc)[NB], const T* row, bool see, int d0, int d) {
-  const int half = (threadIdx.x >> 5) & 1;
+  int half = (threadIdx.x >> 5) & 1;
+  asm volatile("" : "+v"(half));   // nothing of this is worked out ahead of a loop, for it hardly ever runs
 #pragma unroll
   for (int db = 0; db < NB; ++db)
 #pragma unroll
@@ -298,11 +357,16 @@ struct Copy {
 
   // rows of `ld` bytes from `base` (the same in all threads), `rows` of them
   // (<= 0: none); the rest, and columns past d, are zeros
+  // FRESH: the offsets are worked out each time (about 10 instructions a
+  // chunk) instead of staying in registers through a loop.
+  template <bool FRESH = false>
   static __device__ __forceinline__ void rows(uint8_t* tile, const T* base, int ld, int64_t rows, int d) {
-    const int tid = threadIdx.x, n = (int)(rows < R ? rows : R);
+    int tid = threadIdx.x;
+    if constexpr (FRESH) asm volatile("" : "+v"(tid));
+    const int n = (int)(rows < R ? rows : R);
     const int span = n > 0 ? (n - 1) * ld + d * (int)sizeof(T) : 0;
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, span, kBufFlags);
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int row = tid / L::CPR + i * STEP, c = (tid % L::CPR) ^ L::swz(row);
@@ -345,81 +409,6 @@ struct Copy {
     return ((uint64_t)hi << 32) | lo;
   }
 };
-
-// The same through registers: the loads of the next tile are issued before
-// the products of the present one and stored after them. For kernels with
-// registers to spare: plain LDS reads then do not wait for copies in flight.
-template <typename T, int DP, int R, int NT>
-struct Stage {
-  using L = Tile<T, DP>;
-  static constexpr int N = R * L::CPR / NT, STEP = NT / L::CPR;
-  static_assert(N >= 1 && R * L::CPR % NT == 0 && NT % L::CPR == 0, "tile split");
-  u32x4 r[N];
-  __device__ __forceinline__ void load(const T* base, int ld, int64_t rows, int d) {
-    const int row = threadIdx.x / L::CPR, c = threadIdx.x % L::CPR;
-    const int n = (int)(rows < R ? rows : R);
-    const int span = n > 0 ? (n - 1) * ld + d * (int)sizeof(T) : 0;
-    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, span, kBufFlags);
-    const uint32_t o = c * L::E < d ? (uint32_t)(row * ld + c * 16) : kBufOOB;
-#pragma unroll
-    for (int i = 0; i < N; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, o + (uint32_t)(i * STEP * ld), 0, 0);
-  }
-  __device__ __forceinline__ void store(uint8_t* tile) const {
-    const int row = threadIdx.x / L::CPR, c = threadIdx.x % L::CPR;
-#pragma unroll
-    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(tile + L::off(row + i * STEP, c)) = r[i];
-  }
-};
-
-// Plain fragment reads of a 16-bit tile: a lane's row (chunks 2c + lane / 32)
-// of rows RB .., and its columns of 32-column blocks (c[2 x + s]: block x,
-// rows 16 s ..).
-template <int DP>
-struct Frags16 {
-  using L = Tile<__bf16, DP>;
-  int ro[L::KS], lo[L::DB], hi[L::DB];   // the lane's offsets in a tile
-  __device__ __forceinline__ Frags16() {
-    const int lane = threadIdx.x & 63, half = lane >> 5;
-    const int a = L::off(lane & 31, half);
-#pragma unroll
-    for (int c = 0; c < L::KS; ++c) ro[c] = a ^ (c << 5);
-    const int g = (lane >> 4) & 1, sl = lane & 15, row = 4 * half + (sl >> 2), chunk = 2 * g + ((sl >> 1) & 1);
-    const int l = L::off(row, chunk) + ((sl & 1) << 3), h = L::off(row + 8, chunk) + ((sl & 1) << 3);
-#pragma unroll
-    for (int x = 0; x < L::DB; ++x) {
-      lo[x] = l ^ (x << 6);
-      hi[x] = h ^ (x << 6);
-    }
-  }
-  template <int RB>
-  __device__ __forceinline__ void rows(u32x4 (&r)[L::KS], const uint8_t* tile) const {
-#pragma unroll
-    for (int c = 0; c < L::KS; ++c) r[c] = *reinterpret_cast<const u32x4*>(tile + RB * L::PITCH + ro[c]);
-  }
-  template <int RB>
-  __device__ __forceinline__ void cols(u32x4 (&r)[2 * L::DB], const uint8_t* tile) const {
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-#pragma unroll
-    for (int x = 0; x < L::DB; ++x)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const uint8_t* t = tile + (RB + 16 * s) * L::PITCH;
-        const u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(t + lo[x])));
-        const u32x2 q = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(t + hi[x])));
-        r[2 * x + s] = u32x4{p[0], p[1], q[0], q[1]};
-      }
-  }
-};
-
-// x is computed here, neither later (sunk to its use past a branch) nor, for a
-// value from memory, waited for later (inside a loop, together with what the
-// loop has loaded since).
-__device__ __forceinline__ void pin(uint32_t& x) { asm volatile("" : "+v"(x)); }
-template <int N>
-__device__ __forceinline__ void pin(u32x4 (&x)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
-}
 
 // acc (columns d in rows, this lane's row in its column) * f to the lane's
 // row of d elements at `out`, 16 bytes a store.

@@ -415,28 +415,29 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
   }
 }
 
-// The same for 16-bit I/O and DP <= 128, one wave a SIMD with registers to
-// spare: a step is 64 queries in two halves A and B, in four phases of matrix
-// products that the vector work of the other half runs beside:
-//   S and dP of A | S and dP of B, weights of A | dV and dK of A, weights of B
-//   | dV and dK of B
-// Each phase's fragments are read from LDS in the phase before it.
-template <int DP, int NW>
-__global__ __launch_bounds__(64 * NW, DP <= 64 ? 2 : 1) void k_window_dkv16(const WindowBwdArgs g) {
+// The same for 16-bit I/O and DP <= 128, two waves a SIMD: QH waves share the
+// 32 keys of a wave above, each with 64 / QH queries of a step and its own
+// sums (added at the end), so that one's vector work runs beside the other's
+// matrix products. The values wait in LDS instead of registers.
+template <int DP, int QH>
+__global__ __launch_bounds__(256 * QH, 2) void k_window_dkv16(const WindowBwdArgs g) {
   typedef __bf16 T;
   const WindowArgs& a = g.f;
-  constexpr int KB = 32 * NW, NT = 64 * NW, QT = 64, NB = DP / 32;
+  constexpr int KB = 128, NT = 256 * QH, QT = 64, NB = DP / 32, QW = QT / QH;
   using L = Tile<T, DP>;
-  constexpr int BYTES = QT * L::PITCH, STAGE = 2 * BYTES + 1024;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE];
+  constexpr int BYTES = QT * L::PITCH, STAGE = 2 * BYTES + 1024, VB = KB * L::PITCH;
+  constexpr int RING = DP > 64 ? 3 : 2;   // stages: copies run RING - 1 steps ahead
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[VB + RING * STAGE];
   __shared__ uint32_t mask[2];
   __shared__ int found;
+  uint8_t* const ring = smem + VB;
   DkvJob job(a, g.plan, blockIdx.x, gridDim.x);
   const int bk = job.bk, b = bk / a.Hkv, hk = bk % a.Hkv;
   const int len = length_of(a, b);
   job.queries(a, g.plan, len);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
-  const int kw = job.tile * KB + 32 * wave, j = kw + (lane & 31), jc = min(j, a.n_kv - 1);
+  const int kg = wave & 3, qh = wave >> 2;
+  const int kw = job.tile * KB + 32 * kg, j = kw + (lane & 31), jc = min(j, a.n_kv - 1);
   const bool live = j < len;
   const int iend = min(a.n_q, len - a.q_start);   // queries past it are padding
   const int ilo = max(j - a.look - a.q_start, 0);  // the queries of the job that see key j: ilo .. ihi
@@ -444,174 +445,149 @@ __global__ __launch_bounds__(64 * NW, DP <= 64 ? 2 : 1) void k_window_dkv16(cons
   const uint32_t span = (uint32_t)max(ihi - ilo, 0);
   const int first = ihi < ilo ? (1 << 30) : ilo - 4 * half;
 
-  u32x4 kf[L::KS], vf[L::KS];
+  u32x4 kf[L::KS];
   load_row<T, DP>(kf, row_of<T>(a.k, b, hk, jc), live, a.d);
-  load_row<T, DP>(vf, row_of<T>(a.v, b, hk, jc), live, a.d);
   f32x16 dk[NB], dv[NB];
 #pragma unroll
   for (int x = 0; x < NB; ++x) dk[x] = dv[x] = f32x16{};
   const float c = a.scale * kLog2e;
   const int steps = job.qb > job.qa ? (job.qb - job.qa + QT - 1) / QT : 0;
-  const int gh = a.G / g.plan.gs, n = steps * gh;
+  const int gh = a.G / g.plan.gs, n = steps * gh, h0 = hk * a.G + job.head_part * gh;
   const int ldq = (int)(a.q.st * sizeof(T)), ldo = (int)(g.dout.st * sizeof(T));
-  Stage<T, DP, QT, NT> sq, so;
-  const Frags16<DP> fr;
-  float s_row = 0.0f;
-  const int h0 = hk * a.G + job.head_part * gh;
-  auto load = [&](int x) __attribute__((always_inline)) {
-    const int h = h0 + x / steps, i0 = job.qa + (x % steps) * QT;
-    sq.load(row_of<T>(a.q, b, h, i0), ldq, job.qb - i0, a.d);
-    so.load(row_of<T>(g.dout, b, h, i0), ldo, job.qb - i0, a.d);
-    if (threadIdx.x < 2 * QT) {   // nlse, then ndelta; past the last query zeros (masked)
-      const int i = i0 + threadIdx.x % QT;
-      const float* from = (int)threadIdx.x < QT ? g.nlse : g.ndelta;
-      s_row = i < job.qb ? from[((int64_t)b * a.H + h) * a.n_q + i] : 0.0f;
+  using Cp = Copy<T, DP, QT, NT>;
+  typedef __attribute__((address_space(3))) void lds_void;
+  int ch = h0, ci = job.qa;   // head and first query of the next copy
+  auto copy = [&](int stage) __attribute__((always_inline)) {
+    uint8_t* to = ring + stage * STAGE;
+    Cp::template rows<(DP > 64)>(to, row_of<T>(a.q, b, ch, ci), ldq, job.qb - ci, a.d);
+    Cp::template rows<(DP > 64)>(to + BYTES, row_of<T>(g.dout, b, ch, ci), ldo, job.qb - ci, a.d);
+    if (wave < 2) {   // nlse and ndelta of the queries; past the last one zeros (masked)
+      const float* from = (wave ? g.ndelta : g.nlse) + ((int64_t)b * a.H + ch) * a.n_q + ci;
+      const __amdgpu_buffer_rsrc_t rsrc =
+          __builtin_amdgcn_make_buffer_rsrc((void*)from, (short)0, min(QT, job.qb - ci) * 4, kBufFlags);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + 2 * BYTES + wave * QT * 4), 4, lane * 4, 0, 0, 0);
+    }
+    ci += QT;
+    if (ci >= job.qb) {
+      ci = job.qa;
+      ++ch;
     }
   };
-  auto store = [&](uint8_t* to) __attribute__((always_inline)) {
-    sq.store(to);
-    so.store(to + BYTES);
-    if (threadIdx.x < 2 * QT) reinterpret_cast<float*>(to + 2 * BYTES)[threadIdx.x] = s_row;
+  // queries i0 .. against the keys k0 .. k1: nothing (0), something (1) or all (2)
+  auto seen = [&](int i0, int count, int k0, int k1) __attribute__((always_inline)) {
+    const int pa = a.q_start + i0, pe = a.q_start + min(i0 + count, min(job.qb, iend)) - 1;
+    if (pa > pe || k0 >= len || k0 > pe + a.look || (k0 >= a.sinks && k1 <= pa - a.win)) return 0;
+    return pe - pa == count - 1 && k1 < len && k1 <= pa + a.look && (k0 > pe - a.win || k1 < a.sinks) ? 2 : 1;
   };
-  using Cp = Copy<T, DP, QT, NT>;
-  auto body = [&](auto stage, int x) __attribute__((always_inline)) {
-    uint8_t* qs = smem + decltype(stage)::value * STAGE;
+  if (threadIdx.x == 0) found = -1;
+  if (n > 0) {
+    Copy<T, DP, KB, NT>::rows(smem, row_of<T>(a.v, b, hk, job.tile * KB), (int)(a.v.st * sizeof(T)),
+                              len - job.tile * KB, a.d);
+    for (int x = 0; x < RING - 1 && x < n; ++x) copy(x);
+  }
+  __syncthreads();
+  int i0 = job.qa, h = h0, stage = 0, to = RING - 1;
+  for (int x = 0; x < n; ++x) {
+    uint8_t* qs = ring + stage * STAGE;
     uint8_t* os = qs + BYTES;
-    float* rows = reinterpret_cast<float*>(qs + 2 * BYTES);
-    const int i0 = job.qa + (x % steps) * QT;
-    // the step against the workgroup's and the wave's keys: nothing, something or all
-    auto seen = [&](int k0, int k1) __attribute__((always_inline)) {
-      const int pa = a.q_start + i0, pe = a.q_start + min(i0 + QT, min(job.qb, iend)) - 1;
-      if (pa > pe || k0 >= len || k0 > pe + a.look || (k0 >= a.sinks && k1 <= pa - a.win)) return 0;
-      return pe - pa == QT - 1 && k1 < len && k1 <= pa + a.look && (k0 > pe - a.win || k1 < a.sinks) ? 2 : 1;
-    };
     uint64_t bado = 0;
-    if (seen(job.tile * KB, job.tile * KB + KB - 1) != 2 &&
+    if (seen(i0, QT, job.tile * KB, job.tile * KB + KB - 1) != 2 &&
         __builtin_expect((Copy<T, DP, 2 * QT, NT>::holds_nonfinite(qs, x, &found)), 0)) {
       const uint64_t badq = Cp::scrub(qs, mask);
       bado = Cp::scrub(os, mask);
       // a query's infinity or NaN makes its weights NaN, a cotangent's their cotangents
+      float* rows = reinterpret_cast<float*>(qs + 2 * BYTES);
       if (threadIdx.x < QT) {
         if (badq >> threadIdx.x & 1) rows[threadIdx.x] = __builtin_nanf("");
         if (bado >> threadIdx.x & 1) rows[QT + threadIdx.x] = __builtin_nanf("");
       }
       __syncthreads();
     }
-    if (x + 1 < n) load(x + 1);
-    const int what = seen(kw, kw + 31);
-    if (what) {
-      u32x4 f0[L::KS], f1[L::KS], f2[L::KS], f3[L::KS];
-      f32x16 sa, da, sb, db;
-      RowsB<T> pa, da16, pb, db16;
-      const int lo = first - i0;
-      // the accumulators' first values: rows 8e + 4 half .. of half RB
-      auto start = [&](auto rb, f32x16& s, f32x16& d) __attribute__((always_inline)) {
+    if (x + RING - 1 < n) copy(to);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(rows + decltype(rb)::value + 8 * e + 4 * half);
-          const f32x4 y = *reinterpret_cast<const f32x4*>(rows + QT + decltype(rb)::value + 8 * e + 4 * half);
+    for (int rb = 0; rb < QW; rb += 32) {
+      const int r0 = qh * QW + rb;   // the 32 queries of the step
+      const int what = seen(i0 + r0, 32, kw, kw + 31);
+      if (!what) continue;
+      const uint8_t *qt = qs + r0 * L::PITCH, *ot = os + r0 * L::PITCH;
+      // the accumulators start from nlse and ndelta of rows 8e + 4 half ..
+      const uint32_t at = lds_addr(qs + 2 * BYTES) + r0 * 4 + 16 * half;
+      const uint32_t ad[4] = {at, at + 32, at + 64, at + 96};
+      f32x16 s, d;
+      auto start = [&](f32x16& acc, auto off) __attribute__((always_inline)) {
+        u32x4 r[4];
+        read_rows4<decltype(off)::value>(r, ad);
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            s[4 * e + u] = x[u];
-            d[4 * e + u] = y[u];
-          }
+        for (int e = 0; e < 16; ++e) acc[e] = __uint_as_float(r[e >> 2][e & 3]);
+      };
+      start(s, std::integral_constant<int, 0>{});
+      mma_dot_add<T, DP, 0>(s, qt, kf);
+      start(d, std::integral_constant<int, 4 * QT>{});
+      mma_dot_lds<DP>(d, ot, smem + 32 * kg * L::PITCH);
+      if (what == 1) {
+        const int lo = first - i0 - r0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const bool see = (uint32_t)(8 * (e >> 2) + (e & 3) - lo) <= span;
+          s[e] = see ? s[e] : neg_inf();
+          d[e] = see ? d[e] : 0.0f;
         }
-      };
-      auto hide = [&](auto rb, f32x16& s, f32x16& d) __attribute__((always_inline)) {
-        if (what == 2) return;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const bool see = (uint32_t)(decltype(rb)::value + 8 * (r >> 2) + (r & 3) - lo) <= span;
-          s[r] = see ? s[r] : neg_inf();
-          d[r] = see ? d[r] : 0.0f;
-        }
-      };
-      // weights and their cotangents of elements e, e + 1
-      auto weigh = [&](int e, const f32x16& s, const f32x16& d, RowsB<T>& p16, RowsB<T>& d16)
-          __attribute__((always_inline)) {
-        const float p0 = __builtin_amdgcn_exp2f(s[e] * c), p1 = __builtin_amdgcn_exp2f(s[e + 1] * c);
-        uint32_t x = pack_bf16(p0, p1), y = pack_bf16(p0 * d[e], p1 * d[e + 1]);
-        pin(x);
-        pin(y);
-        p16.v[e >> 3][(e & 7) >> 1] = x;
-        d16.v[e >> 3][(e & 7) >> 1] = y;
-      };
-      const std::integral_constant<int, 0> A;
-      const std::integral_constant<int, 32> B;
-      start(A, sa, da);
-      fr.template rows<0>(f0, qs);
-      fr.template rows<0>(f1, os);
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (DP > 64) {
-        fr.template rows<32>(f2, qs);
-        fr.template rows<32>(f3, os);
-        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int i = 0; i < L::KS; ++i) {
-        mma_chunk<T>(sa, f0[i], kf[i]);
-        mma_chunk<T>(da, f1[i], vf[i]);
+      for (int e = 0; e < 16; ++e) {
+        s[e] = __builtin_amdgcn_exp2f(s[e] * c);
+        d[e] *= s[e];
       }
-      hide(A, sa, da);
-      start(B, sb, db);
-      if constexpr (DP == 64) {
-        fr.template rows<32>(f2, qs);
-        fr.template rows<32>(f3, os);
-      }
-      fr.template cols<0>(f0, os);
-      fr.template cols<0>(f1, qs);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < L::KS; ++i) {
-        mma_chunk<T>(sb, f2[i], kf[i]);
-        mma_chunk<T>(db, f3[i], vf[i]);
-#pragma unroll
-        for (int e = 0; e < 16 / L::KS; e += 2) weigh(16 / L::KS * i + e, sa, da, pa, da16);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      hide(B, sb, db);
-      fr.template cols<32>(f2, os);
-      fr.template cols<32>(f3, qs);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < 2 * NB; ++i) {
-        mma_chunk<T>(dv[i >> 1], f0[i], pa.v[i & 1]);
-        mma_chunk<T>(dk[i >> 1], f1[i], da16.v[i & 1]);
-#pragma unroll
-        for (int e = 0; e < 8 / NB; e += 2) weigh(8 / NB * i + e, sb, db, pb, db16);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int i = 0; i < 2 * NB; ++i) {
-        mma_chunk<T>(dv[i >> 1], f2[i], pb.v[i & 1]);
-        mma_chunk<T>(dk[i >> 1], f3[i], db16.v[i & 1]);
-      }
+      mma_rows<T, DP, NB, 0>(dv, RowsB<T>(s), ot, 0);
+      mma_rows<T, DP, NB, 0>(dk, RowsB<T>(d), qt, 0);
     }
 #pragma unroll 1
     for (; __builtin_expect(bado != 0, 0); bado &= bado - 1) {   // dv takes the cotangents' infinities and NaN
-      const int i = i0 + __builtin_ctzll(bado);
-      add_nonfinite<T, NB>(dv, row_of<T>(g.dout, b, h0 + x / steps, i), i >= ilo && i <= ihi, 0, a.d);
+      const int r = __builtin_ctzll(bado), i = i0 + r;
+      add_nonfinite<T, NB>(dv, row_of<T>(g.dout, b, h, i), r / QW == qh && i >= ilo && i <= ihi, 0, a.d);
     }
-    if (x + 1 < n) store(smem + (1 - decltype(stage)::value) * STAGE);
-    __syncthreads();
-  };
-  if (threadIdx.x == 0) found = -1;
-  pin(kf);
-  pin(vf);
-  if (n > 0) {
-    load(0);
-    store(smem);
+    i0 += QT;
+    if (i0 >= job.qb) {
+      i0 = job.qa;
+      ++h;
+    }
+    stage = stage + 1 == RING ? 0 : stage + 1;
+    to = to + 1 == RING ? 0 : to + 1;
+    // the next step's copies are done; those of the steps behind it go on
+    if (RING == 3 && x + 2 < n) {
+      if (wave < 2) wait_loads<2 * Cp::N + 1>();
+      else wait_loads<2 * Cp::N>();
+    } else {
+      wait_loads<0>();
+    }
+    barrier_only();
   }
-  __syncthreads();
-  for (int x = 0; x < n; x += 2) {
-    body(std::integral_constant<int, 0>{}, x);
-    if (x + 1 < n) body(std::integral_constant<int, 1>{}, x + 1);
+  if constexpr (QH == 2) {   // the second wave's sums to the first, dk and then dv
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      f32x16 (&acc)[NB] = which ? dv : dk;
+      float* to = reinterpret_cast<float*>(smem) + (kg * NB * 16) * 64 + lane;
+      static_assert(4 * NB * 16 * 64 * 4 <= VB + RING * STAGE, "sums of four waves");
+      __syncthreads();
+      if (qh == 1)
+#pragma unroll
+        for (int x = 0; x < NB; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) to[(x * 16 + e) * 64] = acc[x][e];
+      __syncthreads();
+      if (qh == 0)
+#pragma unroll
+        for (int x = 0; x < NB; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[x][e] += to[(x * 16 + e) * 64];
+    }
+    if (qh == 1) return;
   }
   if (job.slot < 0) {
     store_row<T, NB>(row_of<T>(g.dk, b, hk, jc), dk, a.scale, 0, a.d, j < a.n_kv, !live);
     store_row<T, NB>(row_of<T>(g.dv, b, hk, jc), dv, 1.0f, 0, a.d, j < a.n_kv, !live);
   } else {
-    float* part = g.part + ((int64_t)bk * g.plan.slots() + job.slot) * 2 * KB * a.d + (int64_t)(32 * wave + (lane & 31)) * a.d;
+    float* part = g.part + ((int64_t)bk * g.plan.slots() + job.slot) * 2 * KB * a.d + (int64_t)(32 * kg + (lane & 31)) * a.d;
     store_row<float, NB>(part, dk, a.scale, 0, a.d, true, !live);
     store_row<float, NB>(part + (int64_t)KB * a.d, dv, 1.0f, 0, a.d, true, !live);
   }
@@ -676,7 +652,7 @@ hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
   }
   if (a.n_kv > 0) {
     if constexpr (H16 && DP <= 128)
-      k_window_dkv16<DP, 4><<<(unsigned)(bk * g.plan.jobs()), 256, 0, s>>>(g);
+      k_window_dkv16<DP, DP / 64><<<(unsigned)(bk * g.plan.jobs()), 256 * (DP / 64), 0, s>>>(g);
     else
       k_window_dkv<T, DP, DO, QT, 4><<<(unsigned)(bk * g.plan.jobs() * (DP / DO)), 256, 0, s>>>(g);
     const DkvPlan& pl = g.plan;
