@@ -772,48 +772,66 @@ def rmsnorm_out_backward(o, dy, weight=None, eps=1e-6, with_dweight=True, out=No
 
 # ---- the attention half of a hybrid layer (strided tensors are taken as they lie)
 
+# These calls can be as short as a kernel launch, so their checks read each
+# property of a tensor once.
+
 def _io(t, name):
     import torch
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return IO_BF16
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return IO_FP32
     raise LactError(-1, f"unsupported {name} dtype {t.dtype}")
 
 
-def _view(t, batch=0, head=1, token=2):
-    """LactView of a tensor whose last dimension is a vector; batch None: no batch dimension."""
-    return LactView(t.data_ptr(), 0 if batch is None else t.stride(batch), t.stride(head), t.stride(token))
+def _view(t):
+    """LactView of a tensor [batch, head, token, d]."""
+    s = t.stride()
+    return LactView(t.data_ptr(), s[0], s[1], s[2])
+
+
+def _view_t(t):
+    """LactView of a tensor [batch, token, head, d]."""
+    s = t.stride()
+    return LactView(t.data_ptr(), s[0], s[2], s[1])
+
+
+def _view_n(t):
+    """LactView of a tensor [token, head, d]."""
+    s = t.stride()
+    return LactView(t.data_ptr(), 0, s[1], s[0])
 
 
 def _check(t, name, shape, like):
     """A tensor of `shape`, of like's type and on its device, vectors consecutive."""
-    if tuple(t.shape) != tuple(shape):
+    dev = like.get_device()
+    if t.shape == shape and t.dtype is like.dtype and dev >= 0 and t.get_device() == dev and \
+            (t.stride(-1) == 1 or shape[-1] <= 1):
+        return
+    if t.shape != shape:
         raise LactError(-1, f"{name} must be {list(shape)}, not {list(t.shape)}")
     if t.dtype != like.dtype:
         raise LactError(-1, f"{name} must be {like.dtype}, not {t.dtype}")
-    if t.device != like.device or not t.is_cuda:
-        raise LactError(-1, f"{name} must be a device tensor on {like.device}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise LactError(-1, f"{name}'s last dimension must be contiguous")
+    if dev < 0 or t.get_device() != dev:
+        raise LactError(-1, f"{name} must be a device tensor, on the first one's device")
+    raise LactError(-1, f"{name}'s last dimension must be contiguous")
 
 
 def _check_aux(t, name, shape, dtype, like):
-    if t is None:
-        return
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous() or t.device != like.device:
+    if t is not None and (t.shape != shape or t.dtype is not dtype or t.get_device() != like.get_device()
+                          or not t.is_contiguous()):
         raise LactError(-1, f"{name} must be a contiguous {dtype} tensor {list(shape)} on {like.device}")
 
 
 def _call(fn, like, stream, *args):
     """fn(*args, stream) on like's device and its current stream (or `stream`)."""
     import torch
-    i = like.device.index
+    i = like.get_device()
     if torch.cuda.current_device() == i:
-        rc = fn(*args, torch.cuda.current_stream(i).cuda_stream if stream is None else stream)
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(i) if stream is None else stream)
     else:
         with torch.cuda.device(i):
-            rc = fn(*args, torch.cuda.current_stream(i).cuda_stream if stream is None else stream)
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(i) if stream is None else stream)
     if rc:
         _raise(rc)
 
@@ -873,7 +891,7 @@ def qk_norm_rope(q, k, wq=None, wk=None, inv_freq=None, *, positions=None, pos0=
     qn, kn = out
     _check(qn, "qn", (B, H, n, d), q)
     _check(kn, "kn", (B, k.shape[2], n, d), q)
-    _call(lib().lact_qk_norm_rope, q, stream, desc, _view(q, 0, 2, 1), _view(k, 0, 2, 1), _p(wq), _p(wk),
+    _call(lib().lact_qk_norm_rope, q, stream, desc, _view_t(q), _view_t(k), _p(wq), _p(wk),
           _p(inv_freq) if desc.rot else None, _p(positions), _view(qn), _view(kn))
     return qn, kn
 
@@ -905,9 +923,9 @@ def qk_norm_rope_backward(q, k, dqn, dkn, wq=None, wk=None, inv_freq=None, *, po
     nb = 0
     if dwq is not None or dwk is not None:
         workspace, nb = _workspace(lib().lact_qk_norm_rope_backward_workspace_bytes, desc, workspace, q)
-    _call(lib().lact_qk_norm_rope_backward, q, stream, desc, _view(q, 0, 2, 1), _view(k, 0, 2, 1), _p(wq), _p(wk),
-          _p(inv_freq) if desc.rot else None, _p(positions), _view(dqn), _view(dkn), _view(dq, 0, 2, 1),
-          _view(dk, 0, 2, 1), _p(dwq), _p(dwk), _p(workspace), nb)
+    _call(lib().lact_qk_norm_rope_backward, q, stream, desc, _view_t(q), _view_t(k), _p(wq), _p(wk),
+          _p(inv_freq) if desc.rot else None, _p(positions), _view(dqn), _view(dkn), _view_t(dq),
+          _view_t(dk), _p(dwq), _p(dwk), _p(workspace), nb)
     return dq, dk, dwq, dwk
 
 
@@ -1000,8 +1018,8 @@ def paged_append(k, v, k_cache, v_cache, table, lens, cu_new, *, stream=None):
     if k.shape[1] != desc.Hkv:
         raise LactError(-1, "k must be [n_new, Hkv, d]")
     _check(v, "v", k.shape, k)
-    _call(lib().lact_paged_append, k, stream, desc, _view(k, None, 1, 0), _view(v, None, 1, 0), _view(k_cache, 0, 2, 1),
-          _view(v_cache, 0, 2, 1), _p(table), _p(lens), _p(cu_new))
+    _call(lib().lact_paged_append, k, stream, desc, _view_n(k), _view_n(v), _view_t(k_cache),
+          _view_t(v_cache), _p(table), _p(lens), _p(cu_new))
 
 
 def paged_attention(q, k_cache, v_cache, table, lens, cu_new, *, window=None, sinks=0, scale=None, out=None,
@@ -1015,8 +1033,8 @@ def paged_attention(q, k_cache, v_cache, table, lens, cu_new, *, window=None, si
     o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
     _check(o, "o", q.shape, q)
     workspace, nb = _workspace(lib().lact_paged_attention_workspace_bytes, desc, workspace, q)
-    _call(lib().lact_paged_attention, q, stream, desc, _view(q, None, 1, 0), _view(k_cache, 0, 2, 1),
-          _view(v_cache, 0, 2, 1), _p(table), _p(lens), _p(cu_new), _view(o, None, 1, 0), _p(workspace), nb)
+    _call(lib().lact_paged_attention, q, stream, desc, _view_n(q), _view_t(k_cache),
+          _view_t(v_cache), _p(table), _p(lens), _p(cu_new), _view_n(o), _p(workspace), nb)
     return o
 
 

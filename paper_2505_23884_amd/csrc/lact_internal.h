@@ -596,7 +596,7 @@ struct RopeArgs {
   float eps;
   float* dw[2];                 // reverse: [d] or [heads][d], or nullptr
   float* part;                  // reverse: partial sums of dw
-  int tb, hs, nblk;             // tokens a step, head parts (forward), workgroups
+  int tb, hs[2], nblk[2];       // tokens a step (a power of two), head parts (forward), workgroups of q and k
 };
 void rope_plan(RopeArgs& a, bool bf16, bool bwd);
 size_t rope_part_floats(const RopeArgs& a);

@@ -5,11 +5,12 @@
 //   g = R(-pos) dy,  n = w o g,  dx = r n - (r^3 / d) x <x, n>,  dw = sum g o x r
 //
 // Bound by HBM: x is read and y written once (the reverse reads x and dy and
-// writes dx). A workgroup takes `tb` tokens of every head: their angles are
-// computed once, in fp64 (a position of 10^5 times a frequency keeps 10^-11
-// of a turn) reduced to a fraction of a turn, into LDS, and used by all heads.
-// A group of lanes owns a vector; a lane holds two pieces of GE elements that
-// rotate into each other, so nothing is exchanged but the sum of squares.
+// writes dx). A workgroup takes `tb` tokens of q's heads or of k's: their
+// angles are computed once, in fp64 (a position of 10^5 times a frequency
+// keeps 10^-11 of a turn) reduced to a fraction of a turn, into LDS, and used
+// by all heads. A group of lanes owns a vector; a lane holds two pieces of GE
+// elements that rotate into each other, so nothing is exchanged but the sum of
+// squares.
 #include <algorithm>
 
 #include "lact_attn.h"
@@ -22,33 +23,36 @@ using namespace attn;
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeTokens = 16;     // most tokens a step
-constexpr int kRopeMaxD = 512;
 
+// GE elements as they lie in memory, and as floats.
 template <typename T, int GE>
-__device__ __forceinline__ void load_piece(float (&x)[GE], const T* p) {
-  if constexpr (sizeof(T) == 4) {
-    static_assert(GE == 4, "fp32 pieces are 16 bytes");
-    const f32x4 u = *reinterpret_cast<const f32x4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = u[i];
-  } else {
-    uint32_t u[GE / 2];
-    if constexpr (GE == 8) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+struct Raw {
+  static_assert(sizeof(T) == 2 || GE == 4, "fp32 pieces are 16 bytes");
+  static constexpr int N = GE * (int)sizeof(T) / 4;
+  uint32_t u[N];
+  __device__ __forceinline__ void load(const T* p, bool ok) {
+    if constexpr (N == 4) {
+      const u32x4 v = ok ? *reinterpret_cast<const u32x4*>(p) : u32x4{};
 #pragma unroll
       for (int i = 0; i < 4; ++i) u[i] = v[i];
     } else {
-      const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+      const u32x2 v = ok ? *reinterpret_cast<const u32x2*>(p) : u32x2{};
       u[0] = v[0];
       u[1] = v[1];
     }
+  }
+  __device__ __forceinline__ void get(float (&x)[GE]) const {
 #pragma unroll
-    for (int i = 0; i < GE / 2; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    for (int i = 0; i < N; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        x[i] = __uint_as_float(u[i]);
+      } else {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+      }
     }
   }
-}
+};
 
 template <typename T, int GE>
 __device__ __forceinline__ void store_piece(T* p, const float (&x)[GE]) {
@@ -79,31 +83,42 @@ struct Pieces {
   }
 };
 
-// Rotation of a lane's pieces by the angles of its token (cs: cos, sin pairs
-// of the token's rot / 2 frequencies), by -angle with s = -1.
+// cos and sin of a lane's pairs, for the token whose rot / 2 (cos, sin) pairs
+// are at cs, and the rotation of its pieces by them (by -angle with s = -1).
 template <int GE>
-__device__ __forceinline__ void turn(const RopeArgs& a, const Pieces<GE>& pc, float (&x)[2][GE], const f32x2* cs, float s) {
-  if (pc.turned) {
+struct Angles {
+  float c[GE], s[GE];   // half-split: pair i; interleaved: pair i / 2 of piece i % 2 ...
+  __device__ __forceinline__ void load(const RopeArgs& a, const Pieces<GE>& pc, const f32x2* cs) {
 #pragma unroll
     for (int i = 0; i < GE; ++i) {
-      const f32x2 t = cs[pc.e[0] + i];
-      const float u = x[0][i], v = x[1][i], sn = s * t[1];
-      x[0][i] = u * t[0] - v * sn;
-      x[1][i] = v * t[0] + u * sn;
+      // interleaved: pairs 0 .. GE / 2 - 1 are piece 0's, the rest piece 1's
+      const int k = i / (GE / 2), e = pc.e[k] + 2 * (i % (GE / 2));
+      const bool on = a.interleaved ? e < a.rot : pc.turned;
+      const f32x2 t = on ? cs[a.interleaved ? e >> 1 : pc.e[0] + i] : f32x2{1.0f, 0.0f};
+      c[i] = t[0];
+      s[i] = t[1];
     }
-  } else if (a.interleaved) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int i = 0; i < GE; i += 2) {
-        if (pc.e[k] + i >= a.rot) continue;
-        const f32x2 t = cs[(pc.e[k] + i) >> 1];
-        const float u = x[k][i], v = x[k][i + 1], sn = s * t[1];
-        x[k][i] = u * t[0] - v * sn;
-        x[k][i + 1] = v * t[0] + u * sn;
-      }
   }
-}
+  __device__ __forceinline__ void turn(const RopeArgs& a, const Pieces<GE>& pc, float (&x)[2][GE], float sign) const {
+    if (pc.turned) {
+#pragma unroll
+      for (int i = 0; i < GE; ++i) {
+        const float u = x[0][i], v = x[1][i], sn = sign * s[i];
+        x[0][i] = u * c[i] - v * sn;
+        x[1][i] = v * c[i] + u * sn;
+      }
+    } else if (a.interleaved) {
+#pragma unroll
+      for (int i = 0; i < GE; ++i) {
+        const int k = i / (GE / 2), e = 2 * (i % (GE / 2));
+        if (pc.e[k] + e >= a.rot) continue;
+        const float u = x[k][e], v = x[k][e + 1], sn = sign * s[i];
+        x[k][e] = u * c[i] - v * sn;
+        x[k][e + 1] = v * c[i] + u * sn;
+      }
+    }
+  }
+};
 
 // cos and sin of tokens t0 .. of the step into cs[token][rot / 2]
 __device__ __forceinline__ void angles(const RopeArgs& a, f32x2* cs, int64_t t0, int count) {
@@ -119,191 +134,241 @@ __device__ __forceinline__ void angles(const RopeArgs& a, f32x2* cs, int64_t t0,
   }
 }
 
+// Sum over the G lanes of a group (a power of two): within 16 lanes by DPP,
+// an instruction a step.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
 __device__ __forceinline__ float group_add(float v, int G) {
-  for (int o = G >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  if (G >= 2) v = dpp_add<0xb1>(v);    // lanes 1 apart
+  if (G >= 4) v = dpp_add<0x4e>(v);    // 2 apart
+  if (G >= 8) v = dpp_add<0x141>(v);   // the other four of eight
+  if (G >= 16) v = dpp_add<0x140>(v);  // the other eight of sixteen
+  if (G >= 32) v += __shfl_xor(v, 16, 64);
+  if (G >= 64) v += __shfl_xor(v, 32, 64);
   return v;
 }
 
-// One token of the step and one head (q's, then k's).
-struct RopeAt {
-  int which, h;
+// Batch and token of token t.
+struct RopeToken {
   int64_t b, l;
-  __device__ __forceinline__ RopeAt(const RopeArgs& a, int64_t t, int head) {
-    which = head >= a.H[0];
-    h = which ? head - a.H[0] : head;
-    if (a.B * a.n < ((int64_t)1 << 31)) {
-      const uint32_t bi = (uint32_t)t / (uint32_t)a.n;
-      b = bi;
-      l = (uint32_t)t - bi * (uint32_t)a.n;
-    } else {
-      b = t / a.n;
-      l = t - b * a.n;
-    }
+  __device__ __forceinline__ RopeToken(const RopeArgs& a, int64_t t) {
+    const uint32_t bi = (uint32_t)t / (uint32_t)a.n;   // B n < 2^31
+    b = bi;
+    l = (uint32_t)t - bi * (uint32_t)a.n;
   }
   template <typename T>
-  __device__ __forceinline__ T* row(const AttnView& v) const {
+  __device__ __forceinline__ T* row(const AttnView& v, int h) const {
     return reinterpret_cast<T*>(v.p) + b * v.sb + h * v.sh + l * v.st;
   }
 };
 
 template <typename T, int GE>
+__device__ __forceinline__ void load_pieces(Raw<T, GE> (&x)[2], const Pieces<GE>& pc, const T* row) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) x[k].load(row + pc.e[k], pc.ok[k]);
+}
+
+// A lane's weights, 1 without any.
+template <int GE>
+__device__ __forceinline__ void load_weights(float (&w)[2][GE], const Pieces<GE>& pc, const float* from) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int i = 0; i < GE; ++i) w[k][i] = from && pc.ok[k] ? from[pc.e[k] + i] : 1.0f;
+}
+
+// A workgroup takes q's heads or k's (the first nblk[0] workgroups q's). Its
+// groups stand for tokens gi % tb of the step and for every (groups / tb)-th
+// head from gi / tb on: the token's angles stay in registers over the heads.
+template <typename T, int GE>
 __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeArgs a, int G) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   f32x2* cs = reinterpret_cast<f32x2*>(smem);
-  const int64_t tokens = (int64_t)a.B * a.n, t0 = (int64_t)(blockIdx.x / a.hs) * a.tb;
-  const int count = (int)(tokens - t0 < a.tb ? tokens - t0 : a.tb), heads = a.H[0] + a.H[1];
-  const int part = blockIdx.x % a.hs, h0 = heads * part / a.hs, h1 = heads * (part + 1) / a.hs;
+  const int which = (int)blockIdx.x >= a.nblk[0], blk = blockIdx.x - (which ? a.nblk[0] : 0);
+  const int hs = a.hs[which], H = a.H[which];
+  const int64_t tokens = (int64_t)a.B * a.n, t0 = (int64_t)(blk / hs) * a.tb;
+  const int count = (int)(tokens - t0 < a.tb ? tokens - t0 : a.tb);
+  const int part = blk % hs, h0 = H * part / hs, h1 = H * (part + 1) / hs;
   angles(a, cs, t0, count);
   __syncthreads();
-  const int lg = threadIdx.x & (G - 1), NG = kRopeThreads / G;
+  const int lg = threadIdx.x & (G - 1), NG = kRopeThreads / G, gi = threadIdx.x / G;
+  const int ti = gi & (a.tb - 1), step = NG / a.tb;
+  if (ti >= count) return;
   const Pieces<GE> pc(a, lg);
-  for (int v = threadIdx.x / G; v < count * (h1 - h0); v += NG) {
-    const int ti = v % count, head = h0 + v / count;
-    const RopeAt at(a, t0 + ti, head);
-    const T* src = at.row<const T>(a.x[at.which]);
+  const RopeToken at(a, t0 + ti);
+  Angles<GE> an;
+  an.load(a, pc, cs + ti * (a.rot / 2));
+  float w[2][GE];
+  if (!a.per_head) load_weights<GE>(w, pc, a.w[which]);
+  const AttnView &xv = a.x[which], &yv = a.y[which];
+  int h = h0 + gi / a.tb;
+  Raw<T, GE> next[2];   // the loads run one vector ahead
+  if (h < h1) load_pieces<T, GE>(next, pc, at.row<const T>(xv, h));
+  for (; h < h1; h += step) {
     float x[2][GE];
+    next[0].get(x[0]);
+    next[1].get(x[1]);
+    if (h + step < h1) load_pieces<T, GE>(next, pc, at.row<const T>(xv, h + step));
+    if (a.per_head) load_weights<GE>(w, pc, a.w[which] ? a.w[which] + (int64_t)h * a.d : nullptr);
     float ss = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      if (pc.ok[k]) load_piece<T, GE>(x[k], src + pc.e[k]);
-#pragma unroll
-      for (int i = 0; i < GE; ++i) {
-        if (!pc.ok[k]) x[k][i] = 0.0f;
-        ss += x[k][i] * x[k][i];
-      }
-    }
-    const float r = 1.0f / sqrtf(group_add(ss, G) / (float)a.d + a.eps);
-    const float* w = a.w[at.which];
-    if (w && a.per_head) w += (int64_t)at.h * a.d;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int i = 0; i < GE; ++i) x[k][i] *= w && pc.ok[k] ? r * w[pc.e[k] + i] : r;
-    turn<GE>(a, pc, x, cs + ti * (a.rot / 2), 1.0f);
-    T* dst = at.row<T>(a.y[at.which]);
+      for (int i = 0; i < GE; ++i) ss += x[k][i] * x[k][i];
+    const float r = 1.0f / sqrtf(group_add(ss, G) / (float)a.d + a.eps);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < GE; ++i) x[k][i] *= r * w[k][i];
+    an.turn(a, pc, x, 1.0f);
+    T* dst = at.row<T>(yv, h);
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       if (pc.ok[k]) store_piece<T, GE>(dst + pc.e[k], x[k]);
   }
 }
 
+// One vector of the reverse: dx to its place, and its part of dw added to acc.
+template <typename T, int GE>
+__device__ __forceinline__ void rope_back(const RopeArgs& a, const Pieces<GE>& pc, const Angles<GE>& an,
+                                          const RopeToken& at, int which, int h, int G, const float (&w)[2][GE],
+                                          float (&acc)[2][GE], const Raw<T, GE> (&rx)[2], const Raw<T, GE> (&rg)[2]) {
+  float x[2][GE], g[2][GE], n[2][GE];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    rx[k].get(x[k]);
+    rg[k].get(g[k]);
+  }
+  an.turn(a, pc, g, -1.0f);
+  float ss = 0.0f, dot = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int i = 0; i < GE; ++i) {
+      n[k][i] = g[k][i] * w[k][i];
+      ss += x[k][i] * x[k][i];
+      dot += x[k][i] * n[k][i];
+    }
+  const float r = 1.0f / sqrtf(group_add(ss, G) / (float)a.d + a.eps);
+  const float c = r * r * r * (group_add(dot, G) / (float)a.d);
+  T* dst = at.row<T>(a.dx[which], h);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+#pragma unroll
+    for (int i = 0; i < GE; ++i) {
+      acc[k][i] += g[k][i] * x[k][i] * r;
+      n[k][i] = r * n[k][i] - c * x[k][i];
+    }
+    if (pc.ok[k]) store_piece<T, GE>(dst + pc.e[k], n[k]);
+  }
+}
+
 // The reverse. dw is summed per lane over the vectors of its group, over the
 // groups of the workgroup through LDS, and over the workgroups by
-// k_rope_dw_sum, all in a fixed order. With a weight per head the heads are
-// the outer loop and each head's sum is written as it ends.
+// k_rope_dw_sum, all in a fixed order. With a weight per head (PER_HEAD) the
+// heads are the outer loop, each head's sum is written as it ends, and the
+// angles are worked out again for each.
 template <typename T, int GE, bool PER_HEAD>
 __global__ __launch_bounds__(kRopeThreads) void k_rope_bwd(const RopeArgs a, int G) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   f32x2* cs = reinterpret_cast<f32x2*>(smem);
   float* red = reinterpret_cast<float*>(smem + (size_t)a.tb * (a.rot / 2) * 8);   // [NG][d]
-  const int64_t tokens = (int64_t)a.B * a.n;
-  const int heads = a.H[0] + a.H[1];
+  const int which = (int)blockIdx.x >= a.nblk[0], blk = blockIdx.x - (which ? a.nblk[0] : 0);
+  const int H = a.H[which];
+  const int64_t tokens = (int64_t)a.B * a.n, stride = (int64_t)a.nblk[which] * a.tb;
   const int lg = threadIdx.x & (G - 1), NG = kRopeThreads / G, gi = threadIdx.x / G;
+  const int ti = gi & (a.tb - 1), step = NG / a.tb;
   const Pieces<GE> pc(a, lg);
-  float acc[PER_HEAD ? 1 : 2][2][GE] = {};
-  const bool any_dw = a.dw[0] || a.dw[1];
-  // the sums of `which` (q or k), head slot `at` of this workgroup's partials
-  auto flush = [&](float (&s)[2][GE], int at) {
+  float acc[2][GE] = {}, w[2][GE];
+  // the workgroup's sums to `to`
+  auto flush = [&](float* to) {
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < GE; ++i) {
-        if (pc.ok[k]) red[gi * a.d + pc.e[k] + i] = s[k][i];
-        s[k][i] = 0.0f;
+        if (pc.ok[k]) red[gi * a.d + pc.e[k] + i] = acc[k][i];
+        acc[k][i] = 0.0f;
       }
     __syncthreads();
-    const int slots = PER_HEAD ? heads : 2;
     for (int e = threadIdx.x; e < a.d; e += kRopeThreads) {
       float sum = 0.0f;
       for (int g = 0; g < NG; ++g) sum += red[g * a.d + e];
-      a.part[((int64_t)blockIdx.x * slots + at) * a.d + e] = sum;
+      to[e] = sum;
     }
   };
-  auto vector = [&](int64_t t, int ti, int head) {
-    const RopeAt at(a, t, head);
-    const T* src = at.row<const T>(a.x[at.which]);
-    const T* gsrc = at.row<const T>(a.y[at.which]);
-    float x[2][GE], g[2][GE];
-    float ss = 0.0f, dot = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      if (pc.ok[k]) {
-        load_piece<T, GE>(x[k], src + pc.e[k]);
-        load_piece<T, GE>(g[k], gsrc + pc.e[k]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < GE; ++i) x[k][i] = g[k][i] = 0.0f;
-      }
-    }
-    turn<GE>(a, pc, g, cs + ti * (a.rot / 2), -1.0f);
-    const float* w = a.w[at.which];
-    if (w && a.per_head) w += (int64_t)at.h * a.d;
-    float n[2][GE];
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int i = 0; i < GE; ++i) {
-        n[k][i] = w && pc.ok[k] ? g[k][i] * w[pc.e[k] + i] : g[k][i];
-        ss += x[k][i] * x[k][i];
-        dot += x[k][i] * n[k][i];
-      }
-    const float r = 1.0f / sqrtf(group_add(ss, G) / (float)a.d + a.eps);
-    const float c = r * r * r * (group_add(dot, G) / (float)a.d);
-    T* dst = at.row<T>(a.dx[at.which]);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-#pragma unroll
-      for (int i = 0; i < GE; ++i) {
-        const float gxr = g[k][i] * x[k][i] * r;
-        if (PER_HEAD || !at.which) acc[0][k][i] += gxr;
-        else acc[PER_HEAD ? 0 : 1][k][i] += gxr;
-        n[k][i] = r * n[k][i] - c * x[k][i];
-      }
-      if (pc.ok[k]) store_piece<T, GE>(dst + pc.e[k], n[k]);
-    }
-  };
+  // partials: q's workgroups, then k's, PER_HEAD [head][d] each
+  float* part = a.part + ((int64_t)(which ? a.nblk[0] : 0) * (PER_HEAD ? a.H[0] : 1) + (int64_t)blk * (PER_HEAD ? H : 1)) * a.d;
+  auto tokens_of = [&](int64_t t0) { return (int)(tokens - t0 < a.tb ? tokens - t0 : a.tb); };
   if constexpr (PER_HEAD) {
-    for (int head = 0; head < heads; ++head) {
-      for (int64_t t0 = (int64_t)blockIdx.x * a.tb; t0 < tokens; t0 += (int64_t)gridDim.x * a.tb) {
-        const int count = (int)(tokens - t0 < a.tb ? tokens - t0 : a.tb);
+    for (int h = 0; h < H; ++h) {
+      load_weights<GE>(w, pc, a.w[which] ? a.w[which] + (int64_t)h * a.d : nullptr);
+      for (int64_t t0 = (int64_t)blk * a.tb; t0 < tokens; t0 += stride) {
+        const int count = tokens_of(t0);
         __syncthreads();
         angles(a, cs, t0, count);
         __syncthreads();
-        for (int v = gi; v < count; v += NG) vector(t0 + v, v, head);
+        if (gi >= count) continue;
+        Angles<GE> an;
+        an.load(a, pc, cs + gi * (a.rot / 2));
+        const RopeToken at(a, t0 + gi);
+        Raw<T, GE> x[2], g[2];
+        load_pieces<T, GE>(x, pc, at.row<const T>(a.x[which], h));
+        load_pieces<T, GE>(g, pc, at.row<const T>(a.y[which], h));
+        rope_back<T, GE>(a, pc, an, at, which, h, G, w, acc, x, g);
       }
-      if (any_dw) flush(acc[0], head);
+      if (a.dw[which]) flush(part + (int64_t)h * a.d);
     }
   } else {
-    for (int64_t t0 = (int64_t)blockIdx.x * a.tb; t0 < tokens; t0 += (int64_t)gridDim.x * a.tb) {
-      const int count = (int)(tokens - t0 < a.tb ? tokens - t0 : a.tb);
+    load_weights<GE>(w, pc, a.w[which]);
+    for (int64_t t0 = (int64_t)blk * a.tb; t0 < tokens; t0 += stride) {
+      const int count = tokens_of(t0);
       __syncthreads();
       angles(a, cs, t0, count);
       __syncthreads();
-      for (int v = gi; v < count * heads; v += NG) vector(t0 + v % count, v % count, v / count);
+      if (ti >= count) continue;
+      Angles<GE> an;
+      an.load(a, pc, cs + ti * (a.rot / 2));
+      const RopeToken at(a, t0 + ti);
+      int h = gi / a.tb;
+      Raw<T, GE> nx[2], ng[2];   // the loads run one vector ahead
+      auto load = [&](int head) {
+        load_pieces<T, GE>(nx, pc, at.row<const T>(a.x[which], head));
+        load_pieces<T, GE>(ng, pc, at.row<const T>(a.y[which], head));
+      };
+      if (h < H) load(h);
+      for (; h < H; h += step) {
+        Raw<T, GE> x[2], g[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          x[k] = nx[k];
+          g[k] = ng[k];
+        }
+        if (h + step < H) load(h + step);
+        rope_back<T, GE>(a, pc, an, at, which, h, G, w, acc, x, g);
+      }
     }
-    if (any_dw) {
-      flush(acc[0], 0);
-      flush(acc[1], 1);
-    }
+    if (a.dw[which]) flush(part);
   }
 }
 
-// dw[i] = sum over the workgroups' partials, 8 rows of them a time in a fixed
-// order; columns [0, n0) go to dw0, the rest to dw1.
-__global__ __launch_bounds__(256) void k_rope_dw_sum(const float* part, float* dw0, float* dw1, int nblk, int n0, int n) {
-  __shared__ float red[8][32];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
+// dw[i] = the sum of the workgroups' partials in a fixed order: 16 columns a
+// workgroup, 64 rows of partials a time.
+__global__ __launch_bounds__(1024) void k_rope_dw_sum(const float* part, float* dw, int nblk, int n) {
+  __shared__ float red[64][16];
+  const int x = threadIdx.x & 15, r = threadIdx.x >> 4, col = blockIdx.x * 16 + x;
   float s = 0.0f;
   if (col < n)
-    for (int x = r; x < nblk; x += 8) s += part[(int64_t)x * n + col];
-  red[r][threadIdx.x & 31] = s;
+    for (int i = r; i < nblk; i += 64) s += part[(int64_t)i * n + col];
+  red[r][x] = s;
   __syncthreads();
-  if (r || col >= n) return;
-#pragma unroll
-  for (int x = 1; x < 8; ++x) s += red[x][threadIdx.x];
-  float* out = col < n0 ? dw0 : dw1;
-  if (out) out[col < n0 ? col : col - n0] = s;
+  for (int o = 32; o > 0; o >>= 1) {
+    if (r < o) red[r][x] += red[r + o][x];
+    __syncthreads();
+  }
+  if (r == 0 && col < n) dw[col] = red[0][x];
 }
 
 // Elements of a piece: 16 bytes, or 4 elements where half the rotated ones
@@ -319,50 +384,60 @@ int lanes(const RopeArgs& a, int ge) {
 
 void rope_plan(RopeArgs& a, bool bf16, bool bwd) {
   const int64_t tokens = (int64_t)a.B * a.n;
-  const int heads = a.H[0] + a.H[1], groups = kRopeThreads / lanes(a, piece(a, bf16));
-  a.tb = (int)std::max<int64_t>(1, std::min<int64_t>(kRopeTokens, tokens / 1024));
+  const int groups = kRopeThreads / lanes(a, piece(a, bf16));
+  a.tb = 1;
+  while (a.tb * 2 <= std::min(kRopeTokens, groups) && tokens >= (int64_t)a.tb * 2048) a.tb *= 2;
   const int64_t steps = (tokens + a.tb - 1) / a.tb;
-  a.hs = 1;
-  if (bwd) {
-    a.nblk = (int)std::min<int64_t>(steps, 1024);
-  } else {
-    // few tokens: their heads over several workgroups, a vector a group at least
-    if (steps < 512)
-      a.hs = (int)std::max<int64_t>(1, std::min<int64_t>(heads * (int64_t)a.tb / groups, 512 / std::max<int64_t>(steps, 1)));
-    a.nblk = (int)std::min<int64_t>(steps * a.hs, 0x7fffffff);
+  for (int w = 0; w < 2; ++w) {
+    a.hs[w] = 1;
+    if (bwd) {
+      // three workgroups a CU, as many as its registers hold, q's and k's in proportion
+      // to the heads ([4, 8191, 16 + 4, 128], both directions: 768 in all 233 us, 1024
+      // 247, 2048 239); a partial sum of dw each
+      const int share = std::max(1, (int)((int64_t)768 * a.H[w] / (a.H[0] + a.H[1])));
+      a.nblk[w] = (int)std::min<int64_t>(steps, share);
+    } else {
+      // few tokens: their heads over several workgroups, a vector a group at least
+      const int64_t most = std::max<int64_t>(1, (int64_t)a.H[w] * a.tb / groups);
+      if (steps < 512) a.hs[w] = (int)std::min<int64_t>(most, 512 / std::max<int64_t>(steps, 1));
+      a.nblk[w] = (int)(steps * a.hs[w]);   // tokens < 2^31, and hs is 1 beyond 512 steps
+    }
   }
 }
 
 size_t rope_part_floats(const RopeArgs& a) {
-  return (size_t)a.nblk * (a.per_head ? a.H[0] + a.H[1] : 2) * a.d;
+  return ((size_t)a.nblk[0] * (a.per_head ? a.H[0] : 1) + (size_t)a.nblk[1] * (a.per_head ? a.H[1] : 1)) * a.d;
 }
 
 hipError_t launch_rope(const RopeArgs& a, bool bf16, hipStream_t s) {
   const size_t lds = (size_t)a.tb * (a.rot / 2) * 8;
-  const int ge = piece(a, bf16), G = lanes(a, ge);
-  if (!bf16) k_rope<float, 4><<<a.nblk, kRopeThreads, lds, s>>>(a, G);
-  else if (ge == 8) k_rope<__bf16, 8><<<a.nblk, kRopeThreads, lds, s>>>(a, G);
-  else k_rope<__bf16, 4><<<a.nblk, kRopeThreads, lds, s>>>(a, G);
+  const int ge = piece(a, bf16), G = lanes(a, ge), grid = a.nblk[0] + a.nblk[1];
+  if (!bf16) k_rope<float, 4><<<grid, kRopeThreads, lds, s>>>(a, G);
+  else if (ge == 8) k_rope<__bf16, 8><<<grid, kRopeThreads, lds, s>>>(a, G);
+  else k_rope<__bf16, 4><<<grid, kRopeThreads, lds, s>>>(a, G);
   return hipGetLastError();
 }
 
 template <typename T, int GE>
 static void bwd_one(const RopeArgs& a, int G, hipStream_t s) {
   const size_t lds = (size_t)a.tb * (a.rot / 2) * 8 + (size_t)(kRopeThreads / G) * a.d * 4;
-  if (a.per_head) k_rope_bwd<T, GE, true><<<a.nblk, kRopeThreads, lds, s>>>(a, G);
-  else k_rope_bwd<T, GE, false><<<a.nblk, kRopeThreads, lds, s>>>(a, G);
+  const int grid = a.nblk[0] + a.nblk[1];
+  if (a.per_head) k_rope_bwd<T, GE, true><<<grid, kRopeThreads, lds, s>>>(a, G);
+  else k_rope_bwd<T, GE, false><<<grid, kRopeThreads, lds, s>>>(a, G);
 }
 
 hipError_t launch_rope_bwd(const RopeArgs& a, bool bf16, hipStream_t s) {
   const int ge = piece(a, bf16), G = lanes(a, ge);
-  if (a.nblk > 0) {
+  if (a.nblk[0] > 0) {
     if (!bf16) bwd_one<float, 4>(a, G, s);
     else if (ge == 8) bwd_one<__bf16, 8>(a, G, s);
     else bwd_one<__bf16, 4>(a, G, s);
   }
-  if (a.dw[0] || a.dw[1]) {
-    const int n0 = (a.per_head ? a.H[0] : 1) * a.d, n = n0 + (a.per_head ? a.H[1] : 1) * a.d;
-    k_rope_dw_sum<<<(n + 31) / 32, 256, 0, s>>>(a.part, a.dw[0], a.dw[1], a.nblk, n0, n);
+  const float* part = a.part;
+  for (int w = 0; w < 2; ++w) {
+    const int n = (a.per_head ? a.H[w] : 1) * a.d;
+    if (a.dw[w]) k_rope_dw_sum<<<(n + 15) / 16, 1024, 0, s>>>(part, a.dw[w], a.nblk[w], n);
+    part += (size_t)a.nblk[w] * n;
   }
   return hipGetLastError();
 }
