@@ -81,9 +81,6 @@ struct Tile {
     else return (((row >> 1) & 1) << 2) | ((row >> 1) & 2) | ((row >> 3) & 1);
   }
   static __device__ __forceinline__ int off(int row, int chunk) { return row * PITCH + ((chunk ^ swz(row)) << 4); }
-  static __device__ __forceinline__ u32x4 row_chunk(const uint8_t* t, int row, int chunk) {
-    return *reinterpret_cast<const u32x4*>(t + off(row, chunk));
-  }
 };
 
 // acc += A B over the elements of one chunk pair (lanes 0-31 hold the first
@@ -153,8 +150,8 @@ __device__ __forceinline__ uint32_t finite_or_zero(uint32_t x) {
   }
 }
 
-// LDS fragments of 16-bit tiles are read in batches, each with its wait in the
-// same asm statement: the compiler would drain the copies in flight to the
+// LDS fragments are read in batches, each with its wait in the same asm
+// statement: the compiler would drain the copies in flight to the
 // other stage before every read that it can see, since it cannot tell the
 // stages apart. The waves of a SIMD cover each other's waits.
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
@@ -215,30 +212,45 @@ __device__ __forceinline__ void read_cols4(u32x2 (&r)[16], const uint32_t (&lo)[
       : "memory");
 }
 
+// One fp32 column over 32 rows: r[i] of row 8 (i / 4) + i % 4 from the lane's
+// first, whose addresses with the swizzles of rows 0 .. 3 and 8 .. 11 are a[0 .. 7].
+template <int OFF, int PITCH>
+__device__ __forceinline__ void read_col32(float (&r)[16], const uint32_t (&a)[8]) {
+  asm volatile(
+      "ds_read_b32 %0, %16 offset:%24\n\tds_read_b32 %1, %17 offset:%25\n\t"
+      "ds_read_b32 %2, %18 offset:%26\n\tds_read_b32 %3, %19 offset:%27\n\t"
+      "ds_read_b32 %4, %20 offset:%24\n\tds_read_b32 %5, %21 offset:%25\n\t"
+      "ds_read_b32 %6, %22 offset:%26\n\tds_read_b32 %7, %23 offset:%27\n\t"
+      "ds_read_b32 %8, %16 offset:%28\n\tds_read_b32 %9, %17 offset:%29\n\t"
+      "ds_read_b32 %10, %18 offset:%30\n\tds_read_b32 %11, %19 offset:%31\n\t"
+      "ds_read_b32 %12, %20 offset:%28\n\tds_read_b32 %13, %21 offset:%29\n\t"
+      "ds_read_b32 %14, %22 offset:%30\n\tds_read_b32 %15, %23 offset:%31\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7]),
+        "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]), "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15])
+      : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(a[4]), "v"(a[5]), "v"(a[6]), "v"(a[7]), "n"(OFF),
+        "n"(OFF + PITCH), "n"(OFF + 2 * PITCH), "n"(OFF + 3 * PITCH), "n"(OFF + 16 * PITCH), "n"(OFF + 17 * PITCH),
+        "n"(OFF + 18 * PITCH), "n"(OFF + 19 * PITCH)
+      : "memory");
+}
+
 // acc (32 rows of the tile from RB x 32 columns of b) += rows . b over d; b
 // holds a lane's column as Tile::KS chunks. N chunks a batch of reads.
 template <typename T, int DP, int RB, int N = (Tile<T, DP>::KS < 8 ? 4 : 8)>
 __device__ __forceinline__ void mma_dot_add(f32x16& acc, const uint8_t* tile, const u32x4 (&b)[(Tile<T, DP>::KS)]) {
   using L = Tile<T, DP>;
   const int lane = threadIdx.x & 63;
-  if constexpr (sizeof(T) == 2) {
-    // chunk 2c + half of the row: the lane's first address with bits 5 and up of c flipped in
-    const uint32_t a0 = lds_addr(tile) + L::off(lane & 31, lane >> 5);
+  // chunk 2c + half of the row: the lane's first address with bits 5 and up of c flipped in
+  const uint32_t a0 = lds_addr(tile) + L::off(lane & 31, lane >> 5);
 #pragma unroll
-    for (int c = 0; c < L::KS; c += N) {
-      uint32_t a[N];
-      u32x4 r[N];
+  for (int c = 0; c < L::KS; c += N) {
+    uint32_t a[N];
+    u32x4 r[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) a[i] = a0 ^ (uint32_t)((c + i) << 5);
-      if constexpr (N == 4) read_rows4<RB * L::PITCH>(r, a);
-      else read_rows8<RB * L::PITCH>(r, a);
+    for (int i = 0; i < N; ++i) a[i] = a0 ^ (uint32_t)((c + i) << 5);
+    if constexpr (N == 4) read_rows4<RB * L::PITCH>(r, a);
+    else read_rows8<RB * L::PITCH>(r, a);
 #pragma unroll
-      for (int i = 0; i < N; ++i) mma_chunk<T>(acc, r[i], b[c + i]);
-    }
-  } else {
-#pragma unroll
-    for (int c = 0; c < L::KS; ++c)
-      mma_chunk<T>(acc, L::row_chunk(tile, RB + (lane & 31), 2 * c + (lane >> 5)), b[c]);
+    for (int i = 0; i < N; ++i) mma_chunk<T>(acc, r[i], b[c + i]);
   }
 }
 template <typename T, int DP, int RB>
@@ -299,15 +311,24 @@ __device__ __forceinline__ void mma_rows(f32x16 (&acc)[NB], const RowsB<T>& b, c
         }
     }
   } else {
+    // the lane's column of block db0 in rows 4 half + 0 .. 3 and 8 further
+    uint32_t a[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = 8 * (i >> 2) + 4 * half;   // + i % 4: in the read's offset, but not in the swizzle
+      const int c = (lane & 31) >> 2;
+      a[i] = lds_addr(tile) + row * L::PITCH + ((c ^ L::swz(row + (i & 3))) << 4) + ((lane & 3) << 2);
+    }
 #pragma unroll
     for (int x = 0; x < NB; ++x) {
-      const int col = 32 * (db0 + x) + (lane & 31);
+      uint32_t ax[8];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int row = RB + 8 * (i >> 2) + 4 * half + (i & 3);
-        const float a = *reinterpret_cast<const float*>(tile + L::off(row, col >> 2) + ((col & 3) << 2));
-        acc[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, b.v[i], acc[x], 0, 0, 0);
-      }
+      for (int i = 0; i < 8; ++i) ax[i] = a[i] ^ (uint32_t)((db0 + x) << 7);
+      float r[16];
+      read_col32<RB * L::PITCH, L::PITCH>(r, ax);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        acc[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(r[i], b.v[i], acc[x], 0, 0, 0);
     }
   }
 }

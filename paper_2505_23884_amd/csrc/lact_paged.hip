@@ -18,6 +18,7 @@
 // tensors here, and a page outside the cache holds nothing (its positions are
 // masked, its slots not written).
 #include <algorithm>
+#include <type_traits>
 
 #include "lact_attn.h"
 #include "lact_internal.h"
@@ -170,11 +171,17 @@ __device__ __forceinline__ void finish(const PagedArgs& a, const RowOf& row, int
     *reinterpret_cast<f32x2*>(a.part + (int64_t)a.splits * rows * a.d + at * 2) = f32x2{st.m, l};
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(64 * kWaves) void k_paged_wide(const PagedArgs a) {
+// 16 bytes of zeros for the lanes of a copy that have nothing to read.
+__device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
+
+template <typename T, int DP, int KT, int OCC>
+__global__ __launch_bounds__(64 * kWaves, OCC) void k_paged_wide(const PagedArgs a) {
   using L = Tile<T, DP>;
-  constexpr int BYTES = kKT * L::PITCH, NT = 64 * kWaves;
+  constexpr int BYTES = KT * L::PITCH, NT = 64 * kWaves;
+  using Cp = Copy<T, DP, KT, NT>;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BYTES];
+  __shared__ uint32_t mask[2];
+  __shared__ int found;
   Seq s;
   int r0;
   if (!find_rows(a, blockIdx.x, 32 * kWaves, s, r0)) return;
@@ -182,7 +189,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_paged_wide(const PagedArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const RowOf row(a, s, hk, r0 + 32 * wave + (lane & 31));
   const int rl = min(r0 + 32 * kWaves, s.rows) - 1, wr = r0 + 32 * wave, wl = min(wr + 32, s.rows) - 1;
-  const KeyTiles kt(a, s.len, s.p0 + r0 / a.G, s.p0 + rl / a.G, kKT);
+  const int pa = s.p0 + r0 / a.G, pb = s.p0 + rl / a.G;
+  const KeyTiles kt(a, s.len, pa, pb, KT);
   const int wa = s.p0 + wr / a.G, wb = wl >= wr ? s.p0 + wl / a.G : wa - 1;
   const int x0 = (int)((int64_t)kt.count() * split / a.splits), x1 = (int)((int64_t)kt.count() * (split + 1) / a.splits);
   const int32_t* table = a.table + (int64_t)s.b * a.max_pages;
@@ -194,49 +202,59 @@ __global__ __launch_bounds__(64 * kWaves) void k_paged_wide(const PagedArgs a) {
   st.init();
   const float c = a.scale * kLog2e;
   const int jhi = row.ok ? row.p : -1;
-  PagedStage<T, DP, NT> sg;
-  // slots run two tiles ahead of the products, the loads one
-  auto slot = [&](int x) __attribute__((always_inline)) { return x < x1 && lane < kKT ? slot_of(a, table, kt.tile(x) * kKT + lane, s.len) : -1; };
-  const int pa = s.p0 + r0 / a.G, pb = s.p0 + rl / a.G;
-  bool scrubbed = false;
-  // the tile that was loaded into LDS for all waves
-  auto store = [&](int x, uint8_t* to, uint32_t whole) __attribute__((always_inline)) {
-    const bool edge = whole != 0xffffffffu || sees(a, s.len, pa, pb, kt.tile(x) * kKT, kKT) != 2;
-    const bool bad = edge && sg.any_nonfinite();
-    if (__builtin_expect(bad, 0)) sg.scrub();
-    sg.store(to, to + BYTES);
-    if (edge) {
-      scrubbed = __syncthreads_or(bad);
-    } else {
-      scrubbed = false;
-      __syncthreads();
+  // slots (a lane a key) run two tiles ahead of the products, the copies one
+  auto slot = [&](int x) __attribute__((always_inline)) {
+    return x < x1 && lane < KT ? slot_of(a, table, kt.tile(x) * KT + lane, s.len) : (int64_t)-1;
+  };
+  auto copy = [&](int x, int64_t at) __attribute__((always_inline)) {
+    uint8_t* to = smem + ((x - x0) & 1) * 2 * BYTES;
+    typedef __attribute__((address_space(1))) const void gvoid;
+    typedef __attribute__((address_space(3))) void lvoid;
+#pragma unroll
+    for (int i = 0; i < Cp::N; ++i) {
+      const int r = threadIdx.x / L::CPR + i * Cp::STEP, e = ((threadIdx.x % L::CPR) ^ L::swz(r)) * L::E;
+      const int64_t o = shfl64(at, r);
+      const bool ok = o >= 0 && e < a.d;
+      uint8_t* dst = to + (i * NT + wave * 64) * 16;
+      __builtin_amdgcn_global_load_lds((gvoid*)(ok ? (const void*)(kb + o + e) : (const void*)kZeros), (lvoid*)dst, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gvoid*)(ok ? (const void*)(vb + o + e) : (const void*)kZeros),
+                                       (lvoid*)(dst + BYTES), 16, 0, 0);
     }
   };
-  int64_t at = slot(x0), here = at;
-  uint32_t there = (uint32_t)__ballot(at >= 0);
-  if (x0 < x1) {
-    sg.load(kb, vb, at, a.d);
-    at = slot(x0 + 1);
-    store(x0, smem, there);
-  }
+  int64_t here = slot(x0), next = slot(x0 + 1);
+  if (threadIdx.x == 0) found = -1;
+  if (x0 < x1) copy(x0, here);
+  __syncthreads();
   for (int x = x0; x < x1; ++x) {
-    const uint8_t* ks = smem + ((x - x0) & 1) * 2 * BYTES;
-    const uint32_t there_next = (uint32_t)__ballot(at >= 0);
-    const int64_t next = at;
-    if (x + 1 < x1) {
-      sg.load(kb, vb, at, a.d);
-      at = slot(x + 2);
-    }
-    const int k0 = kt.tile(x) * kKT;
-    const int what = sees(a, s.len, wa, wb, k0, kKT);
+    uint8_t* ks = smem + ((x - x0) & 1) * 2 * BYTES;
+    const int k0 = kt.tile(x) * KT;
+    const uint64_t there = __ballot(here >= 0);
+    const bool whole = there == (KT == 64 ? ~0ull : 0xffffffffull);
+    uint64_t bad = 0;   // keys whose values were scrubbed
+    if ((!whole || sees(a, s.len, pa, pb, k0, KT) != 2) &&
+        __builtin_expect(Cp::holds_nonfinite(ks + BYTES, x, &found), 0))
+      bad = Cp::scrub(ks + BYTES, mask);
+    if (x + 1 < x1) copy(x + 1, next);
+    const int64_t after = slot(x + 2);
     const Sight sight(a, row.p, jhi, k0);
-    const uint32_t mine = there >> (4 * (lane >> 5));
+    const uint64_t mine = there >> (4 * (lane >> 5));
     auto see = [&](int r) __attribute__((always_inline)) { return sight.see(r) && (mine >> r & 1); };
-    if (what) softmax_step<T, DP, 0>(st, q, ks, ks + BYTES, c, what == 1 || there != 0xffffffffu, see);
-    if (__builtin_expect(scrubbed, 0)) restore_nonfinite<T, DP>(st, vb, here, a.d, see);
-    if (x + 1 < x1) store(x + 1, smem + ((x - x0 + 1) & 1) * 2 * BYTES, there_next);
-    there = there_next;
+    auto step = [&](auto rb) __attribute__((always_inline)) {
+      constexpr int RB = decltype(rb)::value;
+      const int what = sees(a, s.len, wa, wb, k0 + RB, 32);
+      if (what) softmax_step<T, DP, RB>(st, q, ks, ks + BYTES, c, what == 1 || !whole, see);
+    };
+    step(std::integral_constant<int, 0>{});
+    if constexpr (KT == 64) step(std::integral_constant<int, 32>{});
+#pragma unroll 1
+    for (; __builtin_expect(bad != 0, 0); bad &= bad - 1) {
+      const int j = __builtin_ctzll(bad);
+      const int64_t o = shfl64(here, j);
+      if (o >= 0) add_nonfinite<T, DP / 32>(st.o, vb + o, see(j - 4 * (lane >> 5)), 0, a.d);
+    }
     here = next;
+    next = after;
+    __syncthreads();
   }
   finish<T, DP>(a, row, split, st);
 }
@@ -399,9 +417,10 @@ template <typename T, int DP>
 hipError_t run(const PagedArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)row_tiles(a, a.wide), (unsigned)a.Hkv, (unsigned)a.splits);
   if constexpr (sizeof(T) == 4 && DP == 256) {
-    k_paged_wide<T, DP><<<grid, 64 * kWaves, 0, s>>>(a);   // a wave's own tile would not fit
+    k_paged_wide<T, DP, 32, 1><<<grid, 64 * kWaves, 0, s>>>(a);   // a wave's own tile would not fit
   } else {
-    if (a.wide) k_paged_wide<T, DP><<<grid, 64 * kWaves, 0, s>>>(a);
+    constexpr bool H = sizeof(T) == 2 && DP <= 128;
+    if (a.wide) k_paged_wide<T, DP, H ? 64 : 32, H ? 2 : 1><<<grid, 64 * kWaves, 0, s>>>(a);
     else k_paged_narrow<T, DP><<<grid, 64 * kWaves, 0, s>>>(a);
   }
   if (a.splits > 1) {
@@ -420,8 +439,22 @@ void paged_plan(PagedArgs& a, bool bf16) {
   // are better shared by four waves
   a.wide = (int64_t)a.T * a.G > 32 * (int64_t)a.B || (!bf16 && a.d > 128);
   const int64_t groups = (int64_t)row_tiles(a, a.wide) * a.Hkv;
-  const int64_t most = std::max<int64_t>(1, ((int64_t)a.max_pages * a.page + kKT - 1) / kKT / (a.wide ? 4 : 2 * kWaves));
-  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(1024 + groups - 1) / groups, most, 32}));
+  const int64_t most = std::max<int64_t>(1, ((int64_t)a.max_pages * a.page + kKT - 1) / kKT / (2 * kWaves));
+  if (!a.wide) {
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(1024 + groups - 1) / groups, most, 32}));
+    return;
+  }
+  // The split that fills the rounds of 512 workgroups (two a CU) best; its sums
+  // and their joining cost about a tenth (6 sequences of 4096 to 8192 tokens,
+  // 350 to 700 new, 416 workgroups: unsplit 352 us, two to six parts 384 to 388).
+  double best = 0;
+  for (int s = 1; s <= std::min<int64_t>(most, 16); ++s) {
+    const double t = (double)((groups * s + 511) / 512) / s * (s > 1 ? 1.08 + 0.02 * s : 1.0);
+    if (s == 1 || t < best) {
+      best = t;
+      a.splits = s;
+    }
+  }
 }
 
 hipError_t launch_paged(const PagedArgs& a, bool bf16, hipStream_t s) {

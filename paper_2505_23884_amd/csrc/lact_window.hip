@@ -324,12 +324,15 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
     uint8_t* to = smem + (x & 1) * STAGE;
     Cp::rows(to, row_of<T>(a.q, b, h, i0), ldq, job.qb - i0, a.d);
     Cp::rows(to + BYTES, row_of<T>(g.dout, b, h, i0), ldo, job.qb - i0, a.d);
-    if (wave < 2) {   // nlse and ndelta of the queries; past the last one zeros (masked)
-      const float* from = (wave ? g.ndelta : g.nlse) + ((int64_t)b * a.H + h) * a.n_q + i0;
-      const __amdgpu_buffer_rsrc_t rsrc =
-          __builtin_amdgcn_make_buffer_rsrc((void*)from, (short)0, min(QT, job.qb - i0) * 4, kBufFlags);
-      if (lane < QT)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + 2 * BYTES + wave * QT * 4), 4, lane * 4, 0, 0, 0);
+    if (wave == 0) {   // nlse and ndelta of the queries; past the last one zeros (masked)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const float* from = (y ? g.ndelta : g.nlse) + ((int64_t)b * a.H + h) * a.n_q + i0;
+        const __amdgpu_buffer_rsrc_t rsrc =
+            __builtin_amdgcn_make_buffer_rsrc((void*)from, (short)0, min(QT, job.qb - i0) * 4, kBufFlags);
+        if (lane < QT)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(to + 2 * BYTES + y * QT * 4), 4, lane * 4, 0, 0, 0);
+      }
     }
   };
   const int kb0 = job.tile * KB, kb1 = kb0 + KB - 1;
@@ -630,11 +633,22 @@ __global__ __launch_bounds__(256) void k_window_dkv_sum(const WindowBwdArgs g) {
 
 int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
+// Below so many workgroups of four waves, workgroups of one: its LDS holds two
+// of them a CU, so up to 512 run at once, each on less work ([1, 2, 256, 64]
+// fp32, window 64, training: 55 us, with four waves 94; [1, 8, 512, 64], window
+// 256: 44 and 47; from 512 on they only take turns: [1, 16 / 4, 2048, 128] fp32,
+// window 1024: 1605 and 808).
+constexpr int kFewBlocks = 128;
+
+// Workgroups of one wave (32 queries) where those of four would leave CUs idle.
+bool single_waves(const WindowArgs& a) { return (int64_t)a.B * a.H * cdiv(a.n_q, 128) < kFewBlocks; }
+
 template <typename T, int DP>
 hipError_t fwd(const WindowArgs& a, hipStream_t s) {
   constexpr int OCC = sizeof(T) == 4 || DP > 128 ? 1 : DP > 64 ? 2 : 4;
   const int64_t bh = (int64_t)a.B * a.H;
-  k_window_fwd<T, DP, 4, OCC><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(a);
+  if (single_waves(a)) k_window_fwd<T, DP, 1, 1><<<(unsigned)(bh * cdiv(a.n_q, 32)), 64, 0, s>>>(a);
+  else k_window_fwd<T, DP, 4, OCC><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -648,11 +662,14 @@ hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
     int G = 1;
     while (G < 64 && G * (16 / (int)sizeof(T)) < a.d) G *= 2;
     k_window_delta<T><<<(unsigned)((bh * a.n_q + 256 / G - 1) / (256 / G)), 256, 0, s>>>(g, G);
-    k_window_dq<T, DP, 4, (H16 && DP <= 128 ? 2 : 1)><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(g);
+    if (single_waves(a)) k_window_dq<T, DP, 1, 1><<<(unsigned)(bh * cdiv(a.n_q, 32)), 64, 0, s>>>(g);
+    else k_window_dq<T, DP, 4, (H16 && DP <= 128 ? 2 : 1)><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(g);
   }
   if (a.n_kv > 0) {
     if constexpr (H16 && DP <= 128)
       k_window_dkv16<DP, DP / 64><<<(unsigned)(bk * g.plan.jobs()), 256 * (DP / 64), 0, s>>>(g);
+    else if (g.plan.kb == 32)
+      k_window_dkv<T, DP, DO, QT, 1><<<(unsigned)(bk * g.plan.jobs() * (DP / DO)), 64, 0, s>>>(g);
     else
       k_window_dkv<T, DP, DO, QT, 4><<<(unsigned)(bk * g.plan.jobs() * (DP / DO)), 256, 0, s>>>(g);
     const DkvPlan& pl = g.plan;
@@ -674,9 +691,10 @@ hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
 // size beside 256 others take another round, 720 us; without sinks 400), and
 // all of them, by heads first, where the tiles alone would leave CUs idle.
 DkvPlan window_dkv_plan(const WindowArgs& a, bool bf16) {
-  (void)bf16;
   DkvPlan p{};
-  p.kb = 128;
+  // (16-bit of up to 128 columns has kernels of 128 keys only)
+  const bool few = (int64_t)a.B * a.H * cdiv(a.n_kv, 128) < kFewBlocks && (!bf16 || a.d > 128);
+  p.kb = few ? 32 : 128;
   p.ntile = cdiv(a.n_kv, p.kb);
   const int n_q = std::max(a.n_q, 1);
   const int reach = (int)std::min<int64_t>(n_q, (int64_t)a.win + a.look + p.kb);   // queries that see a tile
@@ -691,7 +709,7 @@ DkvPlan window_dkv_plan(const WindowArgs& a, bool bf16) {
     p.st = cdiv(std::min(a.sinks, a.n_kv), p.kb);
     parts(std::max(256, cdiv(reach, 256) * 64), &p.np_s, &p.ch_s);
   }
-  while (tiles * p.gs < 256 && p.gs < a.G) {
+  while (tiles * p.gs < (few ? 512 : 256) && p.gs < a.G) {
     int f = 2;
     while (a.G / p.gs % f) ++f;   // the least factor of what is left of the group
     p.gs *= f;
