@@ -189,10 +189,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
   load_row<T, DP>(q, row_of<T>(a.q, b, h, ic), live, a.d);
   load_row<T, DP>(go, row_of<T>(g.dout, b, h, ic), live, a.d);
   const float nlse2 = (live ? g.nlse[(int64_t)bh * a.n_q + ic] : neg_inf()) * a.scale * kLog2e;
-  const float ndelta = live ? g.ndelta[(int64_t)bh * a.n_q + ic] : 0.0f;
-  f32x16 dq[DP / 32];
-#pragma unroll
-  for (int x = 0; x < DP / 32; ++x) dq[x] = f32x16{};
+  float ndelta = live ? g.ndelta[(int64_t)bh * a.n_q + ic] : 0.0f;
   const float c = a.scale * kLog2e;
   const int n = kt.count();
   const int ldk = (int)(a.k.st * sizeof(T)), ldv = (int)(a.v.st * sizeof(T));
@@ -204,9 +201,11 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
     Cp::rows(to + BYTES, row_of<T>(a.v, b, hk, k0), ldv, len - k0, a.d);
   };
   const int pa = a.q_start + r0, pb = a.q_start + min(r0 + QB - 1, last);
-  auto step = [&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad) __attribute__((always_inline)) {
+  // The cotangents of the scores of rows RB .. of the tile.
+  auto scores = [&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad, f32x16& s)
+      __attribute__((always_inline)) {
     constexpr int RB = decltype(rb)::value;
-    f32x16 s, dp;
+    f32x16 dp;
     mma_dot<T, DP, RB>(s, ks, q);
     mma_dot<T, DP, RB>(dp, ks + BYTES, go);
 #pragma unroll
@@ -220,26 +219,50 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = sight.see(RB + 8 * (e >> 2) + (e & 3)) ? s[e] : 0.0f;
     }
-    mma_rows<T, DP, DP / 32, RB>(dq, RowsB<T>(s), ks, 0);
   };
-  if (threadIdx.x == 0) found = -1;
-  if (n > 0) copy(0);
-  __syncthreads();
-  for (int x = 0; x < n; ++x) {
-    uint8_t* ks = smem + (x & 1) * 2 * BYTES;
-    const int k0 = kt.tile(x) * KT;
-    uint64_t bad = 0;
-    if (sees(a, len, pa, pb, k0, KT) != 2 && __builtin_expect(Cp::holds_nonfinite(ks, x, &found), 0))
-      bad = Cp::scrub(ks, mask);
-    if (x + 1 < n) copy(x + 1);
-    auto part = [&](auto rb) __attribute__((always_inline)) {
-      const int what = sees(a, len, wa, wb, k0 + rb, 32);
-      if (what) step(ks, k0, rb, what == 1 || bad != 0, bad);
-    };
-    part(std::integral_constant<int, 0>{});
-    if constexpr (KT == 64) part(std::integral_constant<int, 32>{});
+  // use(tile, k0, RB, masked, bad) for each 32 keys that the wave sees something of
+  auto over_tiles = [&](auto use) __attribute__((always_inline)) {
+    if (threadIdx.x == 0) found = -1;
+    if (n > 0) copy(0);
     __syncthreads();
+    for (int x = 0; x < n; ++x) {
+      uint8_t* ks = smem + (x & 1) * 2 * BYTES;
+      const int k0 = kt.tile(x) * KT;
+      uint64_t bad = 0;
+      if (sees(a, len, pa, pb, k0, KT) != 2 && __builtin_expect(Cp::holds_nonfinite(ks, x, &found), 0))
+        bad = Cp::scrub(ks, mask);
+      if (x + 1 < n) copy(x + 1);
+      auto part = [&](auto rb) __attribute__((always_inline)) {
+        const int what = sees(a, len, wa, wb, k0 + rb, 32);
+        if (what) use(ks, k0, rb, what == 1 || bad != 0, bad);
+      };
+      part(std::integral_constant<int, 0>{});
+      if constexpr (KT == 64) part(std::integral_constant<int, 32>{});
+      __syncthreads();
+    }
+  };
+  if (sizeof(T) == 2 && n <= 256 / KT) {
+    // delta from a rounded o is off by 2^-8 of its terms, which shows in rows
+    // of few keys (their o is large): the cotangents of a row's scores sum to
+    // zero, so a pass over its keys finds what is missing.
+    float rest = 0.0f;
+    over_tiles([&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad) __attribute__((always_inline)) {
+      f32x16 s;
+      scores(ks, k0, rb, masked, bad, s);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) rest += s[e];
+    });
+    ndelta -= half_sum(rest);
+    if (live && lane < 32) g.ndelta[(int64_t)bh * a.n_q + i] = ndelta;
   }
+  f32x16 dq[DP / 32];
+#pragma unroll
+  for (int x = 0; x < DP / 32; ++x) dq[x] = f32x16{};
+  over_tiles([&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad) __attribute__((always_inline)) {
+    f32x16 s;
+    scores(ks, k0, rb, masked, bad, s);
+    mma_rows<T, DP, DP / 32, decltype(rb)::value>(dq, RowsB<T>(s), ks, 0);
+  });
   store_row<T, DP / 32>(row_of<T>(g.dq, b, h, ic), dq, a.scale, 0, a.d, i < a.n_q, !live);
 }
 
