@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2505_23884_amd as P
-from attention_reference import HALF, attention, check, norm_rope, visible
+from attention_reference import HALF, attention, check, head, norm_rope, visible
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -262,3 +262,214 @@ def test_paged_append_writes_the_slots_and_nothing_else(lens, new, Hkv, d, page,
     P.paged_append(k, v, kc, vc, table, ln, cu_new)
     torch.cuda.synchronize()
     assert torch.equal(kc, kw) and torch.equal(vc, vw)
+
+
+def test_pages_outside_the_cache_hold_nothing():
+    lens, new, H, Hkv, d, page = [100, 70], [3, 1], 4, 2, 64, 16
+    q, kc, vc, table, ln, cu_new, K, V, cu = paged_setup(lens, new, H, Hkv, d, page, BF, seed=3)
+    table[0, 2], table[1, 0], table[1, 4] = -1, kc.shape[0], 2 ** 31 - 1
+    gone = {0: [(32, 48)], 1: [(0, 16), (64, 80)]}
+    o = P.paged_attention(q, kc, vc, table, ln, cu_new)
+    torch.cuda.synchronize()
+    for b in range(2):
+        keep = torch.ones(lens[b], dtype=torch.bool)
+        for x, y in gone[b]:
+            keep[x:y] = False
+        for i in range(new[b]):           # each token over the keys that are there, all of them before it
+            p = lens[b] - new[b] + i
+            rows = keep.clone()
+            rows[p + 1:] = False
+            if not rows.any():
+                continue
+            qb = q[cu[b] + i][None, :, None].cpu()
+            want, tol = attention(qb, K[b][:, :, rows], V[b][:, :, rows], lookahead=None)
+            check(f"{b} {i}", o[cu[b] + i][None, :, None], want["o"], tol["o"])
+    k = rnd(9, 4, Hkv, d).to(DEV)
+    before = kc.clone()
+    P.paged_append(k, k, kc, vc, table, ln, cu_new)
+    torch.cuda.synchronize()
+    changed = (kc.view(torch.int16) != before.view(torch.int16)).flatten(2).any(-1)
+    want = torch.zeros_like(changed)
+    for i, p in enumerate((97, 98, 99)):
+        want[table[0, p // page].item(), p % page] = True
+    assert torch.equal(changed, want)      # the second sequence's slot lies on a page that is none
+
+
+def test_lengths_and_offsets_out_of_range_are_clamped():
+    q, kc, vc, table, ln, cu_new, K, V, cu = paged_setup([40, 50], [2, 3], 2, 1, 64, 16, BF, seed=4)
+    width = table.shape[1] * 16
+    out = torch.full_like(q, 7.0)
+    P.paged_attention(torch.nan_to_num(q), torch.nan_to_num(kc), torch.nan_to_num(vc), table,
+                      torch.tensor([width + 1000, -5], dtype=torch.int32, device=DEV), cu_new, out=out)
+    torch.cuda.synchronize()
+    assert bool((out[2:5] == 0).all())                       # a sequence of no tokens: nothing to see
+    assert bool(torch.isfinite(out[:2].float()).all()) and bool((out[5:] == 7.0).all())
+    out.fill_(7.0)
+    P.paged_attention(q, kc, vc, table, ln, torch.tensor([0, 100000, 100000], dtype=torch.int32, device=DEV), out=out)
+    torch.cuda.synchronize()
+
+
+def test_cache_of_more_than_four_gigabytes():
+    pages, page, Hkv, d = 40000, 64, 8, 128
+    if torch.cuda.mem_get_info()[0] < 14 << 30:
+        pytest.skip("needs 14 GB of GPU memory")
+    kc, vc = (torch.zeros(pages, page, Hkv, d, dtype=BF, device=DEV) for _ in range(2))
+    last = [pages - 1, pages - 2, 39000, 5]
+    table = torch.tensor([last], dtype=torch.int32, device=DEV)
+    K, V = rnd(1, 1, Hkv, 200, d), rnd(2, 1, Hkv, 200, d)
+    ln, cu_new = torch.tensor([200], dtype=torch.int32, device=DEV), torch.tensor([0, 200], dtype=torch.int32, device=DEV)
+    P.paged_append(K[0].transpose(0, 1).contiguous().to(DEV), V[0].transpose(0, 1).contiguous().to(DEV), kc, vc, table, ln, cu_new)
+    for H, new in ((8, 1), (16, 1), (8, 150)):
+        q = rnd(3, new, H, d).to(DEV)
+        cu = torch.tensor([0, new], dtype=torch.int32, device=DEV)
+        o = P.paged_attention(q, kc, vc, table, ln, cu, window=90, sinks=2)
+        torch.cuda.synchronize()
+        want, tol = attention(q.transpose(0, 1)[None].cpu(), K, V, q_start=200 - new, window=90, sinks=2)
+        check(f"H {H} new {new}", o.transpose(0, 1)[None], want["o"], tol["o"])
+
+
+def layer(q, k, v, wq, wk, inv, do, **opt):
+    """Forward and reverse of one layer's attention half."""
+    qn, kn = P.qk_norm_rope(q, k, wq, wk, inv)
+    vt = v.transpose(1, 2)
+    o, lse = P.window_attention(qn, kn, vt, with_lse=True, **opt)
+    dqn, dkn, dv = P.window_attention_backward(qn, kn, vt, o, lse, do, **opt)
+    dq, dk, dwq, dwk = P.qk_norm_rope_backward(q, k, dqn, dkn, wq, wk, inv)
+    return o, dq, dk, dv, dwq, dwk
+
+
+def layer_inputs(seed=0, B=2, n=150, H=4, Hkv=2, d=64, dtype=BF):
+    fused = rnd(seed, B, n, H + 2 * Hkv, d, dtype=dtype).to(DEV)
+    wq, wk = (torch.rand(d, generator=torch.Generator().manual_seed(seed + x)).to(DEV) + 0.5 for x in (1, 2))
+    inv = (10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).to(DEV)
+    return fused[:, :, :H], fused[:, :, H:H + Hkv], fused[:, :, H + Hkv:], wq, wk, inv, rnd(seed + 3, B, H, n, d, dtype=dtype).to(DEV)
+
+
+OPT = dict(window=40, sinks=2)
+
+
+def test_two_runs_are_bitwise_equal():
+    x = layer_inputs()
+    for a, b in zip(layer(*x, **OPT), layer(*x, **OPT)):
+        assert torch.equal(a, b)
+
+
+def test_chain_in_fp32_against_differences():
+    x = q, k, v, wq, wk, inv, do = tuple(t.clone() for t in layer_inputs(5, B=1, n=40, H=2, Hkv=1, d=16, dtype=F32))
+    got = layer(*x, **OPT)[1:]
+    pos = torch.arange(40)[None]
+    see = visible(40, 40, 40, 0, OPT["window"], OPT["sinks"], 0)
+    g64 = do.double().cpu()
+
+    def normed(a, w):
+        return norm_rope(a, w, inv, pos, 1e-6, False)
+
+    def loss(a, b, c, u, w):      # the layer's definition in 64 bits
+        qn, kn = normed(a, u), normed(b, w)
+        return float(sum((head(qn[0, h], kn[0, 0], c[0, :, 0], see, 0.25)["o"] * g64[0, h]).sum() for h in range(2)))
+
+    base = [t.double().cpu() for t in (q, k, v, wq, wk)]
+    # The attention's bounds for its cotangents, twice for the rounding of its own
+    # inputs, through the norm: its reverse is a linear map of norm at most
+    # 2 max(r w), and an element of a weight's gradient is a product with a column of x r.
+    _, tol = attention(normed(q, wq).float(), normed(k, wk).float(), v.transpose(1, 2), do=do, **OPT)
+    unit = [t / (t.square().mean(-1, keepdim=True) + 1e-6).sqrt() for t in base[:2]]
+    gain = [float(((t.square().mean(-1, keepdim=True) + 1e-6).rsqrt() * w).max()) for t, w in zip(base[:2], base[3:])]
+    n = [2 * float(tol[y].norm()) for y in ("dq", "dk", "dv")]
+    bound = [2 * gain[0] * n[0], 2 * gain[1] * n[1], n[2], *(n[i] * float(unit[i].flatten(0, 2).norm(dim=0).max()) for i in (0, 1))]
+    for i, g in enumerate((got[0], got[1], got[2].transpose(1, 2), got[3], got[4])):
+        step = rnd(20 + i, *base[i].shape, dtype=torch.float64)
+        h = 1e-5
+        at = [loss(*(t + (sign * h * step if j == i else 0) for j, t in enumerate(base))) for sign in (1, -1)]
+        want = (at[0] - at[1]) / (2 * h)
+        have = float((g.double().cpu() * step).sum())
+        assert abs(have - want) <= bound[i] * float(step.norm()) + 1e-7 * abs(want), i
+        assert bound[i] < 0.02 * float(g.norm()), i      # (a bound that would notice a missing term)
+
+
+def test_decoding_token_by_token_matches_the_prefill():
+    B, n, H, Hkv, d, page = 2, 90, 4, 2, 64, 16
+    q, k, v, wq, wk, inv, _ = layer_inputs(7, B, n, H, Hkv, d)
+    qn, kn = P.qk_norm_rope(q, k, wq, wk, inv)
+    want, tol = attention(qn, kn, v.transpose(1, 2).contiguous(), **OPT)
+    width = -(-n // page)
+    kc, vc = (torch.full((B * width, page, Hkv, d), float("nan"), dtype=BF, device=DEV) for _ in range(2))
+    table = torch.randperm(B * width, generator=torch.Generator().manual_seed(1)).view(B, width).to(DEV, torch.int32)
+    done = 0
+    got = torch.empty(B, n, H, d, dtype=BF, device=DEV)
+    for m in (50, 1, 1, 20, 1, 17):       # a prompt, tokens, a chunk, ...
+        at = slice(done, done + m)
+        done += m
+        qt, kt = P.qk_norm_rope(q[:, at], k[:, at], wq, wk, inv, pos0=done - m)
+        rows = lambda t, h: t.transpose(1, 2).reshape(B * m, h, d)
+        ln = torch.full((B,), done, dtype=torch.int32, device=DEV)
+        cu = torch.arange(0, (B + 1) * m, m, dtype=torch.int32, device=DEV)
+        P.paged_append(rows(kt, Hkv), v[:, at].reshape(B * m, Hkv, d), kc, vc, table, ln, cu)
+        got[:, at] = P.paged_attention(rows(qt, H), kc, vc, table, ln, cu, **OPT).view(B, m, H, d)
+    torch.cuda.synchronize()
+    assert done == n
+    check("decoded", got.transpose(1, 2), want["o"], tol["o"])
+
+
+def test_captured_and_replayed_on_another_stream():
+    x = layer_inputs(11)
+    q, kc, vc, table, ln, cu_new, _, _, cu = paged_setup([300, 90], [1, 4], 4, 2, 64, 16, BF, seed=8)
+    kc, vc, q = (torch.nan_to_num(t) for t in (kc, vc, q))
+    new = rnd(12, q.shape[0], 2, 64).to(DEV)
+
+    def step():
+        P.paged_append(new, new, kc, vc, table, ln, cu_new)
+        return (*layer(*x, **OPT), P.paged_attention(q, kc, vc, table, ln, cu_new, window=200, out=torch.zeros_like(q)))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(3):
+        with torch.no_grad():
+            x[0].copy_(rnd(30 + i, *x[0].shape))
+            q.copy_(rnd(40 + i, *q.shape))
+            new.copy_(rnd(50 + i, *new.shape))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in out]
+        for a, b in zip(replayed, step()):
+            assert torch.equal(a, b), i
+
+
+def test_outputs_given_and_bindings_refuse():
+    q, k, v = rnd(1, 2, 4, 70, 64).to(DEV), rnd(2, 2, 2, 70, 64).to(DEV), rnd(3, 2, 2, 70, 64).to(DEV)
+    o, lse = P.window_attention(q, k, v, with_lse=True, **OPT)
+    out = torch.full((2, 70, 4, 64), 9.0, dtype=BF, device=DEV)      # heads behind tokens
+    P.window_attention(q, k, v, out=out.transpose(1, 2), **OPT)
+    assert torch.equal(out.transpose(1, 2), o)
+    do = rnd(4, 2, 4, 70, 64).to(DEV)
+    want = P.window_attention_backward(q, k, v, o, lse, do, **OPT)
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    fused = torch.full((2, 70, 8, 64), 9.0, dtype=BF, device=DEV)
+    parts = [fused[:, :, a:b].transpose(1, 2) for a, b in ((0, 4), (4, 6), (6, 8))]
+    P.window_attention_backward(q, k, v, o, lse, do, out=parts, workspace=ws, **OPT)
+    for a, b in zip(parts, want):
+        assert torch.equal(a, b)
+    # keys of one head given to all of a batch's heads by a stride of zero: as if repeated
+    kx, vx = k[:, :1].expand(2, 4, 70, 64), v[:, :1].expand(2, 4, 70, 64)
+    assert torch.equal(P.window_attention(q, kx, vx, **OPT), P.window_attention(q, kx.contiguous(), vx.contiguous(), **OPT))
+    bad = [lambda: P.window_attention(q, k, v.float()), lambda: P.window_attention(q, k, v[:, :, :60]),
+           lambda: P.window_attention(q, k[:, :, :, :32], v), lambda: P.window_attention(q[0], k, v),
+           lambda: P.window_attention(q.half(), k.half(), v.half()),
+           lambda: P.window_attention(q, k, v, lengths=torch.tensor([70, 70], device=DEV)),
+           lambda: P.window_attention(q.transpose(2, 3), k, v), lambda: P.window_attention(q, k.cpu(), v),
+           lambda: P.window_attention(q, k, v, scale=-1.0), lambda: P.window_attention(q[:, :3], k, v),
+           lambda: P.window_attention(q, k, v, out=torch.empty_like(q)[:, :1].expand_as(q)),
+           lambda: P.window_attention_backward(q, k, v, o, None, do),
+           lambda: P.window_attention_backward(q, k, v, o, lse, do, workspace=ws[:64]),
+           lambda: P.qk_norm_rope(q, k, torch.ones(64, device=DEV, dtype=BF)),
+           lambda: P.qk_norm_rope(q.transpose(1, 2), k.transpose(1, 2), inv_freq=torch.ones(33, device=DEV, dtype=torch.float64))]
+    for i, call in enumerate(bad):
+        with pytest.raises(P.LactError):
+            call()
+            pytest.fail(f"call {i} was taken")
