@@ -111,8 +111,8 @@ int check_attn(const lact_attn_desc* s) {
   if (s->n_q > kAttnTokens || s->n_kv > kAttnTokens || s->q_start > kAttnTokens || s->q_start < -kAttnTokens ||
       s->q_start + s->n_q > kAttnTokens)
     return LACT_EUNSUPPORTED;
-  // the largest grids: a row of lse and delta a group of lanes; tiles of keys in parts
-  if ((int64_t)s->B * s->H * (s->n_q / 4 + 1) > kMaxGrid || (int64_t)s->B * s->H * (s->n_kv / 128 + 1) * 128 > kMaxGrid)
+  // the largest grids: tiles of 32 queries; tiles of keys in parts
+  if ((int64_t)s->B * s->H * (s->n_q / 32 + 1) > kMaxGrid || (int64_t)s->B * s->H * (s->n_kv / 128 + 1) * 128 > kMaxGrid)
     return LACT_EUNSUPPORTED;
   return LACT_OK;
 }

@@ -127,41 +127,26 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_fwd(const WindowArgs a)
 }
 
 // ------------------------------------------------------------------ reverse
-// -lse / scale and -delta, once per query: the accumulators of the scores and
-// of do . v start from them. G lanes a row.
-template <typename T>
-__global__ __launch_bounds__(256) void k_window_delta(const WindowBwdArgs g, int G) {
-  const WindowArgs& a = g.f;
-  constexpr int E = 16 / (int)sizeof(T);
-  const int lg = threadIdx.x & (G - 1);
-  const int64_t rows = (int64_t)a.B * a.H * a.n_q, r = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
-  if (r >= rows) return;   // whole groups
-  const int64_t bh = r / a.n_q;
-  const int b = (int)(bh / a.H), h = (int)(bh % a.H);
-  const int64_t i = r - bh * a.n_q;
+// The sum of x y over the lane's half of a row (load_row).
+template <typename T, int N>
+__device__ __forceinline__ float dot_half(const u32x4 (&x)[N], const u32x4 (&y)[N]) {
   float sum = 0.0f;
-  for (int e = lg * E; e < a.d; e += G * E) {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(row_of<T>(a.o, b, h, i) + e);
-    const u32x4 y = *reinterpret_cast<const u32x4*>(row_of<T>(g.dout, b, h, i) + e);
+#pragma unroll
+  for (int c = 0; c < N; ++c)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if constexpr (sizeof(T) == 2)
-        sum += __uint_as_float(x[k] << 16) * __uint_as_float(y[k] << 16) +
-               __uint_as_float(x[k] & 0xffff0000u) * __uint_as_float(y[k] & 0xffff0000u);
+        sum += __uint_as_float(x[c][k] << 16) * __uint_as_float(y[c][k] << 16) +
+               __uint_as_float(x[c][k] & 0xffff0000u) * __uint_as_float(y[c][k] & 0xffff0000u);
       else
-        sum += __uint_as_float(x[k]) * __uint_as_float(y[k]);
+        sum += __uint_as_float(x[c][k]) * __uint_as_float(y[c][k]);
     }
-  }
-  for (int o = G >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-  if (lg == 0) {
-    const float l = a.lse[r];
-    g.nlse[r] = l == neg_inf() ? neg_inf() : -l / a.scale;   // an empty row's too: weights exp2(-inf) = 0
-    g.ndelta[r] = -sum;
-  }
+  return sum;
 }
 
 // dq: queries stay in registers with their cotangents, keys and values pass
-// through LDS as in the forward.
+// through LDS as in the forward. Leaves -lse / scale and -delta of its queries
+// for dk and dv, whose accumulators start from them.
 template <typename T, int DP, int NW, int OCC>
 __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs g) {
   const WindowArgs& a = g.f;
@@ -188,8 +173,15 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
   u32x4 q[L::KS], go[L::KS];
   load_row<T, DP>(q, row_of<T>(a.q, b, h, ic), live, a.d);
   load_row<T, DP>(go, row_of<T>(g.dout, b, h, ic), live, a.d);
-  const float nlse2 = (live ? g.nlse[(int64_t)bh * a.n_q + ic] : neg_inf()) * a.scale * kLog2e;
-  float ndelta = live ? g.ndelta[(int64_t)bh * a.n_q + ic] : 0.0f;
+  const int64_t at = (int64_t)bh * a.n_q + ic;
+  float nlse = live ? a.lse[at] : neg_inf(), ndelta;
+  nlse = nlse == neg_inf() ? neg_inf() : -nlse / a.scale;   // an empty row's too: weights exp2(-inf) = 0
+  {
+    u32x4 o[L::KS];
+    load_row<T, DP>(o, row_of<T>(a.o, b, h, ic), live, a.d);
+    ndelta = -half_sum(dot_half<T>(o, go));
+  }
+  const float nlse2 = nlse * a.scale * kLog2e;
   const float c = a.scale * kLog2e;
   const int n = kt.count();
   const int ldk = (int)(a.k.st * sizeof(T)), ldv = (int)(a.v.st * sizeof(T));
@@ -252,8 +244,12 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
 #pragma unroll
       for (int e = 0; e < 16; ++e) rest += s[e];
     });
-    ndelta -= half_sum(rest);
-    if (live && lane < 32) g.ndelta[(int64_t)bh * a.n_q + i] = ndelta;
+    rest = half_sum(rest);
+    if (__builtin_isfinite(rest)) ndelta -= rest;   // (an infinite key that weighs nothing leaves the row its delta)
+  }
+  if (i < a.n_q && lane < 32) {
+    g.nlse[at] = nlse;
+    g.ndelta[at] = ndelta;
   }
   f32x16 dq[DP / 32];
 #pragma unroll
@@ -682,9 +678,6 @@ hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
   constexpr int DO = DP <= 128 ? DP : H16 ? 128 : 64, QT = 32;
   const int64_t bh = (int64_t)a.B * a.H, bk = (int64_t)a.B * a.Hkv;
   if (a.n_q > 0) {
-    int G = 1;
-    while (G < 64 && G * (16 / (int)sizeof(T)) < a.d) G *= 2;
-    k_window_delta<T><<<(unsigned)((bh * a.n_q + 256 / G - 1) / (256 / G)), 256, 0, s>>>(g, G);
     if (single_waves(a)) k_window_dq<T, DP, 1, 1><<<(unsigned)(bh * cdiv(a.n_q, 32)), 64, 0, s>>>(g);
     else k_window_dq<T, DP, 4, (H16 && DP <= 128 ? 2 : 1)><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(g);
   }

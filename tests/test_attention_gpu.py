@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2505_23884_amd as P
-from attention_reference import HALF, attention, check, head, norm_rope, visible
+from attention_reference import HALF, attention, bounds, check, head, norm_rope, visible
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -473,3 +473,24 @@ def test_outputs_given_and_bindings_refuse():
         with pytest.raises(P.LactError):
             call()
             pytest.fail(f"call {i} was taken")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+def test_an_infinite_key_that_weighs_nothing_stays_out_of_the_others(dtype):
+    # its score is -inf for every query, so the others' gradients are those without it
+    q, k, v, do = (rnd(60 + i, 1, 2, 70, 64, dtype=dtype) for i in range(4))
+    q[..., 5] = -q[..., 5].abs() - 0.1
+    k[:, :, 30] = k[:, :, 30].abs()
+    k[:, :, 30, 5] = math.inf
+    without = [j for j in range(70) if j != 30]
+    x = [t.to(DEV) for t in (q, k, v)]
+    o, lse = P.window_attention(*x, lookahead=None, with_lse=True)
+    dq, dk, dv = P.window_attention_backward(*x, o, lse, do.to(DEV), lookahead=None)
+    see = torch.ones(70, 69, dtype=torch.bool)
+    for h in range(2):
+        r = head(q[0, h], k[0, h, without], v[0, h, without], see, 0.125, do[0, h])
+        t = bounds(r, q[0, h], k[0, h, without], do, 0.125, dtype)
+        check("o", o[0, h], r["o"], t["o"])
+        check("dk", dk[0, h][without], r["dk"], t["dk"])
+        check("dv", dv[0, h][without], r["dv"], t["dv"])
+        assert bool((dv[0, h, 30] == 0).all()) and bool(torch.isnan(dq[0, h, :, 5]).all())
