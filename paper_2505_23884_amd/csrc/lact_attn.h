@@ -376,18 +376,31 @@ struct Copy {
   static_assert(N >= 1 && R * L::CPR % NT == 0 && NT % L::CPR == 0, "tile split");
   typedef __attribute__((address_space(3))) void lds_void;
 
+  // A wave of a workgroup may have tiles of its own (NT = 64): its barriers
+  // are only waits.
+  static __device__ __forceinline__ int thread() { return NT == 64 ? threadIdx.x & 63 : threadIdx.x; }
+  static __device__ __forceinline__ void sync() {
+    if constexpr (NT == 64) {
+      wait_loads<0>();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+      __builtin_amdgcn_wave_barrier();
+    } else {
+      __syncthreads();
+    }
+  }
+
   // rows of `ld` bytes from `base` (the same in all threads), `rows` of them
   // (<= 0: none); the rest, and columns past d, are zeros
   // FRESH: the offsets are worked out each time (about 10 instructions a
   // chunk) instead of staying in registers through a loop.
   template <bool FRESH = false>
   static __device__ __forceinline__ void rows(uint8_t* tile, const T* base, int ld, int64_t rows, int d) {
-    int tid = threadIdx.x;
+    int tid = thread();
     if constexpr (FRESH) asm volatile("" : "+v"(tid));
     const int n = (int)(rows < R ? rows : R);
     const int span = n > 0 ? (n - 1) * ld + d * (int)sizeof(T) : 0;
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, span, kBufFlags);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = NT == 64 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int row = tid / L::CPR + i * STEP, c = (tid % L::CPR) ^ L::swz(row);
@@ -399,24 +412,24 @@ struct Copy {
   static __device__ __forceinline__ bool any_nonfinite(const uint8_t* tile) {
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < N; ++i) bad |= nonfinite<T>(*reinterpret_cast<const u32x4*>(tile + (i * NT + threadIdx.x) * 16));
+    for (int i = 0; i < N; ++i) bad |= nonfinite<T>(*reinterpret_cast<const u32x4*>(tile + (i * NT + thread()) * 16));
     return bad;
   }
-  // whether tile x holds an infinity or NaN, by the whole workgroup with a
+  // whether tile x holds an infinity or NaN, by all NT threads with a
   // barrier; `found`: a word of LDS, -1 at first
   static __device__ __forceinline__ bool holds_nonfinite(const uint8_t* tile, int x, int* found) {
     if (any_nonfinite(tile)) *found = x;
-    __syncthreads();
+    sync();
     return *found == x;
   }
   // scrubs the tile; the rows that held one, a bit each (`mask`: two words of
-  // LDS). By the whole workgroup, with barriers before and after.
+  // LDS). By all NT threads, with barriers before and after.
   static __device__ __forceinline__ uint64_t scrub(uint8_t* tile, uint32_t* mask) {
-    if (threadIdx.x < 2) mask[threadIdx.x] = 0;
-    __syncthreads();
+    if (thread() < 2) mask[thread()] = 0;
+    sync();
 #pragma unroll 1
     for (int i = 0; i < N; ++i) {
-      const int at = i * NT + threadIdx.x, row = at / L::CPR;
+      const int at = i * NT + thread(), row = at / L::CPR;
       u32x4 x = *reinterpret_cast<const u32x4*>(tile + at * 16);
       if (!nonfinite<T>(x)) continue;
       atomicOr(&mask[row >> 5], 1u << (row & 31));
@@ -424,9 +437,9 @@ struct Copy {
       for (int k = 0; k < 4; ++k) x[k] = finite_or_zero<T>(x[k]);
       *reinterpret_cast<u32x4*>(tile + at * 16) = x;
     }
-    __syncthreads();
+    sync();
     const uint32_t lo = __builtin_amdgcn_readfirstlane(mask[0]), hi = __builtin_amdgcn_readfirstlane(mask[1]);
-    __syncthreads();
+    sync();
     return ((uint64_t)hi << 32) | lo;
   }
 };
@@ -491,6 +504,26 @@ struct Softmax {
     for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int k = 0; k < 16; ++k) o[i][k] *= f;
+  }
+  // The lane's sums to LDS, a float every 64 (16 NB + 2 of them), and those of
+  // other keys added.
+  __device__ __forceinline__ void put(float* to) const {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) to[(i * 16 + k) * 64] = o[i][k];
+    to[NB * 16 * 64] = m;
+    to[(NB * 16 + 1) * 64] = l;
+  }
+  __device__ __forceinline__ void join(const float* from) {
+    const float m2 = from[NB * 16 * 64], up = fmaxf(m, m2);
+    const float f = m == up ? 1.0f : __builtin_amdgcn_exp2f(m - up), g = m2 == up ? 1.0f : __builtin_amdgcn_exp2f(m2 - up);
+    m = up;
+    l = l * f + from[(NB * 16 + 1) * 64] * g;
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) o[i][k] = o[i][k] * f + from[(i * 16 + k) * 64] * g;
   }
 };
 

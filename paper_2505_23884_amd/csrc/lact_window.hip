@@ -53,22 +53,27 @@ template <typename T, int DP> constexpr int key_tile() { return sizeof(T) == 2 &
 
 // ------------------------------------------------------------------ forward
 // A workgroup of NW waves owns 32 NW queries of one head, a wave 32 of them;
-// keys and values pass through LDS in two stages. Scores are held transposed
+// keys and values pass through LDS in two stages. Or (NW = 1) KS waves share
+// 32 queries, each with every KS-th tile in LDS of its own, and join their sums. Scores are held transposed
 // (lact_attn.h), so the softmax needs one exchange between lanes a tile.
-template <typename T, int DP, int NW, int OCC>
-__global__ __launch_bounds__(64 * NW, OCC) void k_window_fwd(const WindowArgs a) {
+template <typename T, int DP, int NW, int KS, int OCC>
+__global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_fwd(const WindowArgs a) {
   constexpr int KT = key_tile<T, DP>(), QB = 32 * NW, NT = 64 * NW;
   using L = Tile<T, DP>;
   constexpr int BYTES = KT * L::PITCH;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BYTES];
-  __shared__ uint32_t mask[2];
-  __shared__ int found;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem_[KS * 4 * BYTES];
+  __shared__ uint32_t mask_[2 * KS];
+  __shared__ int found_[KS];
+  const int wave_ = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wave = KS > 1 ? 0 : wave_, ks_ = KS > 1 ? wave_ : 0;   // of the queries; of the keys
+  uint8_t* const smem = smem_ + ks_ * 4 * BYTES;
+  uint32_t* const mask = mask_ + 2 * ks_;
+  int* const found = found_ + ks_;
   const int ntile = (a.n_q + QB - 1) / QB;
   const int w = xcd_order(blockIdx.x, gridDim.x);
   const int bh = w / ntile, qt = ntile - 1 - w % ntile;   // the longest rows of a causal head first
   const int b = bh / a.H, h = bh % a.H, hk = h / a.G;
   const int len = length_of(a, b);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int r0 = qt * QB, i = r0 + 32 * wave + (lane & 31);
   const int last = min(a.n_q, len - a.q_start) - 1;       // the last query of the sequence
   const int p = a.q_start + i;
@@ -87,21 +92,21 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_fwd(const WindowArgs a)
   using Cp = Copy<T, DP, KT, NT>;
   auto copy = [&](int x) __attribute__((always_inline)) {
     const int k0 = kt.tile(x) * KT;
-    uint8_t* to = smem + (x & 1) * 2 * BYTES;
+    uint8_t* to = smem + (x / KS & 1) * 2 * BYTES;
     Cp::rows(to, row_of<T>(a.k, b, hk, k0), ldk, len - k0, a.d);
     Cp::rows(to + BYTES, row_of<T>(a.v, b, hk, k0), ldv, len - k0, a.d);
   };
   const int pa = a.q_start + r0, pb = a.q_start + min(r0 + QB - 1, last);
-  if (threadIdx.x == 0) found = -1;
-  if (n > 0) copy(0);
-  __syncthreads();
-  for (int x = 0; x < n; ++x) {
-    uint8_t* ks = smem + (x & 1) * 2 * BYTES;
+  if (Cp::thread() == 0) *found = -1;
+  if (ks_ < n) copy(ks_);
+  Cp::sync();
+  for (int x = ks_; x < n; x += KS) {
+    uint8_t* ks = smem + (x / KS & 1) * 2 * BYTES;
     const int k0 = kt.tile(x) * KT;
     uint64_t bad = 0;   // keys whose values were scrubbed
-    if (sees(a, len, pa, pb, k0, KT) != 2 && __builtin_expect(Cp::holds_nonfinite(ks + BYTES, x, &found), 0))
+    if (sees(a, len, pa, pb, k0, KT) != 2 && __builtin_expect(Cp::holds_nonfinite(ks + BYTES, x, found), 0))
       bad = Cp::scrub(ks + BYTES, mask);
-    if (x + 1 < n) copy(x + 1);
+    if (x + KS < n) copy(x + KS);
     const Sight sight(a, p, jhi, k0);
     auto step = [&](auto rb) __attribute__((always_inline)) {
       constexpr int RB = decltype(rb)::value;
@@ -115,7 +120,17 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_fwd(const WindowArgs a)
       const int j = __builtin_ctzll(bad);
       add_nonfinite<T, DP / 32>(st.o, row_of<T>(a.v, b, hk, k0 + j), sight.see(j - 4 * (lane >> 5)), 0, a.d);
     }
+    Cp::sync();
+  }
+  if constexpr (KS > 1) {   // the waves' sums to the first
+    float* to = reinterpret_cast<float*>(smem_) + lane;
+    constexpr int PER = DP / 2 + 2;
+    static_assert(PER * 64 * 4 <= 4 * BYTES, "sums of a wave");
     __syncthreads();
+    if (ks_) st.put(to + ks_ * PER * 64);
+    __syncthreads();
+    if (ks_) return;
+    for (int w = 1; w < KS; ++w) st.join(to + w * PER * 64);
   }
   const float l = half_sum(st.l);
   const bool none = !live || l == 0.0f;   // a row that sees nothing: 0, lse -inf
@@ -127,6 +142,27 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_fwd(const WindowArgs a)
 }
 
 // ------------------------------------------------------------------ reverse
+// The sums of W waves to the first of them (true), in order, through LDS
+// (W - 1 times 4 KiB of floats a block).
+template <int W, int NB>
+__device__ __forceinline__ bool join_waves(f32x16 (&acc)[NB], float* lds, int w) {
+  float* at = lds + (threadIdx.x & 63);
+  __syncthreads();
+  if (w)
+#pragma unroll
+    for (int x = 0; x < NB; ++x)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) at[((w - 1) * NB * 16 + x * 16 + e) * 64] = acc[x][e];
+  __syncthreads();
+  if (w) return false;
+  for (int y = 0; y < W - 1; ++y)
+#pragma unroll
+    for (int x = 0; x < NB; ++x)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[x][e] += at[(y * NB * 16 + x * 16 + e) * 64];
+  return true;
+}
+
 // The sum of x y over the lane's half of a row (load_row).
 template <typename T, int N>
 __device__ __forceinline__ float dot_half(const u32x4 (&x)[N], const u32x4 (&y)[N]) {
@@ -145,23 +181,27 @@ __device__ __forceinline__ float dot_half(const u32x4 (&x)[N], const u32x4 (&y)[
 }
 
 // dq: queries stay in registers with their cotangents, keys and values pass
-// through LDS as in the forward. Leaves -lse / scale and -delta of its queries
+// through LDS as in the forward (NW, KS as there). Leaves -lse / scale and -delta of its queries
 // for dk and dv, whose accumulators start from them.
-template <typename T, int DP, int NW, int OCC>
-__global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs g) {
+template <typename T, int DP, int NW, int KS, int OCC>
+__global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwdArgs g) {
   const WindowArgs& a = g.f;
   constexpr int KT = key_tile<T, DP>(), QB = 32 * NW, NT = 64 * NW;
   using L = Tile<T, DP>;
   constexpr int BYTES = KT * L::PITCH;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BYTES];
-  __shared__ uint32_t mask[2];
-  __shared__ int found;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem_[KS * 4 * BYTES];
+  __shared__ uint32_t mask_[2 * KS];
+  __shared__ int found_[KS];
+  const int wave_ = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = KS > 1 ? 0 : wave_, ks_ = KS > 1 ? wave_ : 0;   // of the queries; of the keys
+  uint8_t* const smem = smem_ + ks_ * 4 * BYTES;
+  uint32_t* const mask = mask_ + 2 * ks_;
+  int* const found = found_ + ks_;
   const int ntile = (a.n_q + QB - 1) / QB;
   const int w = xcd_order(blockIdx.x, gridDim.x);
   const int bh = w / ntile, qt = ntile - 1 - w % ntile;
   const int b = bh / a.H, h = bh % a.H, hk = h / a.G;
   const int len = length_of(a, b);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
   const int r0 = qt * QB, i = r0 + 32 * wave + (lane & 31), ic = min(i, a.n_q - 1);
   const int last = min(a.n_q, len - a.q_start) - 1;
   const int p = a.q_start + i;
@@ -188,7 +228,7 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
   using Cp = Copy<T, DP, KT, NT>;
   auto copy = [&](int x) __attribute__((always_inline)) {
     const int k0 = kt.tile(x) * KT;
-    uint8_t* to = smem + (x & 1) * 2 * BYTES;
+    uint8_t* to = smem + (x / KS & 1) * 2 * BYTES;
     Cp::rows(to, row_of<T>(a.k, b, hk, k0), ldk, len - k0, a.d);
     Cp::rows(to + BYTES, row_of<T>(a.v, b, hk, k0), ldv, len - k0, a.d);
   };
@@ -214,23 +254,23 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
   };
   // use(tile, k0, RB, masked, bad) for each 32 keys that the wave sees something of
   auto over_tiles = [&](auto use) __attribute__((always_inline)) {
-    if (threadIdx.x == 0) found = -1;
-    if (n > 0) copy(0);
-    __syncthreads();
-    for (int x = 0; x < n; ++x) {
-      uint8_t* ks = smem + (x & 1) * 2 * BYTES;
+    if (Cp::thread() == 0) *found = -1;
+    if (ks_ < n) copy(ks_);
+    Cp::sync();
+    for (int x = ks_; x < n; x += KS) {
+      uint8_t* ks = smem + (x / KS & 1) * 2 * BYTES;
       const int k0 = kt.tile(x) * KT;
       uint64_t bad = 0;
-      if (sees(a, len, pa, pb, k0, KT) != 2 && __builtin_expect(Cp::holds_nonfinite(ks, x, &found), 0))
+      if (sees(a, len, pa, pb, k0, KT) != 2 && __builtin_expect(Cp::holds_nonfinite(ks, x, found), 0))
         bad = Cp::scrub(ks, mask);
-      if (x + 1 < n) copy(x + 1);
+      if (x + KS < n) copy(x + KS);
       auto part = [&](auto rb) __attribute__((always_inline)) {
         const int what = sees(a, len, wa, wb, k0 + rb, 32);
         if (what) use(ks, k0, rb, what == 1 || bad != 0, bad);
       };
       part(std::integral_constant<int, 0>{});
       if constexpr (KT == 64) part(std::integral_constant<int, 32>{});
-      __syncthreads();
+      Cp::sync();
     }
   };
   if (sizeof(T) == 2 && n <= 256 / KT) {
@@ -244,10 +284,19 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
 #pragma unroll
       for (int e = 0; e < 16; ++e) rest += s[e];
     });
+    if constexpr (KS > 1) {
+      float* all = reinterpret_cast<float*>(smem_) + lane;
+      __syncthreads();
+      all[ks_ * 64] = rest;
+      __syncthreads();
+      rest = 0.0f;
+      for (int w = 0; w < KS; ++w) rest += all[w * 64];
+      __syncthreads();
+    }
     rest = half_sum(rest);
     if (__builtin_isfinite(rest)) ndelta -= rest;   // (an infinite key that weighs nothing leaves the row its delta)
   }
-  if (i < a.n_q && lane < 32) {
+  if (i < a.n_q && lane < 32 && ks_ == 0) {
     g.nlse[at] = nlse;
     g.ndelta[at] = ndelta;
   }
@@ -259,6 +308,10 @@ __global__ __launch_bounds__(64 * NW, OCC) void k_window_dq(const WindowBwdArgs 
     scores(ks, k0, rb, masked, bad, s);
     mma_rows<T, DP, DP / 32, decltype(rb)::value>(dq, RowsB<T>(s), ks, 0);
   });
+  if constexpr (KS > 1) {
+    static_assert(DP / 2 * 64 * 4 <= 4 * BYTES, "sums of a wave");
+    if (!join_waves<KS, DP / 32>(dq, reinterpret_cast<float*>(smem_), ks_)) return;
+  }
   store_row<T, DP / 32>(row_of<T>(g.dq, b, h, ic), dq, a.scale, 0, a.d, i < a.n_q, !live);
 }
 
@@ -300,24 +353,30 @@ struct DkvJob {
 // dk and dv: 32 keys and values a wave stay in registers, queries and
 // cotangents pass through LDS, over every head that shares the keys. DO
 // columns of dk and dv a workgroup (DP, or less where both would not fit the
-// registers: the scores are then computed again for each part).
-template <typename T, int DP, int DO, int QT, int NW>
-__global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
+// registers: the scores are then computed again for each part). NW waves with
+// 32 keys each share a step's queries, or (NW = 1) QS waves share 32 keys, each
+// with every QS-th step's queries in LDS of its own, and add their sums.
+template <typename T, int DP, int DO, int QT, int NW, int QS>
+__global__ __launch_bounds__(64 * NW * QS) void k_window_dkv(const WindowBwdArgs g) {
   const WindowArgs& a = g.f;
   constexpr int KB = 32 * NW, NT = 64 * NW, NB = DO / 32;
   using L = Tile<T, DP>;
   constexpr int BYTES = QT * L::PITCH, STAGE = 2 * BYTES + 1024;   // tiles start at multiples of their pitch
   static_assert(2 * QT * 4 <= 1024, "lse2 and delta of a step");
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * STAGE];
-  __shared__ uint32_t mask[2];
-  __shared__ int found;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem_[QS * 2 * STAGE];
+  __shared__ uint32_t mask_[2 * QS];
+  __shared__ int found_[QS];
+  const int wave_ = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = QS > 1 ? 0 : wave_, qs_ = QS > 1 ? wave_ : 0;   // of the keys; of the queries
+  uint8_t* const smem = smem_ + qs_ * 2 * STAGE;
+  uint32_t* const mask = mask_ + 2 * qs_;
+  int* const found = found_ + qs_;
   constexpr int ND = DP / DO;
   const int dsel = blockIdx.x % ND;
   DkvJob job(a, g.plan, blockIdx.x / ND, gridDim.x / ND);
   const int bk = job.bk, b = bk / a.Hkv, hk = bk % a.Hkv;
   const int len = length_of(a, b);
   job.queries(a, g.plan, len);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
   const int kw = job.tile * KB + 32 * wave, j = kw + (lane & 31), jc = min(j, a.n_kv - 1);
   const bool live = j < len;
   const int iend = min(a.n_q, len - a.q_start);   // queries past it are padding
@@ -340,7 +399,7 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
   typedef __attribute__((address_space(3))) void lds_void;
   auto copy = [&](int x) __attribute__((always_inline)) {
     const int h = hk * a.G + job.head_part * gh + x / steps, i0 = job.qa + (x % steps) * QT;
-    uint8_t* to = smem + (x & 1) * STAGE;
+    uint8_t* to = smem + (x / QS & 1) * STAGE;
     Cp::rows(to, row_of<T>(a.q, b, h, i0), ldq, job.qb - i0, a.d);
     Cp::rows(to + BYTES, row_of<T>(g.dout, b, h, i0), ldo, job.qb - i0, a.d);
     if (wave == 0) {   // nlse and ndelta of the queries; past the last one zeros (masked)
@@ -401,19 +460,19 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
     mma_rows<T, DP, NB, RB>(dv, RowsB<T>(s), os, dsel * NB);
     mma_rows<T, DP, NB, RB>(dk, RowsB<T>(dp), qs, dsel * NB);
   };
-  if (threadIdx.x == 0) found = -1;
-  if (n > 0) copy(0);
-  __syncthreads();
-  for (int x = 0; x < n; ++x) {
-    uint8_t* qs = smem + (x & 1) * STAGE;
+  if (Cp::thread() == 0) *found = -1;
+  if (qs_ < n) copy(qs_);
+  Cp::sync();
+  for (int x = qs_; x < n; x += QS) {
+    uint8_t* qs = smem + (x / QS & 1) * STAGE;
     const int i0 = job.qa + (x % steps) * QT;
     uint64_t badq = 0, bado = 0;
     if (seen(i0, QT, kb0, kb1) != 2 &&
-        __builtin_expect(Cp2::holds_nonfinite(qs, x, &found), 0)) {
+        __builtin_expect(Cp2::holds_nonfinite(qs, x, found), 0)) {
       badq = Cp::scrub(qs, mask);
       bado = Cp::scrub(qs + BYTES, mask);
     }
-    if (x + 1 < n) copy(x + 1);
+    if (x + QS < n) copy(x + QS);
     auto part = [&](auto rb) __attribute__((always_inline)) {
       const int what = seen(i0 + rb, 32, kw, kw + 31);
       if (what) step(qs, i0, rb, what == 1 || (badq | bado) != 0, badq, bado);
@@ -425,7 +484,12 @@ __global__ __launch_bounds__(64 * NW) void k_window_dkv(const WindowBwdArgs g) {
       const int i = i0 + __builtin_ctzll(bado), h = hk * a.G + job.head_part * gh + x / steps;
       add_nonfinite<T, NB>(dv, row_of<T>(g.dout, b, h, i), i >= ilo && i <= ihi, dsel * DO, a.d);
     }
-    __syncthreads();
+    Cp::sync();
+  }
+  if constexpr (QS > 1) {
+    static_assert((QS - 1) * NB * 16 * 64 * 4 <= QS * 2 * STAGE, "sums of the waves");
+    join_waves<QS, NB>(dk, reinterpret_cast<float*>(smem_), qs_);
+    if (!join_waves<QS, NB>(dv, reinterpret_cast<float*>(smem_), qs_)) return;
   }
   if (job.slot < 0) {
     store_row<T, NB>(row_of<T>(g.dk, b, hk, jc), dk, a.scale, dsel * DO, a.d, j < a.n_kv, !live);
@@ -584,26 +648,11 @@ __global__ __launch_bounds__(256 * QH, 2) void k_window_dkv16(const WindowBwdArg
     }
     barrier_only();
   }
-  if constexpr (QH == 2) {   // the second wave's sums to the first, dk and then dv
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      f32x16 (&acc)[NB] = which ? dv : dk;
-      float* to = reinterpret_cast<float*>(smem) + (kg * NB * 16) * 64 + lane;
-      static_assert(4 * NB * 16 * 64 * 4 <= VB + RING * STAGE, "sums of four waves");
-      __syncthreads();
-      if (qh == 1)
-#pragma unroll
-        for (int x = 0; x < NB; ++x)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) to[(x * 16 + e) * 64] = acc[x][e];
-      __syncthreads();
-      if (qh == 0)
-#pragma unroll
-        for (int x = 0; x < NB; ++x)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) acc[x][e] += to[(x * 16 + e) * 64];
-    }
-    if (qh == 1) return;
+  if constexpr (QH == 2) {   // the second wave's sums to the first
+    static_assert(4 * NB * 16 * 64 * 4 <= VB + RING * STAGE, "sums of four waves");
+    float* to = reinterpret_cast<float*>(smem) + kg * NB * 16 * 64;
+    join_waves<2, NB>(dk, to, qh);
+    if (!join_waves<2, NB>(dv, to, qh)) return;
   }
   if (job.slot < 0) {
     store_row<T, NB>(row_of<T>(g.dk, b, hk, jc), dk, a.scale, 0, a.d, j < a.n_kv, !live);
@@ -652,22 +701,30 @@ __global__ __launch_bounds__(256) void k_window_dkv_sum(const WindowBwdArgs g) {
 
 int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// Below so many workgroups of four waves, workgroups of one: its LDS holds two
-// of them a CU, so up to 512 run at once, each on less work ([1, 2, 256, 64]
-// fp32, window 64, training: 55 us, with four waves 94; [1, 8, 512, 64], window
-// 256: 44 and 47; from 512 on they only take turns: [1, 16 / 4, 2048, 128] fp32,
-// window 1024: 1605 and 808).
-constexpr int kFewBlocks = 128;
+// Waves that may share 32 queries (or keys): as many as have room in LDS for
+// tiles of their own.
+constexpr int sharers(bool bf16, int DP) { return DP <= 64 ? 4 : bf16 || DP <= 128 ? 2 : 1; }
 
-// Workgroups of one wave (32 queries) where those of four would leave CUs idle.
-bool single_waves(const WindowArgs& a) { return (int64_t)a.B * a.H * cdiv(a.n_q, 128) < kFewBlocks; }
+// Where workgroups of 128 of n rows would leave CUs idle, workgroups of 32 whose
+// waves take turns at the other side's tiles and join their sums: more CUs and
+// a shorter chain of tiles. Their LDS holds one workgroup a CU, so the limit
+// is the number of workgroups that still run at once. Training, this and
+// workgroups of 128: [1, 2, 256, 64] fp32, window 64: 43 and 94 us;
+// [1, 8 / 4, 2048, 64] fp32, window 512 (128 workgroups): 165 and 260;
+// [1, 8 / 4, 2048, 128] bf16 (the same with two sharers): 118 and 96.
+bool few_blocks(const WindowArgs& a, bool bf16, int n) {
+  const int W = sharers(bf16, a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256);
+  return W > 1 && (int64_t)a.B * a.H * cdiv(n, 128) < 64 * W;
+}
 
 template <typename T, int DP>
 hipError_t fwd(const WindowArgs& a, hipStream_t s) {
-  constexpr int OCC = sizeof(T) == 4 || DP > 128 ? 1 : DP > 64 ? 2 : 4;
+  constexpr int OCC = sizeof(T) == 4 || DP > 128 ? 1 : DP > 64 ? 2 : 4, W = sharers(sizeof(T) == 2, DP);
   const int64_t bh = (int64_t)a.B * a.H;
-  if (single_waves(a)) k_window_fwd<T, DP, 1, 1><<<(unsigned)(bh * cdiv(a.n_q, 32)), 64, 0, s>>>(a);
-  else k_window_fwd<T, DP, 4, OCC><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(a);
+  if (W > 1 && few_blocks(a, sizeof(T) == 2, a.n_q))
+    k_window_fwd<T, DP, (W > 1 ? 1 : 4), W, (W > 1 ? 1 : OCC)><<<(unsigned)(bh * cdiv(a.n_q, 32)), 64 * W, 0, s>>>(a);
+  else
+    k_window_fwd<T, DP, 4, 1, OCC><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -675,19 +732,21 @@ template <typename T, int DP>
 hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
   const WindowArgs& a = g.f;
   constexpr bool H16 = sizeof(T) == 2;
-  constexpr int DO = DP <= 128 ? DP : H16 ? 128 : 64, QT = 32;
+  constexpr int DO = DP <= 128 ? DP : H16 ? 128 : 64, QT = 32, W = sharers(H16, DP);
   const int64_t bh = (int64_t)a.B * a.H, bk = (int64_t)a.B * a.Hkv;
   if (a.n_q > 0) {
-    if (single_waves(a)) k_window_dq<T, DP, 1, 1><<<(unsigned)(bh * cdiv(a.n_q, 32)), 64, 0, s>>>(g);
-    else k_window_dq<T, DP, 4, (H16 && DP <= 128 ? 2 : 1)><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(g);
+    if (W > 1 && few_blocks(a, H16, a.n_q))
+      k_window_dq<T, DP, (W > 1 ? 1 : 4), W, 1><<<(unsigned)(bh * cdiv(a.n_q, 32)), 64 * W, 0, s>>>(g);
+    else
+      k_window_dq<T, DP, 4, 1, (H16 && DP <= 128 ? 2 : 1)><<<(unsigned)(bh * cdiv(a.n_q, 128)), 256, 0, s>>>(g);
   }
   if (a.n_kv > 0) {
     if constexpr (H16 && DP <= 128)
       k_window_dkv16<DP, DP / 64><<<(unsigned)(bk * g.plan.jobs()), 256 * (DP / 64), 0, s>>>(g);
-    else if (g.plan.kb == 32)
-      k_window_dkv<T, DP, DO, QT, 1><<<(unsigned)(bk * g.plan.jobs() * (DP / DO)), 64, 0, s>>>(g);
+    else if (W > 1 && g.plan.kb == 32)
+      k_window_dkv<T, DP, DO, QT, (W > 1 ? 1 : 4), W><<<(unsigned)(bk * g.plan.jobs() * (DP / DO)), 64 * W, 0, s>>>(g);
     else
-      k_window_dkv<T, DP, DO, QT, 4><<<(unsigned)(bk * g.plan.jobs() * (DP / DO)), 256, 0, s>>>(g);
+      k_window_dkv<T, DP, DO, QT, 4, 1><<<(unsigned)(bk * g.plan.jobs() * (DP / DO)), 256, 0, s>>>(g);
     const DkvPlan& pl = g.plan;
     const bool ps = pl.np_s * pl.gs > 1 && pl.st > 0, pa = pl.np_a * pl.gs > 1;
     const int t0 = pl.np_s * pl.gs > 1 ? 0 : pl.st, t1 = pa ? pl.ntile : pl.st;
@@ -709,7 +768,7 @@ hipError_t bwd(const WindowBwdArgs& g, hipStream_t s) {
 DkvPlan window_dkv_plan(const WindowArgs& a, bool bf16) {
   DkvPlan p{};
   // (16-bit of up to 128 columns has kernels of 128 keys only)
-  const bool few = (int64_t)a.B * a.H * cdiv(a.n_kv, 128) < kFewBlocks && (!bf16 || a.d > 128);
+  const bool few = (!bf16 || a.d > 128) && few_blocks(a, bf16, a.n_kv);
   p.kb = few ? 32 : 128;
   p.ntile = cdiv(a.n_kv, p.kb);
   const int n_q = std::max(a.n_q, 1);
