@@ -532,16 +532,14 @@ struct Softmax {
 struct Sight {
   int lo, sink;
   uint32_t span;
-  bool sinks;    // whether the tile holds sinks (the same in all lanes)
   template <class Args>
   __device__ __forceinline__ Sight(const Args& a, int p, int jhi, int k0) {
     const int at = k0 + 4 * (int)((threadIdx.x >> 5) & 1), jlo = p - a.win + 1;
     lo = jhi < jlo ? (1 << 30) : jlo - at;
     span = (uint32_t)max(jhi - jlo, 0);
-    sinks = k0 < a.sinks;
-    sink = min(a.sinks, jhi + 1) - at;
+    sink = k0 < a.sinks ? min(a.sinks, jhi + 1) - at : -(1 << 30);
   }
-  __device__ __forceinline__ bool see(int r) const { return (uint32_t)(r - lo) <= span || (sinks && r < sink); }
+  __device__ __forceinline__ bool see(int r) const { return ((uint32_t)(r - lo) <= span) | (r < sink); }
 };
 
 // The 32 keys of a tile from row RB: scores, weights, and their products with
