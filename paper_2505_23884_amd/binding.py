@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "liblact.so")
@@ -772,11 +773,86 @@ def rmsnorm_out_backward(o, dy, weight=None, eps=1e-6, with_dweight=True, out=No
 
 # ---- the attention half of a hybrid layer (strided tensors are taken as they lie)
 
-# These calls can be as short as a kernel launch, so their checks read each
-# property of a tensor once.
+# These calls can be as short as a kernel launch, which the host then cannot
+# keep up with: their checks read each property of a tensor once, and
+# descriptors and views go to the library as packed bytes. One token's norm and
+# rotation takes 14.8 us with ctypes structures, 12.1 so (the C call 4 of them).
 
-def _io(t, name):
-    import torch
+_pack_view = struct.Struct("Pqqq").pack
+_pack_rope = struct.Struct("4i2q4ifi").pack
+_pack_attn = struct.Struct("4i6qfi").pack
+_pack_paged = struct.Struct("4i2q2i2qfi").pack
+_packed = {}
+
+
+def _fn(name):
+    """The entry point taking descriptors and views as bytes."""
+    f = _packed.get(name)
+    if f is None:
+        L = lib()
+        f = L[name]      # a function object of its own: the attribute keeps its prototype
+        f.restype = getattr(L, name).restype
+        f.argtypes = [ctypes.c_char_p if issubclass(t, ctypes._Pointer) and issubclass(t._type_, ctypes.Structure) else t
+                      for t in getattr(L, name).argtypes]
+        _packed[name] = f
+    return f
+
+
+def _pack(pack, *fields):
+    try:
+        return pack(*fields)
+    except struct.error as e:
+        raise LactError(-1, f"an argument is out of range: {e}") from None
+
+
+def _refuse(t, name, shape, dtype, dev):
+    if t.shape != shape:
+        raise LactError(-1, f"{name} must be {list(shape)}, not {list(t.shape)}")
+    if t.dtype != dtype:
+        raise LactError(-1, f"{name} must be {dtype}, not {t.dtype}")
+    if dev < 0 or t.get_device() != dev:
+        raise LactError(-1, f"{name} must be a device tensor, on the first one's device")
+    raise LactError(-1, f"{name}'s last dimension must be contiguous")
+
+
+def _view(t, name, shape, dtype, dev):
+    """lact_view of a tensor [batch, head, token, d] of that shape, type and
+    device, vectors consecutive."""
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev >= 0:
+        s = t.stride()
+        if s[3] == 1:
+            return _pack_view(t.data_ptr(), s[0], s[1], s[2])
+    _refuse(t, name, shape, dtype, dev)
+
+
+def _view_t(t, name, shape, dtype, dev):
+    """The same of a tensor [batch, token, head, d]."""
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev >= 0:
+        s = t.stride()
+        if s[3] == 1:
+            return _pack_view(t.data_ptr(), s[0], s[2], s[1])
+    _refuse(t, name, shape, dtype, dev)
+
+
+def _view_n(t, name, shape, dtype, dev):
+    """The same of a tensor [token, head, d]."""
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev >= 0:
+        s = t.stride()
+        if s[2] == 1:
+            return _pack_view(t.data_ptr(), 0, s[1], s[0])
+    _refuse(t, name, shape, dtype, dev)
+
+
+def _aux(t, name, shape, dtype, dev):
+    """The address of a contiguous tensor of that shape, type and device, or None."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise LactError(-1, f"{name} must be a contiguous {dtype} tensor {list(shape)} on device {dev}")
+    return t.data_ptr()
+
+
+def _io(t, name, torch):
     if t.dtype is torch.bfloat16:
         return IO_BF16
     if t.dtype is torch.float32:
@@ -784,93 +860,58 @@ def _io(t, name):
     raise LactError(-1, f"unsupported {name} dtype {t.dtype}")
 
 
-def _view(t):
-    """LactView of a tensor [batch, head, token, d]."""
-    s = t.stride()
-    return LactView(t.data_ptr(), s[0], s[1], s[2])
-
-
-def _view_t(t):
-    """LactView of a tensor [batch, token, head, d]."""
-    s = t.stride()
-    return LactView(t.data_ptr(), s[0], s[2], s[1])
-
-
-def _view_n(t):
-    """LactView of a tensor [token, head, d]."""
-    s = t.stride()
-    return LactView(t.data_ptr(), 0, s[1], s[0])
-
-
-def _check(t, name, shape, like):
-    """A tensor of `shape`, of like's type and on its device, vectors consecutive."""
-    dev = like.get_device()
-    if t.shape == shape and t.dtype is like.dtype and dev >= 0 and t.get_device() == dev and \
-            (t.stride(-1) == 1 or shape[-1] <= 1):
-        return
-    if t.shape != shape:
-        raise LactError(-1, f"{name} must be {list(shape)}, not {list(t.shape)}")
-    if t.dtype != like.dtype:
-        raise LactError(-1, f"{name} must be {like.dtype}, not {t.dtype}")
-    if dev < 0 or t.get_device() != dev:
-        raise LactError(-1, f"{name} must be a device tensor, on the first one's device")
-    raise LactError(-1, f"{name}'s last dimension must be contiguous")
-
-
-def _check_aux(t, name, shape, dtype, like):
-    if t is not None and (t.shape != shape or t.dtype is not dtype or t.get_device() != like.get_device()
-                          or not t.is_contiguous()):
-        raise LactError(-1, f"{name} must be a contiguous {dtype} tensor {list(shape)} on {like.device}")
-
-
-def _call(fn, like, stream, *args):
-    """fn(*args, stream) on like's device and its current stream (or `stream`)."""
-    import torch
-    i = like.get_device()
-    if torch.cuda.current_device() == i:
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(i) if stream is None else stream)
+def _call(name, dev, stream, torch, *args):
+    """The entry point on device `dev` and its current stream (or `stream`)."""
+    C = torch._C
+    f = _packed.get(name) or _fn(name)
+    if C._cuda_getDevice() == dev:
+        rc = f(*args, C._cuda_getCurrentRawStream(dev) if stream is None else stream)
     else:
-        with torch.cuda.device(i):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(i) if stream is None else stream)
+        with torch.cuda.device(dev):
+            rc = f(*args, C._cuda_getCurrentRawStream(dev) if stream is None else stream)
     if rc:
         _raise(rc)
 
 
-def _workspace(fn, desc, workspace, like):
-    import torch
-    err = ctypes.c_int(0)
-    n = int(fn(ctypes.byref(desc), ctypes.byref(err)))
-    if err.value:
-        _raise(err.value)
+def _workspace(name, desc, workspace, like, torch):
+    """(tensor that stays alive, address, bytes) of the caller's workspace, or of
+    a new one of the size that the call needs (0 too where the descriptor is
+    refused, which the call itself then says)."""
     if workspace is None:
-        return (torch.empty(n, dtype=torch.uint8, device=like.device) if n else None), n
+        n = _fn(name)(desc, None)
+        if not n:
+            return None, None, 0
+        workspace = like.new_empty(n, dtype=torch.uint8)
+        return workspace, workspace.data_ptr(), n
     if workspace.device != like.device or not workspace.is_contiguous():
         raise LactError(-1, f"workspace must be a contiguous tensor on {like.device}")
-    return workspace, workspace.numel() * workspace.element_size()
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
-def _p(t):
-    return None if t is None else t.data_ptr()
-
-
-def _rope_desc(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved):
-    import torch
+def _rope_args(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved, torch):
+    """Shapes, device and the first arguments of the norm and rotation and its reverse."""
     if q.dim() != 4 or k.dim() != 4:
         raise LactError(-1, "q must be [B, n, H, d] and k [B, n, Hkv, d]")
     B, n, H, d = q.shape
     Hkv = k.shape[2]
-    _check(q, "q", (B, n, H, d), q)
-    _check(k, "k", (B, n, Hkv, d), q)
-    per_head = any(w is not None and w.dim() == 2 for w in (wq, wk))
-    _check_aux(wq, "wq", (H, d) if per_head else (d,), torch.float32, q)
-    _check_aux(wk, "wk", (Hkv, d) if per_head else (d,), torch.float32, q)
-    if inv_freq is not None and inv_freq.dim() != 1:
-        raise LactError(-1, "inv_freq must be [rot / 2]")
-    rot = 0 if inv_freq is None else 2 * inv_freq.shape[0]
-    if rot:
-        _check_aux(inv_freq, "inv_freq", (rot // 2,), torch.float64, q)
-    _check_aux(positions, "positions", (B, n), torch.int32, q)
-    return LactRopeDesc(B, H, Hkv, d, n, int(pos0), rot, int(bool(interleaved)), int(per_head), _io(q, "q"), float(eps), 0)
+    dt, dev = q.dtype, q.get_device()
+    io = _io(q, "q", torch)
+    qv = _view_t(q, "q", (B, n, H, d), dt, dev)
+    kv = _view_t(k, "k", (B, n, Hkv, d), dt, dev)
+    per_head = (wq is not None and wq.dim() == 2) or (wk is not None and wk.dim() == 2)
+    wqp = _aux(wq, "wq", (H, d) if per_head else (d,), torch.float32, dev)
+    wkp = _aux(wk, "wk", (Hkv, d) if per_head else (d,), torch.float32, dev)
+    rot, ip = 0, None
+    if inv_freq is not None:
+        if inv_freq.dim() != 1:
+            raise LactError(-1, "inv_freq must be [rot / 2]")
+        half = inv_freq.shape[0]
+        rot = 2 * half
+        if half:
+            ip = _aux(inv_freq, "inv_freq", (half,), torch.float64, dev)
+    desc = _pack(_pack_rope, B, H, Hkv, d, n, int(pos0), rot, 1 if interleaved else 0, 1 if per_head else 0, io,
+                 float(eps), 0)
+    return (B, n, H, Hkv, d), dt, dev, (desc, qv, kv, wqp, wkp, ip, _aux(positions, "positions", (B, n), torch.int32, dev))
 
 
 def qk_norm_rope(q, k, wq=None, wk=None, inv_freq=None, *, positions=None, pos0=0, eps=1e-6, interleaved=False,
@@ -883,16 +924,10 @@ def qk_norm_rope(q, k, wq=None, wk=None, inv_freq=None, *, positions=None, pos0=
     (pos0 + token). Returns (qn [B, H, n, d], kn [B, Hkv, n, d]), into ``out``
     (two tensors of those shapes, any strides) when it is given."""
     import torch
-    desc = _rope_desc(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved)
-    B, n, H, d = q.shape
-    if out is None:
-        out = (torch.empty(B, H, n, d, dtype=q.dtype, device=q.device),
-               torch.empty(B, k.shape[2], n, d, dtype=q.dtype, device=q.device))
-    qn, kn = out
-    _check(qn, "qn", (B, H, n, d), q)
-    _check(kn, "kn", (B, k.shape[2], n, d), q)
-    _call(lib().lact_qk_norm_rope, q, stream, desc, _view_t(q), _view_t(k), _p(wq), _p(wk),
-          _p(inv_freq) if desc.rot else None, _p(positions), _view(qn), _view(kn))
+    (B, n, H, Hkv, d), dt, dev, args = _rope_args(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved, torch)
+    qn, kn = (q.new_empty((B, H, n, d)), q.new_empty((B, Hkv, n, d))) if out is None else out
+    _call("lact_qk_norm_rope", dev, stream, torch, *args, _view(qn, "qn", (B, H, n, d), dt, dev),
+          _view(kn, "kn", (B, Hkv, n, d), dt, dev))
     return qn, kn
 
 
@@ -903,45 +938,39 @@ def qk_norm_rope_backward(q, k, dqn, dkn, wq=None, wk=None, inv_freq=None, *, po
     dk [B, n, Hkv, d], dwq, dwk); the weights' cotangents are None without a
     weight or with_dweight. ``out`` may hold that tuple."""
     import torch
-    desc = _rope_desc(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved)
-    B, n, H, d = q.shape
-    Hkv = k.shape[2]
-    _check(dqn, "dqn", (B, H, n, d), q)
-    _check(dkn, "dkn", (B, Hkv, n, d), q)
+    (B, n, H, Hkv, d), dt, dev, args = _rope_args(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved, torch)
     if out is None:
         dw = [torch.empty_like(w) if w is not None and with_dweight else None for w in (wq, wk)]
-        out = (torch.empty(B, n, H, d, dtype=q.dtype, device=q.device),
-               torch.empty(B, n, Hkv, d, dtype=q.dtype, device=q.device), *dw)
+        out = (q.new_empty((B, n, H, d)), q.new_empty((B, n, Hkv, d)), *dw)
     dq, dk, dwq, dwk = out
-    _check(dq, "dq", (B, n, H, d), q)
-    _check(dk, "dk", (B, n, Hkv, d), q)
+    dwp = []
     for t, w, name in ((dwq, wq, "dwq"), (dwk, wk, "dwk")):
         if t is not None and w is None:
             raise LactError(-1, f"{name} needs its weight")
-        if t is not None:
-            _check_aux(t, name, w.shape, torch.float32, q)
-    nb = 0
+        dwp.append(None if t is None else _aux(t, name, w.shape, torch.float32, dev))
+    wp, nb = None, 0
     if dwq is not None or dwk is not None:
-        workspace, nb = _workspace(lib().lact_qk_norm_rope_backward_workspace_bytes, desc, workspace, q)
-    _call(lib().lact_qk_norm_rope_backward, q, stream, desc, _view_t(q), _view_t(k), _p(wq), _p(wk),
-          _p(inv_freq) if desc.rot else None, _p(positions), _view(dqn), _view(dkn), _view_t(dq),
-          _view_t(dk), _p(dwq), _p(dwk), _p(workspace), nb)
+        workspace, wp, nb = _workspace("lact_qk_norm_rope_backward_workspace_bytes", args[0], workspace, q, torch)
+    _call("lact_qk_norm_rope_backward", dev, stream, torch, *args, _view(dqn, "dqn", (B, H, n, d), dt, dev),
+          _view(dkn, "dkn", (B, Hkv, n, d), dt, dev), _view_t(dq, "dq", (B, n, H, d), dt, dev),
+          _view_t(dk, "dk", (B, n, Hkv, d), dt, dev), *dwp, wp, nb)
     return dq, dk, dwq, dwk
 
 
-def _attn_desc(q, k, v, window, sinks, lookahead, lengths, scale, q_start):
-    import torch
-    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+def _attn_args(q, k, v, window, sinks, lookahead, lengths, scale, q_start, torch):
+    """Shapes of q and of k and v, type, device and the first arguments of
+    window attention and its reverse."""
+    if q.dim() != 4 or k.dim() != 4:
         raise LactError(-1, "q must be [B, H, n_q, d], k and v [B, Hkv, n_kv, d]")
-    B, H, n_q, d = q.shape
+    sq = B, H, n_q, d = q.shape
     Hkv, n_kv = k.shape[1], k.shape[2]
-    _check(q, "q", (B, H, n_q, d), q)
-    _check(k, "k", (B, Hkv, n_kv, d), q)
-    _check(v, "v", (B, Hkv, n_kv, d), q)
-    _check_aux(lengths, "lengths", (B,), torch.int32, q)
-    return LactAttnDesc(B, H, Hkv, d, n_q, n_kv, n_kv - n_q if q_start is None else int(q_start),
-                        -1 if window is None else int(window), -1 if lookahead is None else int(lookahead), int(sinks),
-                        d ** -0.5 if scale is None else float(scale), _io(q, "q"))
+    sk = (B, Hkv, n_kv, d)
+    dt, dev = q.dtype, q.get_device()
+    desc = _pack(_pack_attn, B, H, Hkv, d, n_q, n_kv, n_kv - n_q if q_start is None else int(q_start),
+                 -1 if window is None else int(window), -1 if lookahead is None else int(lookahead), int(sinks),
+                 d ** -0.5 if scale is None else float(scale), _io(q, "q", torch))
+    return sq, sk, dt, dev, (desc, _view(q, "q", sq, dt, dev), _view(k, "k", sk, dt, dev), _view(v, "v", sk, dt, dev)), \
+        _aux(lengths, "lengths", (B,), torch.int32, dev)
 
 
 def window_attention(q, k, v, *, window=None, sinks=0, lookahead=0, lengths=None, scale=None, q_start=None,
@@ -956,16 +985,14 @@ def window_attention(q, k, v, *, window=None, sinks=0, lookahead=0, lengths=None
     Returns o like q, or (o, lse fp32 [B, H, n_q]) with_lse; ``out`` may hold o,
     or that pair."""
     import torch
-    desc = _attn_desc(q, k, v, window, sinks, lookahead, lengths, scale, q_start)
-    B, H, n_q, _ = q.shape
+    sq, _, dt, dev, args, lp = _attn_args(q, k, v, window, sinks, lookahead, lengths, scale, q_start, torch)
     if out is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty(B, H, n_q, dtype=torch.float32, device=q.device) if with_lse else None
+        o = q.new_empty(sq)
+        lse = q.new_empty(sq[:3], dtype=torch.float32) if with_lse else None
     else:
         o, lse = out if with_lse else (out, None)
-    _check(o, "o", q.shape, q)
-    _check_aux(lse, "lse", (B, H, n_q), torch.float32, q)
-    _call(lib().lact_window_attention, q, stream, desc, _view(q), _view(k), _view(v), _p(lengths), _view(o), _p(lse))
+    _call("lact_window_attention", dev, stream, torch, *args, lp, _view(o, "o", sq, dt, dev),
+          _aux(lse, "lse", sq[:3], torch.float32, dev))
     return (o, lse) if with_lse else o
 
 
@@ -975,37 +1002,29 @@ def window_attention_backward(q, k, v, o, lse, dout, *, window=None, sinks=0, lo
     o and lse and the cotangent dout of o, returns (dq, dk, dv), written into
     ``out`` (that tuple) when it is given."""
     import torch
-    desc = _attn_desc(q, k, v, window, sinks, lookahead, lengths, scale, q_start)
-    _check(o, "o", q.shape, q)
-    _check(dout, "dout", q.shape, q)
+    sq, sk, dt, dev, args, lp = _attn_args(q, k, v, window, sinks, lookahead, lengths, scale, q_start, torch)
     if lse is None:
         raise LactError(-1, "lse of the forward is needed")
-    _check_aux(lse, "lse", q.shape[:3], torch.float32, q)
-    if out is None:
-        out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-    dq, dk, dv = out
-    for t, ref, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
-        _check(t, name, ref.shape, q)
-    workspace, nb = _workspace(lib().lact_window_attention_backward_workspace_bytes, desc, workspace, q)
-    _call(lib().lact_window_attention_backward, q, stream, desc, _view(q), _view(k), _view(v), _view(o), _p(lse),
-          _view(dout), _p(lengths), _view(dq), _view(dk), _view(dv), _p(workspace), nb)
+    dq, dk, dv = (q.new_empty(sq), q.new_empty(sk), q.new_empty(sk)) if out is None else out
+    workspace, wp, nb = _workspace("lact_window_attention_backward_workspace_bytes", args[0], workspace, q, torch)
+    _call("lact_window_attention_backward", dev, stream, torch, *args, _view(o, "o", sq, dt, dev),
+          _aux(lse, "lse", sq[:3], torch.float32, dev), _view(dout, "dout", sq, dt, dev), lp,
+          _view(dq, "dq", sq, dt, dev), _view(dk, "dk", sk, dt, dev), _view(dv, "dv", sk, dt, dev), wp, nb)
     return dq, dk, dv
 
 
-def _paged_desc(x, H, k_cache, v_cache, table, lens, cu_new, window, sinks, scale):
-    import torch
-    if x.dim() != 3 or k_cache.dim() != 4 or table.dim() != 2:
+def _paged_args(x, H, k_cache, v_cache, table, lens, cu_new, window, sinks, scale, torch):
+    """The descriptor, the caches' views and the addresses of the tables."""
+    if k_cache.dim() != 4 or table.dim() != 2:
         raise LactError(-1, "new tokens are [n_new, heads, d], caches [pages, page, Hkv, d], table [B, max_pages]")
-    pages, page, Hkv, d = k_cache.shape
+    sc = pages, page, Hkv, d = k_cache.shape
     B, max_pages = table.shape
-    _check(x, "the new tokens", (x.shape[0], x.shape[1], d), x)
-    _check(k_cache, "k_cache", k_cache.shape, x)
-    _check(v_cache, "v_cache", k_cache.shape, x)
-    _check_aux(table, "table", (B, max_pages), torch.int32, x)
-    _check_aux(lens, "lens", (B,), torch.int32, x)
-    _check_aux(cu_new, "cu_new", (B + 1,), torch.int32, x)
-    return LactPagedDesc(B, H, Hkv, d, x.shape[0], pages, page, max_pages, -1 if window is None else int(window),
-                         int(sinks), d ** -0.5 if scale is None else float(scale), _io(x, "new tokens"))
+    dt, dev, i32 = x.dtype, x.get_device(), torch.int32
+    desc = _pack(_pack_paged, B, H, Hkv, d, x.shape[0], pages, page, max_pages, -1 if window is None else int(window),
+                 int(sinks), d ** -0.5 if scale is None else float(scale), _io(x, "new tokens", torch))
+    return d, dt, dev, desc, (_view_t(k_cache, "k_cache", sc, dt, dev), _view_t(v_cache, "v_cache", sc, dt, dev),
+                              _aux(table, "table", (B, max_pages), i32, dev), _aux(lens, "lens", (B,), i32, dev),
+                              _aux(cu_new, "cu_new", (B + 1,), i32, dev))
 
 
 def paged_append(k, v, k_cache, v_cache, table, lens, cu_new, *, stream=None):
@@ -1014,12 +1033,13 @@ def paged_append(k, v, k_cache, v_cache, table, lens, cu_new, *, stream=None):
     place), table int32 [B, max_pages], lens int32 [B] (tokens of a sequence,
     the new ones included), cu_new int32 [B + 1] (rows of a sequence's new
     tokens, which are its last positions)."""
-    desc = _paged_desc(k, k.shape[1], k_cache, v_cache, table, lens, cu_new, None, 0, 1.0)
-    if k.shape[1] != desc.Hkv:
-        raise LactError(-1, "k must be [n_new, Hkv, d]")
-    _check(v, "v", k.shape, k)
-    _call(lib().lact_paged_append, k, stream, desc, _view_n(k), _view_n(v), _view_t(k_cache),
-          _view_t(v_cache), _p(table), _p(lens), _p(cu_new))
+    import torch
+    if k.dim() != 3 or k_cache.dim() != 4:
+        raise LactError(-1, "k and v are [n_new, Hkv, d], caches [pages, page, Hkv, d]")
+    Hkv = k_cache.shape[2]
+    d, dt, dev, desc, tail = _paged_args(k, Hkv, k_cache, v_cache, table, lens, cu_new, None, 0, 1.0, torch)
+    s = (k.shape[0], Hkv, d)
+    _call("lact_paged_append", dev, stream, torch, desc, _view_n(k, "k", s, dt, dev), _view_n(v, "v", s, dt, dev), *tail)
 
 
 def paged_attention(q, k_cache, v_cache, table, lens, cu_new, *, window=None, sinks=0, scale=None, out=None,
@@ -1029,12 +1049,15 @@ def paged_attention(q, k_cache, v_cache, table, lens, cu_new, *, window=None, si
     paged_append(), window and sinks of window_attention(). Returns o like q
     (rows of no sequence are left as they were), into ``out`` when given."""
     import torch
-    desc = _paged_desc(q, q.shape[1] if q.dim() == 3 else 0, k_cache, v_cache, table, lens, cu_new, window, sinks, scale)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-    _check(o, "o", q.shape, q)
-    workspace, nb = _workspace(lib().lact_paged_attention_workspace_bytes, desc, workspace, q)
-    _call(lib().lact_paged_attention, q, stream, desc, _view_n(q), _view_t(k_cache),
-          _view_t(v_cache), _p(table), _p(lens), _p(cu_new), _view_n(o), _p(workspace), nb)
+    if q.dim() != 3:
+        raise LactError(-1, "q must be [n_new, H, d]")
+    T, H, _ = q.shape
+    d, dt, dev, desc, tail = _paged_args(q, H, k_cache, v_cache, table, lens, cu_new, window, sinks, scale, torch)
+    s = (T, H, d)
+    qv = _view_n(q, "q", s, dt, dev)
+    o = q.new_empty(s) if out is None else out
+    workspace, wp, nb = _workspace("lact_paged_attention_workspace_bytes", desc, workspace, q, torch)
+    _call("lact_paged_attention", dev, stream, torch, desc, qv, *tail, _view_n(o, "o", s, dt, dev), wp, nb)
     return o
 
 

@@ -182,6 +182,13 @@ def test_tensors_of_the_host_are_refused():
             call()
 
 
+def test_numbers_that_no_field_holds_are_refused():
+    t = torch.zeros(1, 2, 8, 64, dtype=torch.bfloat16)
+    for opt in (dict(window=1 << 70), dict(q_start=-(1 << 64)), dict(sinks=1 << 63)):
+        with pytest.raises(P.LactError, match="out of range"):
+            P.window_attention(t, t, t, **opt)
+
+
 @pytest.mark.parametrize("window,sinks,look", [(None, 0, 0), (3, 1, 0), (4, 0, 2), (None, 0, None)])
 def test_attention_gradients_against_differences(window, sinks, look):
     g = torch.Generator().manual_seed(1)
