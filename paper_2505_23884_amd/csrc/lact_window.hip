@@ -707,14 +707,20 @@ constexpr int sharers(bool bf16, int DP) { return DP <= 64 ? 4 : bf16 || DP <= 1
 
 // Where workgroups of 128 of n rows would leave CUs idle, workgroups of 32 whose
 // waves take turns at the other side's tiles and join their sums: more CUs and
-// a shorter chain of tiles. Their LDS holds one workgroup a CU, so the limit
-// is the number of workgroups that still run at once. Training, this and
-// workgroups of 128: [1, 2, 256, 64] fp32, window 64: 43 and 94 us;
-// [1, 8 / 4, 2048, 64] fp32, window 512 (128 workgroups): 165 and 260;
-// [1, 8 / 4, 2048, 128] bf16 (the same with two sharers): 118 and 96.
+// a shorter chain of tiles. Their LDS holds one workgroup a CU, so past 64
+// times four of them they come in rounds, each a W-th as long; fp32's longer
+// products forgive more of these. This and workgroups of 128, in us:
+//   training  [1, 2, 256, 64] fp32, window 64 (4 workgroups of 128)      43   94
+//             [1, 8 / 4, 2048, 64] fp32, window 512 (128)               165  260
+//             [1, 12 / 4, 2048, 64] fp32, window 512 (192)              238  262
+//             [3, 4 / 2, 1264, 80] fp32, window 348 (120)               309  346
+//             [1, 8 / 4, 2048, 128] bf16, window 512 (128)              118   96
+//   forward   [1, 8 / 4, 1536, 128] bf16, window 512 (96)                37   25
+//             [1, 12 / 4, 2048, 64] bf16, window 512 (192)               27   18
+//             [1, 8 / 4, 2048, 64] bf16, window 512 (128)                19   19
 bool few_blocks(const WindowArgs& a, bool bf16, int n) {
   const int W = sharers(bf16, a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256);
-  return W > 1 && (int64_t)a.B * a.H * cdiv(n, 128) < 64 * W;
+  return W > 1 && (int64_t)a.B * a.H * cdiv(n, 128) < (bf16 ? 32 : 64) * W;
 }
 
 template <typename T, int DP>
