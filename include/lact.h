@@ -563,7 +563,7 @@ typedef struct lact_view {
  */
 typedef struct lact_rope_desc {
   int32_t B, H, Hkv, d;
-  int64_t n;                /* tokens of a sequence; B * n < 2^31               */
+  int64_t n;                /* tokens of a sequence; B * n <= 2^25              */
   int64_t pos0;             /* |pos0| <= 2^40                                   */
   int32_t rot;
   int32_t interleaved;      /* 0 or 1                                           */
@@ -607,9 +607,10 @@ int lact_qk_norm_rope_backward(const lact_rope_desc* desc, const lact_view* q, c
  * cotangent dout of o, the cotangents dq, dk, dv (every element written; zero
  * at padding). Sums over a group's heads are in a fixed order.
  *
- * d <= 256; n_q, n_kv, |q_start| and q_start + n_q <= 2^29; scale finite and
- * > 0 (1e-12 to 1e12, else LACT_EUNSUPPORTED). Weights and their cotangents are rounded to bf16 for the second
- * products with bf16 I/O; scores, maxima, sums and accumulators are fp32.
+ * d <= 256; n_q, n_kv, |q_start| and q_start + n_q <= 2^29; B * H times n_q,
+ * or n_kv, <= 2^30; scale finite and > 0 (1e-12 to 1e12, else
+ * LACT_EUNSUPPORTED). Weights and their cotangents are rounded to bf16 for the
+ * second products with bf16 I/O; scores, maxima, sums and accumulators are fp32.
  */
 typedef struct lact_attn_desc {
   int32_t B, H, Hkv, d;
@@ -645,13 +646,14 @@ int lact_window_attention_backward(const lact_attn_desc* desc, const lact_view* 
  * lact_paged_attention attends with the causal window and sinks of
  * lact_window_attention (lookahead 0). Rows of no sequence (before cu_new[0],
  * from cu_new[B] on) are left as they were. Pages that several sequences share
- * are read by all; if an append of one call writes a slot twice, either value
- * may stay.
+ * are read by all; if an append of one call writes a slot twice, any 16 bytes of
+ * it may be of either.
  *
  *   q, o    [n_new][H][d], k, v [n_new][Hkv][d]   views (batch is not used)
  *   table   int32 [B][max_pages]; lens int32 [B]; cu_new int32 [B + 1]          in
  *
- * d <= 256; n_new * H < 2^31; max_pages * page <= 2^29; scale > 0. For
+ * d <= 256; n_new * H <= 2^28, times d <= 2^33 (Hkv for the append);
+ * max_pages * page <= 2^29; scale finite and > 0. For
  * lact_paged_append H, window, sinks and scale are not used.
  */
 typedef struct lact_paged_desc {

@@ -12,7 +12,12 @@ namespace {
 constexpr size_t kWsAlign = 256;
 size_t ws_round(size_t x) { return (x + kWsAlign - 1) / kWsAlign * kWsAlign; }
 constexpr int64_t kMaxTokenStride = (int64_t)1 << 22;   // 64 rows stay within a 31-bit buffer range
-constexpr int64_t kMaxGrid = (int64_t)0x7fffffff;
+constexpr int64_t kMaxInt = (int64_t)0x7fffffff;
+// A launch holds fewer than 2^32 threads in a direction.
+constexpr int64_t kRopeRows = (int64_t)1 << 25;       // tokens of a norm and rotation, four a workgroup of 256 at least
+constexpr int64_t kAttnRows = (int64_t)1 << 30;       // queries, or keys, over the heads, 128 a workgroup of 512 at most
+constexpr int64_t kPagedRows = (int64_t)1 << 28;      // new tokens times heads, 32 a workgroup of 256
+constexpr int64_t kPagedElements = (int64_t)1 << 33;  // four a thread of the append
 
 bool finite(float x) { return x - x == 0.0f; }
 
@@ -69,7 +74,7 @@ int check_rope(const lact_rope_desc* s) {
   if (!(s->eps >= 0.0f) || !finite(s->eps)) return LACT_EINVAL;
   if (!s->interleaved && s->rot % 8) return LACT_EUNSUPPORTED;
   const int64_t far = (int64_t)1 << 40;
-  if (s->n > kMaxGrid || s->B * s->n > kMaxGrid || s->pos0 > far || s->pos0 < -far) return LACT_EUNSUPPORTED;
+  if (s->n > kRopeRows || s->B * s->n > kRopeRows || s->pos0 > far || s->pos0 < -far) return LACT_EUNSUPPORTED;
   return LACT_OK;
 }
 
@@ -111,9 +116,7 @@ int check_attn(const lact_attn_desc* s) {
   if (s->n_q > kAttnTokens || s->n_kv > kAttnTokens || s->q_start > kAttnTokens || s->q_start < -kAttnTokens ||
       s->q_start + s->n_q > kAttnTokens)
     return LACT_EUNSUPPORTED;
-  // the largest grids: tiles of 32 queries; tiles of keys in parts
-  if ((int64_t)s->B * s->H * (s->n_q / 32 + 1) > kMaxGrid || (int64_t)s->B * s->H * (s->n_kv / 128 + 1) * 128 > kMaxGrid)
-    return LACT_EUNSUPPORTED;
+  if ((int64_t)s->B * s->H * std::max(s->n_q, s->n_kv) > kAttnRows) return LACT_EUNSUPPORTED;
   return LACT_OK;
 }
 
@@ -153,8 +156,9 @@ int check_paged(const lact_paged_desc* s, bool attend) {
   LACT_TRY(check_heads(s->B, attend ? s->H : s->Hkv, s->Hkv, s->d, s->io_dtype, 256));
   if (s->n_new < 0 || s->pages < 0 || s->page < 1 || s->max_pages < 0) return LACT_EINVAL;
   if (attend && (s->window < -1 || s->sinks < 0 || !(s->scale > 0.0f) || !finite(s->scale))) return LACT_EINVAL;
-  if (s->pages > kMaxGrid || (int64_t)s->max_pages * s->page > kAttnTokens || s->page > kAttnTokens ||
-      s->n_new > kAttnTokens || s->n_new * (attend ? s->H : s->Hkv) > kMaxGrid || (attend && s->Hkv > 65535))
+  const int64_t rows = std::min(s->n_new, kAttnTokens) * (attend ? s->H : s->Hkv);
+  if (s->pages > kMaxInt || (int64_t)s->max_pages * s->page > kAttnTokens || s->page > kAttnTokens ||
+      s->n_new > kAttnTokens || rows > kPagedRows || rows * s->d > kPagedElements)
     return LACT_EUNSUPPORTED;
   return LACT_OK;
 }

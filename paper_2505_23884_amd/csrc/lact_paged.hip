@@ -43,23 +43,46 @@ __device__ __forceinline__ int seq_len(const Args& a, int b) {
   return clampi(a.len[b], 0, a.max_pages * a.page);
 }
 
-// Row tile `t`: sequence b starts at tile cu[b] G / R + b (rounded down, so
-// that each has room for its last partial tile); some tiles are empty.
+// Row tile `t` of R rows. Up to 64 sequences stand a lane each, in the order of
+// the keys they see, most first: what is left for the end, or comes as a
+// second workgroup to a CU, is short. More than that stand in their own order,
+// sequence b from tile cu[b] G / R + b on (rounded down, so that each has room
+// for its last partial tile). Tiles past the last one are empty.
 __device__ __forceinline__ bool find_rows(const PagedArgs& a, int t, int R, Seq& s, int& r0) {
-  int lo = 0, hi = a.B - 1;
-  auto first = [&](int b) { return (int)((int64_t)clampi(a.cu[b], 0, a.T) * a.G / R) + b; };
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (first(mid) <= t) lo = mid;
-    else hi = mid - 1;
+  int count, k;
+  if (a.B <= 64) {
+    const int lane = threadIdx.x & 63, b = min(lane, a.B - 1);
+    const int t0 = clampi(a.cu[b], 0, a.T), t1 = a.cu[b + 1], len = seq_len(a, b);
+    const int n = lane < a.B ? clampi(t1, t0, a.T) - t0 : 0, tiles = (int)(((int64_t)n * a.G + R - 1) / R);
+    const int keys = min(len, a.win);
+    int start = 0;
+    for (int j = 0; j < a.B; ++j) {
+      const int kj = __builtin_amdgcn_readlane(keys, j), nj = __builtin_amdgcn_readlane(tiles, j);
+      start += (kj > keys) | ((kj == keys) & (j < lane)) ? nj : 0;
+    }
+    const uint64_t mine = __ballot(t >= start && t - start < tiles);
+    if (!mine) return false;
+    s.b = __builtin_ctzll(mine);
+    s.t0 = __builtin_amdgcn_readlane(t0, s.b);
+    s.len = __builtin_amdgcn_readlane(len, s.b);
+    count = __builtin_amdgcn_readlane(n, s.b);
+    k = t - __builtin_amdgcn_readlane(start, s.b);
+  } else {
+    int lo = 0, hi = a.B - 1;
+    auto first = [&](int b) { return (int)((int64_t)clampi(a.cu[b], 0, a.T) * a.G / R) + b; };
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first(mid) <= t) lo = mid;
+      else hi = mid - 1;
+    }
+    s.b = lo;
+    s.t0 = clampi(a.cu[lo], 0, a.T);
+    s.len = seq_len(a, lo);
+    count = clampi(a.cu[lo + 1], s.t0, a.T) - s.t0;
+    k = t - first(lo);
   }
-  s.b = lo;
-  s.t0 = clampi(a.cu[lo], 0, a.T);
-  const int count = clampi(a.cu[lo + 1], s.t0, a.T) - s.t0;
   s.rows = count * a.G;
-  s.len = seq_len(a, lo);
   s.p0 = s.len - count;
-  const int k = t - first(lo);
   if (k < 0 || (int64_t)k * R >= s.rows) return false;
   r0 = k * R;
   return true;
@@ -184,8 +207,8 @@ __global__ __launch_bounds__(64 * kWaves, OCC) void k_paged_wide(const PagedArgs
   __shared__ int found;
   Seq s;
   int r0;
-  if (!find_rows(a, blockIdx.x, 32 * kWaves, s, r0)) return;
-  const int hk = blockIdx.y, split = blockIdx.z;
+  if (!find_rows(a, blockIdx.x / a.Hkv, 32 * kWaves, s, r0)) return;
+  const int hk = blockIdx.x % a.Hkv, split = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const RowOf row(a, s, hk, r0 + 32 * wave + (lane & 31));
   const int rl = min(r0 + 32 * kWaves, s.rows) - 1, wr = r0 + 32 * wave, wl = min(wr + 32, s.rows) - 1;
@@ -267,8 +290,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_paged_narrow(const PagedArgs a)
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kWaves * WAVE];
   Seq s;
   int r0;
-  if (!find_rows(a, blockIdx.x, 32, s, r0)) return;
-  const int hk = blockIdx.y, split = blockIdx.z;
+  if (!find_rows(a, blockIdx.x / a.Hkv, 32, s, r0)) return;
+  const int hk = blockIdx.x % a.Hkv, split = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const RowOf row(a, s, hk, r0 + (lane & 31));
   const int rl = min(r0 + 32, s.rows) - 1;
@@ -439,7 +462,7 @@ int row_tiles(const PagedArgs& a, bool wide) { return (int)((int64_t)a.T * a.G /
 
 template <typename T, int DP>
 hipError_t run(const PagedArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)row_tiles(a, a.wide), (unsigned)a.Hkv, (unsigned)a.splits);
+  const dim3 grid((unsigned)(row_tiles(a, a.wide) * a.Hkv), (unsigned)a.splits);
   if constexpr (sizeof(T) == 4 && DP == 256) {
     k_paged_wide<T, DP, 32, 1><<<grid, 64 * kWaves, 0, s>>>(a);   // a wave's own tile would not fit
   } else {

@@ -789,6 +789,8 @@ DkvPlan window_dkv_plan(const WindowArgs& a, bool bf16) {
   if (reach < n_q) {
     p.st = cdiv(std::min(a.sinks, a.n_kv), p.kb);
     parts(std::max(256, cdiv(reach, 256) * 64), &p.np_s, &p.ch_s);
+    const int64_t enough = 2048 / std::max<int64_t>((int64_t)a.B * a.Hkv * p.st, 1);   // many sink tiles need no parts
+    if (p.np_s > enough) parts(cdiv(n_q, std::max<int64_t>(enough, 1)), &p.np_s, &p.ch_s);
   }
   while (tiles * p.gs < (few ? 512 : 256) && p.gs < a.G) {
     int f = 2;

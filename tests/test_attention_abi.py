@@ -164,6 +164,24 @@ def test_paged_arguments_are_refused():
     assert paged({"n_new": 0}, append=True, k=view(0), v=view(0)) == 0
 
 
+def test_calls_past_the_largest_launch_are_refused():
+    assert rope({"B": 1, "n": (1 << 25) + 1}) == EUNSUPPORTED
+    assert rope({"B": 1 << 10, "n": (1 << 15) + 1}) == EUNSUPPORTED
+    for back in (False, True):
+        assert attn({"B": 1 << 10, "n_q": 1 << 19}, back, ws=1 << 50) == EUNSUPPORTED
+        assert attn({"B": 1 << 10, "n_kv": 1 << 19}, back, ws=1 << 50) == EUNSUPPORTED
+    assert paged({"n_new": (1 << 26) + 1}, ws=1 << 50) == EUNSUPPORTED
+    assert paged({"n_new": (1 << 25) + 1}, append=True) == EUNSUPPORTED       # times 2 heads of 128
+
+
+def test_many_sink_tiles_stay_within_a_workspace():
+    # every key a sink: no tile is cut into parts, so the workspace holds rows only
+    L = P.lib()
+    a = dict(ATTN, B=1, n_q=1 << 18, n_kv=1 << 18, window=64, sinks=1 << 18)
+    n = L.lact_window_attention_backward_workspace_bytes(LactAttnDesc(**a), None)
+    assert 0 < n < 2 * 4 * (4 << 18) + (1 << 20)
+
+
 def test_workspaces_grow_with_the_call():
     L = P.lib()
     f = lambda **k: L.lact_window_attention_backward_workspace_bytes(LactAttnDesc(**dict(ATTN, **k)), None)
