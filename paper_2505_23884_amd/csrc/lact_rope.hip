@@ -10,7 +10,9 @@
 // keeps 10^-11 of a turn) reduced to a fraction of a turn, into LDS, and used
 // by all heads. A group of lanes owns a vector; a lane holds two pieces of GE
 // elements that rotate into each other, so nothing is exchanged but the sum of
-// squares.
+// squares. [4, 8191, 16 + 4, 128] bf16: 101 us for 336 MB (3.3 TB/s, its angles
+// and its launch included), the reverse 122 us for 503 MB (4.1 TB/s); a token
+// of 64 sequences 4.2 us.
 #include <algorithm>
 
 #include "lact_attn.h"
