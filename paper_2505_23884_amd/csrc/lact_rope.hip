@@ -124,10 +124,10 @@ struct Angles {
 
 // cos and sin of tokens t0 .. of the step into cs[token][rot / 2]
 __device__ __forceinline__ void angles(const RopeArgs& a, f32x2* cs, int64_t t0, int count) {
-  const int half = a.rot / 2;
-  for (int x = threadIdx.x; x < count * half; x += kRopeThreads) {
-    const int64_t t = t0 + x / half;
-    const double pos = a.pos ? (double)a.pos[t] : (double)(a.pos0 + t % a.n);
+  const uint32_t half = (uint32_t)a.rot / 2;
+  for (uint32_t x = threadIdx.x; x < count * half; x += kRopeThreads) {
+    const uint32_t t = (uint32_t)t0 + x / half;   // B n <= 2^25
+    const double pos = a.pos ? (double)a.pos[t] : (double)(a.pos0 + t % (uint32_t)a.n);
     const double turns = pos * (a.freq[x % half] * 0.15915494309189533577);   // 1 / (2 pi)
     const float part = 2.0f * (float)(turns - rint(turns));
     float s, c;
@@ -156,7 +156,7 @@ __device__ __forceinline__ float group_add(float v, int G) {
 struct RopeToken {
   int64_t b, l;
   __device__ __forceinline__ RopeToken(const RopeArgs& a, int64_t t) {
-    const uint32_t bi = (uint32_t)t / (uint32_t)a.n;   // B n < 2^31
+    const uint32_t bi = (uint32_t)t / (uint32_t)a.n;   // B n <= 2^25
     b = bi;
     l = (uint32_t)t - bi * (uint32_t)a.n;
   }
@@ -193,21 +193,21 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(const RopeArgs a, int G) 
   const int64_t tokens = (int64_t)a.B * a.n, t0 = (int64_t)(blk / hs) * a.tb;
   const int count = (int)(tokens - t0 < a.tb ? tokens - t0 : a.tb);
   const int part = blk % hs, h0 = H * part / hs, h1 = H * (part + 1) / hs;
-  angles(a, cs, t0, count);
-  __syncthreads();
   const int lg = threadIdx.x & (G - 1), NG = kRopeThreads / G, gi = threadIdx.x / G;
   const int ti = gi & (a.tb - 1), step = NG / a.tb;
-  if (ti >= count) return;
   const Pieces<GE> pc(a, lg);
-  const RopeToken at(a, t0 + ti);
-  Angles<GE> an;
-  an.load(a, pc, cs + ti * (a.rot / 2));
-  float w[2][GE];
-  if (!a.per_head) load_weights<GE>(w, pc, a.w[which]);
+  const RopeToken at(a, t0 + min(ti, count - 1));
   const AttnView &xv = a.x[which], &yv = a.y[which];
   int h = h0 + gi / a.tb;
-  Raw<T, GE> next[2];   // the loads run one vector ahead
+  Raw<T, GE> next[2];   // the loads run one vector ahead, the first beside the angles
   if (h < h1) load_pieces<T, GE>(next, pc, at.row<const T>(xv, h));
+  float w[2][GE];
+  if (!a.per_head) load_weights<GE>(w, pc, a.w[which]);
+  angles(a, cs, t0, count);
+  __syncthreads();
+  if (ti >= count) return;
+  Angles<GE> an;
+  an.load(a, pc, cs + ti * (a.rot / 2));
   for (; h < h1; h += step) {
     float x[2][GE];
     next[0].get(x[0]);
@@ -357,20 +357,28 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope_bwd(const RopeArgs a, int
 }
 
 // dw[i] = the sum of the workgroups' partials in a fixed order: 16 columns a
-// workgroup, 64 rows of partials a time.
-__global__ __launch_bounds__(1024) void k_rope_dw_sum(const float* part, float* dw, int nblk, int n) {
+// workgroup, 64 rows of partials a time; q's weights, then k's.
+struct RopeSum {
+  const float* part[2];
+  float* dw[2];
+  int nblk[2], n[2], groups;   // workgroups of q's weights
+};
+__global__ __launch_bounds__(1024) void k_rope_dw_sum(const RopeSum a) {
   __shared__ float red[64][16];
-  const int x = threadIdx.x & 15, r = threadIdx.x >> 4, col = blockIdx.x * 16 + x;
+  const int which = (int)blockIdx.x >= a.groups, n = a.n[which], nblk = a.nblk[which];
+  const int x = threadIdx.x & 15, r = threadIdx.x >> 4, col = (blockIdx.x - (which ? a.groups : 0)) * 16 + x;
+  const float* part = a.part[which] + col;
   float s = 0.0f;
   if (col < n)
-    for (int i = r; i < nblk; i += 64) s += part[(int64_t)i * n + col];
+#pragma unroll 4
+    for (int i = r; i < nblk; i += 64) s += part[(int64_t)i * n];
   red[r][x] = s;
   __syncthreads();
   for (int o = 32; o > 0; o >>= 1) {
     if (r < o) red[r][x] += red[r + o][x];
     __syncthreads();
   }
-  if (r == 0 && col < n) dw[col] = red[0][x];
+  if (r == 0 && col < n) a.dw[which][col] = red[0][x];
 }
 
 // Elements of a piece: 16 bytes, or 4 elements where half the rotated ones
@@ -435,12 +443,20 @@ hipError_t launch_rope_bwd(const RopeArgs& a, bool bf16, hipStream_t s) {
     else if (ge == 8) bwd_one<__bf16, 8>(a, G, s);
     else bwd_one<__bf16, 4>(a, G, s);
   }
+  RopeSum sum{};
   const float* part = a.part;
+  int grid = 0;
   for (int w = 0; w < 2; ++w) {
     const int n = (a.per_head ? a.H[w] : 1) * a.d;
-    if (a.dw[w]) k_rope_dw_sum<<<(n + 15) / 16, 1024, 0, s>>>(part, a.dw[w], a.nblk[w], n);
+    sum.part[w] = part;
+    sum.dw[w] = a.dw[w];
+    sum.nblk[w] = a.nblk[w];
+    sum.n[w] = n;
     part += (size_t)a.nblk[w] * n;
+    if (a.dw[w]) grid += (n + 15) / 16;
+    if (w == 0) sum.groups = grid;
   }
+  if (grid) k_rope_dw_sum<<<grid, 1024, 0, s>>>(sum);
   return hipGetLastError();
 }
 
