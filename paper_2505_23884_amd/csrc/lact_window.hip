@@ -49,7 +49,10 @@ __device__ __forceinline__ int length_of(const WindowArgs& a, int b) {
   return a.len ? min(max(a.len[b], 0), a.n_kv) : a.n_kv;
 }
 
-template <typename T, int DP> constexpr int key_tile() { return sizeof(T) == 2 && DP <= 128 ? 64 : 32; }
+// Keys a tile: those of a lone wave (of NW = 1) leave room for three more waves' at DP = 128.
+template <typename T, int DP, int NW> constexpr int key_tile() {
+  return sizeof(T) == 2 && DP <= (NW > 1 ? 128 : 64) ? 64 : 32;
+}
 
 // ------------------------------------------------------------------ forward
 // A workgroup of NW waves owns 32 NW queries of one head, a wave 32 of them;
@@ -69,7 +72,7 @@ template <typename T, int DP> constexpr int key_tile() { return sizeof(T) == 2 &
 // weights) was slower by 4 %, a higher priority for matrix work changed nothing.
 template <typename T, int DP, int NW, int KS, int OCC>
 __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_fwd(const WindowArgs a) {
-  constexpr int KT = key_tile<T, DP>(), QB = 32 * NW, NT = 64 * NW;
+  constexpr int KT = key_tile<T, DP, NW>(), QB = 32 * NW, NT = 64 * NW;
   using L = Tile<T, DP>;
   constexpr int BYTES = KT * L::PITCH;
   __shared__ __attribute__((aligned(1024))) uint8_t smem_[KS * 4 * BYTES];
@@ -198,7 +201,7 @@ __device__ __forceinline__ float dot_half(const u32x4 (&x)[N], const u32x4 (&y)[
 template <typename T, int DP, int NW, int KS, int OCC>
 __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwdArgs g) {
   const WindowArgs& a = g.f;
-  constexpr int KT = key_tile<T, DP>(), QB = 32 * NW, NT = 64 * NW;
+  constexpr int KT = key_tile<T, DP, NW>(), QB = 32 * NW, NT = 64 * NW;
   using L = Tile<T, DP>;
   constexpr int BYTES = KT * L::PITCH;
   __shared__ __attribute__((aligned(1024))) uint8_t smem_[KS * 4 * BYTES];
@@ -718,7 +721,7 @@ int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // Waves that may share 32 queries (or keys): as many as have room in LDS for
 // tiles of their own.
-constexpr int sharers(bool bf16, int DP) { return DP <= 64 ? 4 : bf16 || DP <= 128 ? 2 : 1; }
+constexpr int sharers(bool bf16, int DP) { return DP <= (bf16 ? 128 : 64) ? 4 : bf16 || DP <= 128 ? 2 : 1; }
 
 // Where workgroups of 128 of n rows would leave CUs idle, workgroups of 32 whose
 // waves take turns at the other side's tiles and join their sums: more CUs and
@@ -729,13 +732,13 @@ constexpr int sharers(bool bf16, int DP) { return DP <= 64 ? 4 : bf16 || DP <= 1
 //             [1, 8 / 4, 2048, 64] fp32, window 512 (128)               165  260
 //             [1, 12 / 4, 2048, 64] fp32, window 512 (192)              238  262
 //             [3, 4 / 2, 1264, 80] fp32, window 348 (120)               309  346
-//             [1, 8 / 4, 2048, 128] bf16, window 512 (128)              118   96
-//   forward   [1, 8 / 4, 1536, 128] bf16, window 512 (96)                37   25
-//             [1, 12 / 4, 2048, 64] bf16, window 512 (192)               27   18
+//   forward   [1, 8 / 4, 1024, 128] bf16, window 512 (64)                16   25
+//             [1, 8 / 4, 1536, 128] bf16, window 512 (96)                27   25
 //             [1, 8 / 4, 2048, 64] bf16, window 512 (128)                19   19
+//             [1, 12 / 4, 2048, 64] bf16, window 512 (192)               27   18
 bool few_blocks(const WindowArgs& a, bool bf16, int n) {
   const int W = sharers(bf16, a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256);
-  return W > 1 && (int64_t)a.B * a.H * cdiv(n, 128) < (bf16 ? 32 : 64) * W;
+  return W > 1 && (int64_t)a.B * a.H * cdiv(n, 128) < (bf16 ? 24 : 64) * W;
 }
 
 template <typename T, int DP>
