@@ -526,8 +526,9 @@ int lact_rmsnorm_out_backward(const lact_desc* desc, const void* o, const float*
  * consecutive; the data and every stride of an extent over 1 are multiples of
  * 16 bytes (else LACT_EALIGN), strides are >= 0 and a token's at most 2^22
  * (else LACT_EINVAL, LACT_EUNSUPPORTED). An input may repeat itself (stride
- * 0); an output's vectors must not overlap (a stride of 0, or a token stride
- * below d, over an extent over 1: LACT_EINVAL). Outputs must not alias inputs
+ * 0); an output's vectors must not overlap (each stride over an extent over 1
+ * is d at least and steps over all that narrower ones reach, else
+ * LACT_EINVAL). Outputs must not alias inputs
  * or each other. A view of no vectors may have a NULL pointer.
  */
 typedef struct lact_view {

@@ -873,7 +873,18 @@ def _call(name, dev, stream, torch, *args):
         _raise(rc)
 
 
-def _workspace(name, desc, workspace, like, torch):
+def _new(like, shape, stream, torch, dtype=None):
+    """An uninitialised tensor of like's device, from the memory of the stream
+    that works on it."""
+    if stream is None:
+        return like.new_empty(shape) if dtype is None else like.new_empty(shape, dtype=dtype)
+    dev = like.device
+    s = torch.cuda.ExternalStream(stream, device=dev) if stream else torch.cuda.default_stream(dev)
+    with torch.cuda.stream(s):
+        return like.new_empty(shape, dtype=dtype or like.dtype)
+
+
+def _workspace(name, desc, workspace, like, stream, torch):
     """(tensor that stays alive, address, bytes) of the caller's workspace, or of
     a new one of the size that the call needs (0 too where the descriptor is
     refused, which the call itself then says)."""
@@ -881,7 +892,7 @@ def _workspace(name, desc, workspace, like, torch):
         n = _fn(name)(desc, None)
         if not n:
             return None, None, 0
-        workspace = like.new_empty(n, dtype=torch.uint8)
+        workspace = _new(like, n, stream, torch, torch.uint8)
         return workspace, workspace.data_ptr(), n
     if workspace.device != like.device or not workspace.is_contiguous():
         raise LactError(-1, f"workspace must be a contiguous tensor on {like.device}")
@@ -925,7 +936,7 @@ def qk_norm_rope(q, k, wq=None, wk=None, inv_freq=None, *, positions=None, pos0=
     (two tensors of those shapes, any strides) when it is given."""
     import torch
     (B, n, H, Hkv, d), dt, dev, args = _rope_args(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved, torch)
-    qn, kn = (q.new_empty((B, H, n, d)), q.new_empty((B, Hkv, n, d))) if out is None else out
+    qn, kn = (_new(q, (B, H, n, d), stream, torch), _new(q, (B, Hkv, n, d), stream, torch)) if out is None else out
     _call("lact_qk_norm_rope", dev, stream, torch, *args, _view(qn, "qn", (B, H, n, d), dt, dev),
           _view(kn, "kn", (B, Hkv, n, d), dt, dev))
     return qn, kn
@@ -940,8 +951,8 @@ def qk_norm_rope_backward(q, k, dqn, dkn, wq=None, wk=None, inv_freq=None, *, po
     import torch
     (B, n, H, Hkv, d), dt, dev, args = _rope_args(q, k, wq, wk, inv_freq, positions, pos0, eps, interleaved, torch)
     if out is None:
-        dw = [torch.empty_like(w) if w is not None and with_dweight else None for w in (wq, wk)]
-        out = (q.new_empty((B, n, H, d)), q.new_empty((B, n, Hkv, d)), *dw)
+        dw = [_new(w, w.shape, stream, torch) if w is not None and with_dweight else None for w in (wq, wk)]
+        out = (_new(q, (B, n, H, d), stream, torch), _new(q, (B, n, Hkv, d), stream, torch), *dw)
     dq, dk, dwq, dwk = out
     dwp = []
     for t, w, name in ((dwq, wq, "dwq"), (dwk, wk, "dwk")):
@@ -950,7 +961,7 @@ def qk_norm_rope_backward(q, k, dqn, dkn, wq=None, wk=None, inv_freq=None, *, po
         dwp.append(None if t is None else _aux(t, name, w.shape, torch.float32, dev))
     wp, nb = None, 0
     if dwq is not None or dwk is not None:
-        workspace, wp, nb = _workspace("lact_qk_norm_rope_backward_workspace_bytes", args[0], workspace, q, torch)
+        workspace, wp, nb = _workspace("lact_qk_norm_rope_backward_workspace_bytes", args[0], workspace, q, stream, torch)
     _call("lact_qk_norm_rope_backward", dev, stream, torch, *args, _view(dqn, "dqn", (B, H, n, d), dt, dev),
           _view(dkn, "dkn", (B, Hkv, n, d), dt, dev), _view_t(dq, "dq", (B, n, H, d), dt, dev),
           _view_t(dk, "dk", (B, n, Hkv, d), dt, dev), *dwp, wp, nb)
@@ -987,8 +998,8 @@ def window_attention(q, k, v, *, window=None, sinks=0, lookahead=0, lengths=None
     import torch
     sq, _, dt, dev, args, lp = _attn_args(q, k, v, window, sinks, lookahead, lengths, scale, q_start, torch)
     if out is None:
-        o = q.new_empty(sq)
-        lse = q.new_empty(sq[:3], dtype=torch.float32) if with_lse else None
+        o = _new(q, sq, stream, torch)
+        lse = _new(q, sq[:3], stream, torch, torch.float32) if with_lse else None
     else:
         o, lse = out if with_lse else (out, None)
     _call("lact_window_attention", dev, stream, torch, *args, lp, _view(o, "o", sq, dt, dev),
@@ -1005,8 +1016,8 @@ def window_attention_backward(q, k, v, o, lse, dout, *, window=None, sinks=0, lo
     sq, sk, dt, dev, args, lp = _attn_args(q, k, v, window, sinks, lookahead, lengths, scale, q_start, torch)
     if lse is None:
         raise LactError(-1, "lse of the forward is needed")
-    dq, dk, dv = (q.new_empty(sq), q.new_empty(sk), q.new_empty(sk)) if out is None else out
-    workspace, wp, nb = _workspace("lact_window_attention_backward_workspace_bytes", args[0], workspace, q, torch)
+    dq, dk, dv = tuple(_new(q, x, stream, torch) for x in (sq, sk, sk)) if out is None else out
+    workspace, wp, nb = _workspace("lact_window_attention_backward_workspace_bytes", args[0], workspace, q, stream, torch)
     _call("lact_window_attention_backward", dev, stream, torch, *args, _view(o, "o", sq, dt, dev),
           _aux(lse, "lse", sq[:3], torch.float32, dev), _view(dout, "dout", sq, dt, dev), lp,
           _view(dq, "dq", sq, dt, dev), _view(dk, "dk", sk, dt, dev), _view(dv, "dv", sk, dt, dev), wp, nb)
@@ -1055,8 +1066,8 @@ def paged_attention(q, k_cache, v_cache, table, lens, cu_new, *, window=None, si
     d, dt, dev, desc, tail = _paged_args(q, H, k_cache, v_cache, table, lens, cu_new, window, sinks, scale, torch)
     s = (T, H, d)
     qv = _view_n(q, "q", s, dt, dev)
-    o = q.new_empty(s) if out is None else out
-    workspace, wp, nb = _workspace("lact_paged_attention_workspace_bytes", desc, workspace, q, torch)
+    o = _new(q, s, stream, torch) if out is None else out
+    workspace, wp, nb = _workspace("lact_paged_attention_workspace_bytes", desc, workspace, q, stream, torch)
     _call("lact_paged_attention", dev, stream, torch, desc, qv, *tail, _view_n(o, "o", s, dt, dev), wp, nb)
     return o
 

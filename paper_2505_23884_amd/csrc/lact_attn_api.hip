@@ -30,7 +30,17 @@ int check_view(const lact_view* v, int64_t batch, int64_t head, int64_t token, i
   const int64_t ext[3] = {batch, head, token}, st[3] = {v->batch, v->head, v->token};
   for (int i = 0; i < 3; ++i) {
     if (ext[i] == 1) continue;
-    if (st[i] < 0 || (out && st[i] < d)) return LACT_EINVAL;
+    if (st[i] < 0) return LACT_EINVAL;
+  }
+  if (out) {   // from the narrowest stride on, each steps over what lies within it
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int x, int y) { return st[x] < st[y]; });
+    __int128 span = d;
+    for (int i : order) {
+      if (ext[i] == 1) continue;
+      if (st[i] < span) return LACT_EINVAL;
+      span += (__int128)(ext[i] - 1) * st[i];
+    }
   }
   if ((uintptr_t)v->data & 15) return LACT_EALIGN;
   for (int i = 0; i < 3; ++i)

@@ -120,6 +120,10 @@ def test_window_arguments_are_refused():
         assert attn(back=back, lengths=0x1002) == EALIGN
         assert attn(back=back, lse=0x1001) == EALIGN
     assert attn(o=view(token=0)) == EINVAL
+    for head_, token in ((128, 256), (128, 128), (1 << 12, 128), (128, 504)):      # 4 heads of 33 tokens, over each other
+        assert attn(o=view(head=head_, token=token)) == EINVAL
+    assert attn(o=view(batch=33 * 128 + 64, head=33 * 128)) == EINVAL                  # a batch within the heads
+    assert attn(o=view(batch=1 << 62, head=1 << 62)) == EINVAL
     for name in ("dq", "dk", "dv"):
         assert attn(back=True, **{name: view(head=64)}) == EINVAL
     assert attn(back=True, dout=view(0)) == EINVAL

@@ -494,3 +494,44 @@ def test_an_infinite_key_that_weighs_nothing_stays_out_of_the_others(dtype):
         check("dk", dk[0, h][without], r["dk"], t["dk"])
         check("dv", dv[0, h][without], r["dv"], t["dv"])
         assert bool((dv[0, h, 30] == 0).all()) and bool(torch.isnan(dq[0, h, :, 5]).all())
+
+
+def test_work_on_a_given_stream_beside_the_current_one():
+    # outputs and workspaces come from the given stream's memory, so that work of
+    # the current stream, still queued, neither overwrites them nor is overwritten
+    x = layer_inputs(13, n=400)
+    want = layer(*x, **OPT)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    junk = []
+    for _ in range(4):
+        s = side.cuda_stream
+        q, k, v, wq, wk, inv, do = x
+        big = torch.full((1 << 22,), 3.0, device=DEV)
+        del big                                              # its memory is free for the current stream only
+        qn, kn = P.qk_norm_rope(q, k, wq, wk, inv, stream=s)
+        vt = v.transpose(1, 2)
+        o, lse = P.window_attention(qn, kn, vt, with_lse=True, stream=s, **OPT)
+        dqn, dkn, dv = P.window_attention_backward(qn, kn, vt, o, lse, do, stream=s, **OPT)
+        junk.append(torch.full((1 << 20,), float("nan"), device=DEV))
+        dq, dk, dwq, dwk = P.qk_norm_rope_backward(q, k, dqn, dkn, wq, wk, inv, stream=s)
+        side.synchronize()
+        for a, b in zip((o, dq, dk, dv, dwq, dwk), want):
+            assert torch.equal(a, b)
+    torch.cuda.synchronize()
+
+
+def test_many_sequences_and_mixed_lengths():
+    # more sequences than a wave has lanes, and 64 of them: the two ways to find a row's sequence
+    for B in (63, 64, 65, 130):
+        lens = [1 + (37 * b) % 200 for b in range(B)]
+        new = [min(1 + (b % 5) * (b % 3), n) if b % 7 else 0 for b, n in enumerate(lens)]
+        q, kc, vc, table, ln, cu_new, K, V, cu = paged_setup(lens, new, 4, 2, 64, 16, BF, seed=B)
+        o = P.paged_attention(q, kc, vc, table, ln, cu_new, window=70, sinks=1)
+        torch.cuda.synchronize()
+        for b in range(0, B, 9):
+            if not new[b]:
+                continue
+            rows = slice(cu[b], cu[b] + new[b])
+            want, tol = attention(q[rows].transpose(0, 1)[None].cpu(), K[b][:, :, :lens[b]], V[b][:, :, :lens[b]], window=70, sinks=1)
+            check(f"{B} {b}", o[rows].transpose(0, 1)[None], want["o"], tol["o"])
