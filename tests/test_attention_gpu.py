@@ -14,7 +14,7 @@ DEV = "cuda"
 
 def rnd(seed, *shape, dtype=torch.bfloat16, scale=1.0):
     g = torch.Generator().manual_seed(seed)
-    return (torch.randn(*shape, generator=g) * scale).to(dtype)
+    return (torch.randn(*shape, generator=g, dtype=F32) * scale).to(dtype)
 
 
 def strided(x):
@@ -156,7 +156,7 @@ def test_qk_norm_rope_matches_the_formula(i, dtype):
     B, n, H, Hkv, d, rot, inter, per_head, far = ROPE[i]
     fused = rnd(i, B, n, H + 2 * Hkv, d, dtype=dtype).to(DEV)
     q, k = fused[:, :, :H], fused[:, :, H:H + Hkv]
-    wq, wk = ((torch.rand(*((h, d) if per_head else (d,)), generator=torch.Generator().manual_seed(i + 50)) + 0.5).to(DEV)
+    wq, wk = ((torch.rand(*((h, d) if per_head else (d,)), generator=torch.Generator().manual_seed(i + 50), dtype=F32) + 0.5).to(DEV)
               for h in (H, Hkv))
     if i == 0:
         wk = None
@@ -340,7 +340,7 @@ def layer(q, k, v, wq, wk, inv, do, **opt):
 
 def layer_inputs(seed=0, B=2, n=150, H=4, Hkv=2, d=64, dtype=BF):
     fused = rnd(seed, B, n, H + 2 * Hkv, d, dtype=dtype).to(DEV)
-    wq, wk = (torch.rand(d, generator=torch.Generator().manual_seed(seed + x)).to(DEV) + 0.5 for x in (1, 2))
+    wq, wk = (torch.rand(d, generator=torch.Generator().manual_seed(seed + x), dtype=F32).to(DEV) + 0.5 for x in (1, 2))
     inv = (10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).to(DEV)
     return fused[:, :, :H], fused[:, :, H:H + Hkv], fused[:, :, H + Hkv:], wq, wk, inv, rnd(seed + 3, B, H, n, d, dtype=dtype).to(DEV)
 
