@@ -372,7 +372,7 @@ struct DkvJob {
 // 32 keys each share a step's queries, or (NW = 1) QS waves share 32 keys, each
 // with every QS-th step's queries in LDS of its own, and add their sums.
 template <typename T, int DP, int DO, int QT, int NW, int QS>
-__global__ __launch_bounds__(64 * NW * QS) void k_window_dkv(const WindowBwdArgs g) {
+__global__ __launch_bounds__(64 * NW * QS, (DP == 64 && NW > 1 ? 2 : 1)) void k_window_dkv(const WindowBwdArgs g) {
   const WindowArgs& a = g.f;
   constexpr int KB = 32 * NW, NT = 64 * NW, NB = DO / 32;
   using L = Tile<T, DP>;
@@ -743,7 +743,7 @@ bool few_blocks(const WindowArgs& a, bool bf16, int n) {
 
 template <typename T, int DP>
 hipError_t fwd(const WindowArgs& a, hipStream_t s) {
-  constexpr int OCC = sizeof(T) == 4 || DP > 128 ? 1 : DP > 64 ? 2 : 4, W = sharers(sizeof(T) == 2, DP);
+  constexpr int OCC = DP > 128 ? 1 : sizeof(T) == 4 || DP > 64 ? 2 : 4, W = sharers(sizeof(T) == 2, DP);
   const int64_t bh = (int64_t)a.B * a.H;
   if (W > 1 && few_blocks(a, sizeof(T) == 2, a.n_q))
     k_window_fwd<T, DP, (W > 1 ? 1 : 4), W, (W > 1 ? 1 : OCC)><<<(unsigned)(bh * cdiv(a.n_q, 32)), 64 * W, 0, s>>>(a);
