@@ -535,3 +535,86 @@ def test_many_sequences_and_mixed_lengths():
             rows = slice(cu[b], cu[b] + new[b])
             want, tol = attention(q[rows].transpose(0, 1)[None].cpu(), K[b][:, :, :lens[b]], V[b][:, :, :lens[b]], window=70, sinks=1)
             check(f"{B} {b}", o[rows].transpose(0, 1)[None], want["o"], tol["o"])
+
+
+# enough heads that a workgroup takes 128 queries, or keys, in either type
+MANY = [
+    (8, 20, 4, 150, 150, 64, dict(window=60, sinks=3)),
+    (8, 20, 20, 140, 140, 128, dict(window=50, lookahead=7, lengths=[140, 1, 0, 129, 128, 64, 77, 139])),
+    (8, 20, 4, 130, 200, 80, dict(window=90, sinks=70)),
+    (8, 20, 10, 131, 131, 200, dict(lookahead=None)),
+    (4, 80, 16, 129, 270, 128, {}),
+    (6, 60, 20, 65, 65, 24, dict(window=1)),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("i", range(len(MANY)))
+def test_window_attention_of_many_heads(i, dtype):
+    B, H, Hkv, n_q, n_kv, d, opt = MANY[i]
+    opt = dict(opt)
+    q, k, v, do = (rnd(10 * i + x, B, h, n, d, dtype=dtype) for x, h, n in
+                   ((0, H, n_q), (1, Hkv, n_kv), (2, Hkv, n_kv), (3, H, n_q)))
+    want, tol = attention(q, k, v, do=do, **opt)
+    if "lengths" in opt:
+        opt["lengths"] = torch.tensor(opt["lengths"], dtype=torch.int32, device=DEV)
+    q, k, v, do = (strided(x.to(DEV)) if i % 2 else x.to(DEV) for x in (q, k, v, do))
+    print(f"[gpu] window of many heads {MANY[i]} {dtype}", flush=True)
+    o, lse = P.window_attention(q, k, v, with_lse=True, **opt)
+    dq, dk, dv = P.window_attention_backward(q, k, v, o, lse, do, **opt)
+    torch.cuda.synchronize()
+    for name, got in (("o", o), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        check(name, got, want[name], tol[name])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("d,opt", [(64, dict(window=20, sinks=2)), (128, dict(window=70)), (128, dict(window=10, lookahead=10)),
+                                   (200, {})])
+def test_infinities_and_nan_of_one_head_of_many(d, opt, value, dtype):
+    B, H, G, n, b, hk, rows = 8, 40, 2, 150, 3, 7, [75, 3]
+    q, k, v, do = (rnd(x, B, h, n, d, dtype=dtype).to(DEV) for x, h in ((0, H), (1, H // G), (2, H // G), (3, H)))
+    see = visible(n, n, n, 0, opt.get("window"), opt.get("sinks", 0), 0 if "lookahead" not in opt else opt["lookahead"])
+    hit_q, hit_k = see[:, rows].any(1), see[rows].any(0)
+    o0, lse0 = P.window_attention(q, k, v, with_lse=True, **opt)
+    g0 = P.window_attention_backward(q, k, v, o0, lse0, do, **opt)
+    print(f"[gpu] nonfinite of one head d={d} {opt} {value} {dtype}", flush=True)
+
+    def spoil(x, h):
+        x = x.clone()
+        x[b, h, rows, 5] = value
+        return x
+
+    def same(name, got, want, h, where):      # everything but the rows that are reached in heads h of batch b
+        keep = torch.ones(got.shape[:3], dtype=torch.bool, device=DEV)
+        for x in h:
+            keep[b, x] = ~where.to(DEV)
+        assert torch.equal(got[keep], want[keep]), name
+
+    heads = [hk * G, hk * G + 1]
+    one = torch.zeros(n, dtype=torch.bool)
+    one[rows] = True
+    o, lse = P.window_attention(q, k, spoil(v, hk), with_lse=True, **opt)
+    same("o", o, o0, heads, hit_q)
+    assert torch.equal(lse, lse0)
+    assert bool((~torch.isfinite(o[b, heads][:, hit_q.to(DEV), 5].float())).all())
+    ks = spoil(k, hk)
+    o, lse = P.window_attention(q, ks, v, with_lse=True, **opt)
+    same("o of k", o, o0, heads, hit_q)
+    dq, dk, dv = P.window_attention_backward(q, ks, v, o, lse, do, **opt)
+    reached = see[hit_q].any(0)
+    same("dq of k", dq, g0[0], heads, hit_q)
+    same("dk of k", dk, g0[1], [hk], reached)
+    same("dv of k", dv, g0[2], [hk], reached)
+    dq, dk, dv = P.window_attention_backward(q, k, v, o0, lse0, spoil(do, heads[1]), **opt)
+    same("dq of do", dq, g0[0], heads[1:], one)
+    same("dk of do", dk, g0[1], [hk], hit_k)
+    same("dv of do", dv, g0[2], [hk], hit_k)
+    assert bool((~torch.isfinite(dv[b, hk, hit_k.to(DEV), 5].float())).all())
+    qs = spoil(q, heads[1])
+    o, lse = P.window_attention(qs, k, v, with_lse=True, **opt)
+    same("o of q", o, o0, heads[1:], one)
+    dq, dk, dv = P.window_attention_backward(qs, k, v, o, lse, do, **opt)
+    same("dq of q", dq, g0[0], heads[1:], one)
+    same("dk of q", dk, g0[1], [hk], hit_k)
+    same("dv of q", dv, g0[2], [hk], hit_k)
