@@ -618,3 +618,36 @@ def test_infinities_and_nan_of_one_head_of_many(d, opt, value, dtype):
     same("dq of q", dq, g0[0], heads[1:], one)
     same("dk of q", dk, g0[1], [hk], hit_k)
     same("dv of q", dv, g0[2], [hk], hit_k)
+
+
+# long caches: the keys of a row are cut into parts, and these joined
+LONG = [
+    # lens, new, H, Hkv, d, page, options
+    ([5003], [1], 16, 4, 128, 64, dict(window=2048, sinks=4)),
+    ([3000, 10, 0, 700], [1, 1, 0, 1], 8, 2, 64, 16, {}),
+    ([2100, 40], [3, 2], 8, 8, 256, 32, dict(window=1500)),
+    ([1100, 700], [200, 90], 4, 2, 128, 24, dict(sinks=70, window=400)),
+    ([1300, 3], [150, 2], 4, 1, 64, 16, {}),
+    ([900, 1200], [70, 129], 2, 2, 200, 16, {}),
+    ([2500], [2000], 16, 16, 64, 16, {}),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("i", range(len(LONG)))
+def test_paged_attention_in_parts(i, dtype):
+    lens, new, H, Hkv, d, page, opt = LONG[i]
+    q, kc, vc, table, ln, cu_new, K, V, cu = paged_setup(lens, new, H, Hkv, d, page, dtype, seed=200 + i)
+    print(f"[gpu] paged in parts {LONG[i]} {dtype}", flush=True)
+    out = torch.full_like(q, 7.0)
+    P.paged_attention(q, kc, vc, table, ln, cu_new, out=out, **opt)
+    torch.cuda.synchronize()
+    for b in range(len(lens)):
+        rows = slice(cu[b], cu[b] + new[b])
+        if new[b]:
+            want, tol = attention(q[rows].transpose(0, 1)[None].cpu(), K[b], V[b], q_start=lens[b] - new[b], **opt)
+            check(f"{b}", out[rows].transpose(0, 1)[None], want["o"], tol["o"])
+    assert bool((out[cu[-1]:] == 7.0).all())
+    again = torch.full_like(q, 7.0)
+    P.paged_attention(q, kc, vc, table, ln, cu_new, out=again, **opt)
+    assert torch.equal(again, out)
