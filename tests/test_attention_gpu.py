@@ -147,6 +147,10 @@ ROPE = [
     (2, 3, 2, 2, 256, 0, False, False, 0),
     (1, 70, 1, 1, 512, 512, False, False, 0),
     (1, 2100, 2, 1, 72, 16, False, False, 0),
+    (3, 6001, 2, 1, 64, 32, False, False, 50000),
+    (1, 20000, 1, 1, 64, 64, True, True, 0),
+    (2, 9001, 4, 2, 128, 128, False, True, 5),
+    (1, 17000, 5, 1, 256, 256, False, False, 9),
 ]
 
 
