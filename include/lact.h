@@ -612,6 +612,10 @@ int lact_qk_norm_rope_backward(const lact_rope_desc* desc, const lact_view* q, c
  * or n_kv, <= 2^30; scale finite and > 0 (1e-12 to 1e12, else
  * LACT_EUNSUPPORTED). Weights and their cotangents are rounded to bf16 for the
  * second products with bf16 I/O; scores, maxima, sums and accumulators are fp32.
+ * Scores (scale q . k) stay below 2^29 in magnitude, here and over pages: past
+ * it the rounding of a row's maximum is larger than an exponent's range. The
+ * reverse takes the weights from lse, so they are off by |lse| 2^-24 of
+ * themselves.
  */
 typedef struct lact_attn_desc {
   int32_t B, H, Hkv, d;

@@ -655,3 +655,57 @@ def test_paged_attention_in_parts(i, dtype):
     again = torch.full_like(q, 7.0)
     P.paged_attention(q, kc, vc, table, ln, cu_new, out=again, **opt)
     assert torch.equal(again, out)
+
+
+# few heads over long windows: the queries of a tile of keys, and the heads that share it, are cut into parts
+PARTS = [
+    (1, 2, 1, 1300, 1300, 64, {}),
+    (1, 2, 2, 900, 900, 128, dict(window=700, sinks=3)),
+    (1, 4, 1, 800, 800, 128, dict(lookahead=None, lengths=[650])),
+    (2, 3, 1, 700, 1100, 80, dict(window=600, lookahead=40)),
+    (1, 6, 1, 600, 600, 256, {}),
+    (1, 1, 1, 1500, 1500, 64, dict(window=50, sinks=200)),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("i", range(len(PARTS)))
+def test_window_attention_backward_in_parts(i, dtype):
+    B, H, Hkv, n_q, n_kv, d, opt = PARTS[i]
+    opt = dict(opt)
+    q, k, v, do = (rnd(500 + 10 * i + x, B, h, n, d, dtype=dtype) for x, h, n in
+                   ((0, H, n_q), (1, Hkv, n_kv), (2, Hkv, n_kv), (3, H, n_q)))
+    want, tol = attention(q, k, v, do=do, **opt)
+    if "lengths" in opt:
+        opt["lengths"] = torch.tensor(opt["lengths"], dtype=torch.int32, device=DEV)
+    q, k, v, do = (x.to(DEV) for x in (q, k, v, do))
+    print(f"[gpu] window in parts {PARTS[i]} {dtype}", flush=True)
+    o, lse = P.window_attention(q, k, v, with_lse=True, **opt)
+    dq, dk, dv = P.window_attention_backward(q, k, v, o, lse, do, **opt)
+    torch.cuda.synchronize()
+    for name, got in (("o", o), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        check(name, got, want[name], tol[name])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+def test_scores_of_large_magnitude(dtype):
+    # rows that are all but one-hot, and a maximum whose rounding alone is tens of units
+    q, k, v = (rnd(700 + x, 2, 2, 200, 64, dtype=dtype) for x in range(3))
+    for size in (1e2, 1e4):
+        qs, ks = (q.float() * size).to(dtype), (k.float() * size).to(dtype)
+        o, lse = P.window_attention(qs.to(DEV), ks.to(DEV), v.to(DEV), window=90, with_lse=True)
+        want, tol = attention(qs, ks, v, window=90)
+        assert bool(torch.isfinite(o.float()).all())
+        # where the second largest score is further off than the scores' own rounding, o is the first's value
+        s = qs.double() @ ks.double().transpose(2, 3) / 8
+        s = torch.where(visible(200, 200, 200, 0, 90, 0, 0), s, torch.full_like(s, -math.inf))
+        top, at = s.topk(2, dim=-1)
+        sure = (top[..., 0] - top[..., 1] > 40 + 72 * 2.0 ** -23 * (qs.double().abs() @ ks.double().abs().transpose(2, 3)).amax(-1) / 8)
+        sure[..., 0] = True
+        first = torch.gather(v.double(), 2, at[..., :1].expand(-1, -1, -1, 64))
+        assert sure.float().mean() > 0.5
+        err = (o.double().cpu() - first).abs()[sure]
+        assert float(err.max()) <= 2 * HALF[dtype] * float(v.abs().max()) + 1e-5      # the weight's and the output's rounding
+        # a score is a sum of 64 products in fp32, off by up to 64 2^-24 of their magnitudes however
+        # small the sum is, so relative to the magnitudes (attention_reference.head), not to lse
+        check("lse", lse, want["lse"], tol["lse"])
