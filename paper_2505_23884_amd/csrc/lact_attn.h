@@ -120,6 +120,15 @@ template <> struct RowsB<float> {
   __device__ __forceinline__ explicit RowsB(const f32x16& s) : v(s) {}
 };
 
+// What the rounding to bf16 leaves of 32 rows: their product added to that of
+// the rounded ones is the product of the rows to 2^-16.
+__device__ __forceinline__ f32x16 below_bf16(const f32x16& s) {
+  f32x16 r;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) r[e] = s[e] - (float)(__bf16)s[e];
+  return r;
+}
+
 // What stands at a masked place must not reach an output, but zero times an
 // infinity or NaN is NaN, and a weight of zero is how a masked pair enters the
 // second products. Such values are rare: tiles at the edge of some query's

@@ -321,6 +321,10 @@ __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwd
   over_tiles([&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad) __attribute__((always_inline)) {
     f32x16 s;
     scores(ks, k0, rb, masked, bad, s);
+    // Of two keys a row's cotangents are one number and its negative: their
+    // rounding does not average out, so rows of few keys take what it leaves too.
+    if (sizeof(T) == 2 && n <= 64 / KT)
+      mma_rows<T, DP, DP / 32, decltype(rb)::value>(dq, RowsB<T>(below_bf16(s)), ks, 0);
     mma_rows<T, DP, DP / 32, decltype(rb)::value>(dq, RowsB<T>(s), ks, 0);
   });
   if constexpr (KS > 1) {
@@ -475,6 +479,8 @@ __global__ __launch_bounds__(64 * NW * QS, (DP == 64 && NW > 1 ? 2 : 1)) void k_
       }
     }
     mma_rows<T, DP, NB, RB>(dv, RowsB<T>(s), os, dsel * NB);
+    if (sizeof(T) == 2 && steps * QT <= 64)   // as in dq
+      mma_rows<T, DP, NB, RB>(dk, RowsB<T>(below_bf16(dp)), qs, dsel * NB);
     mma_rows<T, DP, NB, RB>(dk, RowsB<T>(dp), qs, dsel * NB);
   };
   if (Cp::thread() == 0) *found = -1;
@@ -645,6 +651,7 @@ __global__ __launch_bounds__(256 * QH, 2) void k_window_dkv16(const WindowBwdArg
         d[e] *= s[e];
       }
       mma_rows<T, DP, NB, 0>(dv, RowsB<T>(s), ot, 0);
+      if (__builtin_expect(steps == 1, 0)) mma_rows<T, DP, NB, 0>(dk, RowsB<T>(below_bf16(d)), qt, 0);   // as in dq
       mma_rows<T, DP, NB, 0>(dk, RowsB<T>(d), qt, 0);
     }
 #pragma unroll 1
