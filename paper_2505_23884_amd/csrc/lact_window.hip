@@ -322,8 +322,10 @@ __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwd
     f32x16 s;
     scores(ks, k0, rb, masked, bad, s);
     // Of two keys a row's cotangents are one number and its negative: their
-    // rounding does not average out, so rows of few keys take what it leaves too.
-    if (sizeof(T) == 2 && n <= 64 / KT)
+    // rounding does not average out, so rows of up to 128 keys take what it leaves
+    // too (error of dq, heads of 2 to 70 tokens: 1.5 to 1.8 times a plain form's
+    // that rounds its outputs only, 1.0 so; 1 % of the time of long calls).
+    if (sizeof(T) == 2 && n <= 128 / KT)
       mma_rows<T, DP, DP / 32, decltype(rb)::value>(dq, RowsB<T>(below_bf16(s)), ks, 0);
     mma_rows<T, DP, DP / 32, decltype(rb)::value>(dq, RowsB<T>(s), ks, 0);
   });
@@ -479,7 +481,7 @@ __global__ __launch_bounds__(64 * NW * QS, (DP == 64 && NW > 1 ? 2 : 1)) void k_
       }
     }
     mma_rows<T, DP, NB, RB>(dv, RowsB<T>(s), os, dsel * NB);
-    if (sizeof(T) == 2 && steps * QT <= 64)   // as in dq
+    if (sizeof(T) == 2 && a.q_start + i0 + RB < 128)   // rows of few keys, as in dq
       mma_rows<T, DP, NB, RB>(dk, RowsB<T>(below_bf16(dp)), qs, dsel * NB);
     mma_rows<T, DP, NB, RB>(dk, RowsB<T>(dp), qs, dsel * NB);
   };
@@ -651,7 +653,10 @@ __global__ __launch_bounds__(256 * QH, 2) void k_window_dkv16(const WindowBwdArg
         d[e] *= s[e];
       }
       mma_rows<T, DP, NB, 0>(dv, RowsB<T>(s), ot, 0);
-      if (__builtin_expect(steps == 1, 0)) mma_rows<T, DP, NB, 0>(dk, RowsB<T>(below_bf16(d)), qt, 0);   // as in dq
+      // rows of few keys, as in dq (1.5 % of a long call; the weights of dv, which
+      // hold no such pairs, as well: 4 %, by registers)
+      if (__builtin_expect(a.q_start + i0 + r0 < 128, 0))
+        mma_rows<T, DP, NB, 0>(dk, RowsB<T>(below_bf16(d)), qt, 0);
       mma_rows<T, DP, NB, 0>(dk, RowsB<T>(d), qt, 0);
     }
 #pragma unroll 1

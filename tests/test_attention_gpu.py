@@ -709,3 +709,26 @@ def test_scores_of_large_magnitude(dtype):
         # a score is a sum of 64 products in fp32, off by up to 64 2^-24 of their magnitudes however
         # small the sum is, so relative to the magnitudes (attention_reference.head), not to lse
         check("lse", lse, want["lse"], tol["lse"])
+
+
+@pytest.mark.parametrize("B,n,H,Hkv,d", [(4, 2, 40, 8, 80), (1, 2, 2, 2, 64), (1, 5, 2, 2, 128), (2, 40, 4, 2, 128), (2, 3, 4, 4, 256)])
+def test_gradients_of_few_keys_are_rounded_once(B, n, H, Hkv, d):
+    # score cotangents of few keys do not average their roundings: beside the output's own half
+    # step there is 2^-15 of each term (their two bf16 parts) and the fp32 arithmetic, no more
+    q, k, v, do = (rnd(800 + x, B, h, n, d).to(DEV) for x, h in ((0, H), (1, Hkv), (2, Hkv), (3, H)))
+    o, lse = P.window_attention(q, k, v, with_lse=True)
+    got = P.window_attention_backward(q, k, v, o, lse, do)
+    see, scale, u, h = visible(n, n, n, 0, None, 0, 0), d ** -0.5, 2.0 ** -24, HALF[BF]
+    want, tol = ([torch.zeros(t.shape, dtype=torch.float64) for t in got] for _ in range(2))
+    for b in range(B):
+        for i in range(H):
+            j = i // (H // Hkv)
+            qi, kj, vj, gi = (t.double().cpu() for t in (q[b, i], k[b, j], v[b, j], do[b, i]))
+            r = head(qi, kj, vj, see, scale, gi)
+            e = r["p"] * (r["e"] + 3 * (d + n + 8) * u) * (r["mdp"] + r["mdelta"]) + r["ds"].abs() * (2.0 ** -15 + r["e"])
+            want[0][b, i] = r["dq"]
+            tol[0][b, i] = e @ kj.abs() * scale
+            want[1][b, j] += r["dk"]
+            tol[1][b, j] += e.t() @ qi.abs() * scale
+    for name, x, w, t in zip(("dq", "dk"), got, want, tol):
+        check(name, x, w, 2 * t + w.abs() * h)      # (twice: the correction of delta carries the same errors)
