@@ -161,13 +161,15 @@ __device__ __forceinline__ void wave_fence() {   // LDS of one wave: its instruc
 }
 
 // The infinities and NaN of a scrubbed tile (offsets `at` of its keys, a lane
-// each) to the rows that see them.
-template <typename T, int DP, class See>
-__device__ __forceinline__ void restore_nonfinite(Softmax<DP / 32>& st, const T* vb, int64_t at, int d, See&& see) {
+// each) to the rows that see them: the sight counts from the lane's first row
+// of the tile, key j is row j - 4 (lane / 32) there, which may be below 0.
+template <typename T, int DP>
+__device__ __forceinline__ void restore_nonfinite(Softmax<DP / 32>& st, const T* vb, int64_t at, int d,
+                                                  const Sight& sight) {
 #pragma unroll 1
   for (int j = 0; j < kKT; ++j) {
     const int64_t o = shfl64(at, j);
-    if (o >= 0) add_nonfinite<T, DP / 32>(st.o, vb + o, see(j - 4 * (int)((threadIdx.x >> 5) & 1)), 0, d);
+    if (o >= 0) add_nonfinite<T, DP / 32>(st.o, vb + o, sight.see(j - 4 * (int)((threadIdx.x >> 5) & 1)), 0, d);
   }
 }
 
@@ -280,7 +282,7 @@ __global__ __launch_bounds__(64 * kWaves, OCC) void k_paged_wide(const PagedArgs
     for (; __builtin_expect(bad != 0, 0); bad &= bad - 1) {
       const int j = __builtin_ctzll(bad);
       const int64_t o = shfl64(here, j);
-      if (o >= 0) add_nonfinite<T, DP / 32>(st.o, vb + o, see(j - 4 * (lane >> 5)), 0, a.d);
+      if (o >= 0) add_nonfinite<T, DP / 32>(st.o, vb + o, sight.see(j - 4 * (lane >> 5)), 0, a.d);
     }
     here = next;
     next = after;
@@ -336,7 +338,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_paged_narrow(const PagedArgs a)
     const uint32_t mine = there >> (4 * (lane >> 5));
     auto see = [&](int r) __attribute__((always_inline)) { return sight.see(r) && (mine >> r & 1); };
     if (what) softmax_step<T, DP, 0>(st, q, ks, ks + BYTES, c, what == 1, see);
-    if (__builtin_expect(scrubbed, 0)) restore_nonfinite<T, DP>(st, vb, here, a.d, see);
+    if (__builtin_expect(scrubbed, 0)) restore_nonfinite<T, DP>(st, vb, here, a.d, sight);
   }
   // the waves' sums: each lane's [32][DP] and (m, l), added by all threads
   __syncthreads();

@@ -732,3 +732,41 @@ def test_gradients_of_few_keys_are_rounded_once(B, n, H, Hkv, d):
             tol[1][b, j] += e.t() @ qi.abs() * scale
     for name, x, w, t in zip(("dq", "dk"), got, want, tol):
         check(name, x, w, 2 * t + w.abs() * h)      # (twice: the correction of delta carries the same errors)
+
+
+# lens, new, H, Hkv, d, page, options, the sequence and positions of a value that is no number
+SPOILT = [
+    ([100], [1], 2, 1, 64, 16, {}, 0, (96, 97, 98, 99, 64, 3)),               # tiles of keys end past the length
+    ([70, 130], [1, 3], 4, 2, 128, 24, dict(window=37, sinks=2), 1, (128, 129, 93, 94, 0, 1)),
+    ([45], [1], 1, 1, 256, 7, dict(window=20), 0, (32, 35, 40, 44)),
+    ([100], [70], 4, 2, 64, 16, {}, 0, (96, 99, 31, 33, 64)),                 # 128 rows a workgroup
+    ([300, 9], [150, 9], 2, 2, 128, 16, dict(window=100, sinks=3), 0, (0, 2, 130, 192, 195, 256)),
+    ([150], [140], 1, 1, 200, 16, dict(window=50), 0, (1, 64, 67, 96, 149)),
+    ([3003], [1], 4, 1, 64, 64, dict(window=1027), 0, (3001, 2976, 2979, 1977, 1984)),      # keys in parts
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("i", range(len(SPOILT)))
+def test_infinities_and_nan_in_pages_reach_every_row_that_sees_them(i, value, dtype):
+    lens, new, H, Hkv, d, page, opt, b, where = SPOILT[i]
+    q, kc, vc, table, ln, cu_new, _, _, cu = paged_setup(lens, new, H, Hkv, d, page, dtype, seed=300 + i)
+    q = q[:cu[-1]].contiguous()
+    print(f"[gpu] nonfinite in pages {SPOILT[i]} {value} {dtype}", flush=True)
+    base = P.paged_attention(q, kc, vc, table, ln, cu_new, **opt)
+    assert bool(torch.isfinite(base.float()).all())
+    cols = torch.arange(d, device=DEV) % 3 == 1          # of every four, and eight, in a row some
+    for at in where:
+        spoilt = vc.clone()
+        spoilt[table[b, at // page], at % page][:, cols] = value
+        got = P.paged_attention(q, kc, spoilt, table, ln, cu_new, **opt)
+        see = visible(new[b], lens[b], lens[b], lens[b] - new[b], opt.get("window"), opt.get("sinks", 0), 0)[:, at]
+        assert bool(see.any())
+        hit = torch.zeros(cu[-1], dtype=torch.bool)
+        hit[cu[b]:cu[b + 1]] = see
+        hit = hit.to(DEV)
+        assert torch.equal(got[~hit], base[~hit]), at
+        assert torch.equal(got[hit][..., ~cols], base[hit][..., ~cols]), at
+        x = got[hit][..., cols]
+        assert bool(torch.isnan(x).all() if math.isnan(value) else (x == value).all()), at
