@@ -455,7 +455,7 @@ __global__ __launch_bounds__(256) void k_paged_append(const AppendArgs a) {
     if (mid < a.B && a.cu[mid] <= token) lo = mid;
     else hi = mid - 1;
   }
-  const int t0 = a.cu[lo], t1 = a.cu[lo + 1];
+  const int t0 = a.cu[lo], t1 = min(a.cu[lo + 1], a.T);   // (as find_rows)
   if (token < t0 || token >= t1) return;
   const int len = clampi(a.len[lo], 0, a.max_pages * a.page);
   const int64_t pos = len - ((int64_t)t1 - token);

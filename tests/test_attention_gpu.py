@@ -770,3 +770,36 @@ def test_infinities_and_nan_in_pages_reach_every_row_that_sees_them(i, value, dt
         assert torch.equal(got[hit][..., ~cols], base[hit][..., ~cols]), at
         x = got[hit][..., cols]
         assert bool(torch.isnan(x).all() if math.isnan(value) else (x == value).all()), at
+
+
+def clamped(B, H, d, n, splits):
+    """Sequences whose offsets, but the first one's, lie past the new tokens: all n of them are the first's."""
+    lens = [900 if splits else 60] + [40] * (B - 1)
+    q, kc, vc, table, ln, _, K, V, _ = paged_setup(lens, [n] + [0] * (B - 1), H, 1, d, 16, BF, seed=B + n)
+    q = q[:n].contiguous()
+    cu = torch.tensor([-9] + [100000] * B, dtype=torch.int32, device=DEV)
+    return q, kc, vc, table, ln, cu, K, V, lens
+
+
+@pytest.mark.parametrize("B,n,splits", [(2, 5, False), (3, 40, False), (70, 5, False), (70, 90, False), (2, 4, True), (70, 4, True)])
+def test_offsets_past_the_new_tokens_give_them_all_to_one_sequence(B, n, splits):
+    q, kc, vc, table, ln, cu, K, V, lens = clamped(B, 4, 64, n, splits)
+    o = P.paged_attention(q, kc, vc, table, ln, cu)
+    torch.cuda.synchronize()
+    want, tol = attention(q.transpose(0, 1)[None].cpu(), K[0], V[0], q_start=lens[0] - n)
+    check("o", o.transpose(0, 1)[None], want["o"], tol["o"])
+
+
+@pytest.mark.parametrize("B,n", [(2, 5), (70, 90)])
+def test_append_takes_offsets_past_the_new_tokens_as_the_attention_does(B, n):
+    _, kc, vc, table, ln, cu, _, _, lens = clamped(B, 4, 64, n, False)
+    kc, vc = torch.nan_to_num(kc, nan=3.0), torch.nan_to_num(vc, nan=3.0)
+    k, v = rnd(1, n, 1, 64).to(DEV), rnd(2, n, 1, 64).to(DEV)
+    kw, vw = kc.clone(), vc.clone()
+    for x in range(n):
+        p = lens[0] - n + x
+        if p >= 0:
+            kw[table[0, p // 16].item(), p % 16], vw[table[0, p // 16].item(), p % 16] = k[x], v[x]
+    P.paged_append(k, v, kc, vc, table, ln, cu)
+    torch.cuda.synchronize()
+    assert torch.equal(kc, kw) and torch.equal(vc, vw)
