@@ -2,7 +2,7 @@
 // reverse: y = R(pos) (w o x r), r = 1 / sqrt(mean(x^2) + eps), with R a
 // rotation of pairs of the first `rot` elements by pos freq_i.
 //
-//   g = R(-pos) dy,  n = w o g,  dx = r n - (r^3 / d) x <x, n>,  dw = sum g o x r
+//   u = r x,  g = R(-pos) dy,  n = w o g,  dx = r (n - u <u, n> / d),  dw = sum g o u
 //
 // Bound by HBM: x is read and y written once (the reverse reads x and dy and
 // writes dx). A workgroup takes `tb` tokens of q's heads or of k's: their
@@ -254,14 +254,15 @@ __device__ __forceinline__ void rope_back(const RopeArgs& a, const Pieces<GE>& p
       dot += x[k][i] * n[k][i];
     }
   const float r = 1.0f / sqrtf(group_add(ss, G) / (float)a.d + a.eps);
-  const float c = r * r * r * (group_add(dot, G) / (float)a.d);
+  const float c = r * group_add(dot, G) / (float)a.d;   // of u, not of x: r^3 leaves fp32's range where x and r do not
   T* dst = at.row<T>(a.dx[which], h);
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
 #pragma unroll
     for (int i = 0; i < GE; ++i) {
-      acc[k][i] += g[k][i] * x[k][i] * r;
-      n[k][i] = r * n[k][i] - c * x[k][i];
+      const float u = x[k][i] * r;
+      acc[k][i] += g[k][i] * u;
+      n[k][i] = r * (n[k][i] - c * u);
     }
     if (pc.ok[k]) store_piece<T, GE>(dst + pc.e[k], n[k]);
   }

@@ -803,3 +803,31 @@ def test_append_takes_offsets_past_the_new_tokens_as_the_attention_does(B, n):
     P.paged_append(k, v, kc, vc, table, ln, cu)
     torch.cuda.synchronize()
     assert torch.equal(kc, kw) and torch.equal(vc, vw)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("size,eps", [(1e-14, 0.0), (1e-13, 1e-30), (1e15, 1e-6)])
+@pytest.mark.parametrize("per_head", [False, True])
+def test_norm_of_small_and_large_vectors(size, eps, per_head, dtype):
+    # r = 1 / rms within fp32's range, r^3 past either end of it
+    B, n, H, Hkv, d = 2, 9, 3, 1, 64
+    q, k = rnd(1, B, n, H, d, dtype=F32).mul(size).to(dtype).to(DEV), rnd(2, B, n, Hkv, d, dtype=F32).mul(size).to(dtype).to(DEV)
+    wq, wk = (rnd(s, *((h, d) if per_head else (d,)), dtype=F32).to(DEV) for s, h in ((3, H), (4, Hkv)))
+    dqn, dkn = rnd(5, B, H, n, d, dtype=dtype).to(DEV), rnd(6, B, Hkv, n, d, dtype=dtype).to(DEV)
+    inv = (10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).to(DEV)
+    pos = torch.arange(n, dtype=torch.int32).repeat(B, 1)
+    qn, kn = P.qk_norm_rope(q, k, wq, wk, inv, eps=eps)
+    dq, dk, dwq, dwk = P.qk_norm_rope_backward(q, k, dqn, dkn, wq, wk, inv, eps=eps)
+    torch.cuda.synchronize()
+    h, u = HALF[dtype], 2.0 ** -24
+    for x, w, y, dy, dx, dw, name in ((q, wq, qn, dqn, dq, dwq, "q"), (k, wk, kn, dkn, dk, dwk, "k")):
+        ry, rdx, rdw, mag, wmag = norm_rope(x, w, inv, pos, eps, False, dy)
+        e = (d + 32) * u
+        r = 1.0 / torch.sqrt(x.double().cpu().square().mean(-1) + eps)
+        amp = ((x.double().cpu() * w.double().cpu()).abs().amax(-1) * r).transpose(1, 2)[..., None]
+        check(name + "n", y, ry, ry.abs() * h + amp * e)
+        # half a step of the smallest normal number where an element of dx lies below it
+        check("d" + name, dx, rdx, rdx.abs() * h + mag.amax(-1, keepdim=True) * e * 2 + 2.0 ** -126 * h)
+        if not per_head:
+            rdw, wmag = rdw.sum(0), wmag.sum(0)
+        check("dw" + name, dw, rdw, wmag.max() * (e + B * n * H * u) + rdw.abs() * u)
