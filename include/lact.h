@@ -564,7 +564,7 @@ typedef struct lact_view {
  */
 typedef struct lact_rope_desc {
   int32_t B, H, Hkv, d;
-  int64_t n;                /* tokens of a sequence; B * n <= 2^25              */
+  int64_t n;                /* tokens of a sequence; B * n <= 2^25 - 4          */
   int64_t pos0;             /* |pos0| <= 2^40                                   */
   int32_t rot;
   int32_t interleaved;      /* 0 or 1                                           */

@@ -14,7 +14,10 @@ size_t ws_round(size_t x) { return (x + kWsAlign - 1) / kWsAlign * kWsAlign; }
 constexpr int64_t kMaxTokenStride = (int64_t)1 << 22;   // 64 rows stay within a 31-bit buffer range
 constexpr int64_t kMaxInt = (int64_t)0x7fffffff;
 // A launch holds fewer than 2^32 threads in a direction.
-constexpr int64_t kRopeRows = (int64_t)1 << 25;       // tokens of a norm and rotation, four a workgroup of 256 at least
+// Tokens of a norm and rotation, of q and of k in one launch: four a workgroup
+// of 256 at least (vectors of more than 256 elements by pieces of four).
+constexpr int64_t kRopeRows = ((int64_t)1 << 25) - 4;
+static_assert(2 * (kRopeRows / 4) * 256 < ((int64_t)1 << 32), "threads of a launch");
 constexpr int64_t kAttnRows = (int64_t)1 << 30;       // queries, or keys, over the heads, 128 a workgroup of 512 at most
 constexpr int64_t kPagedRows = (int64_t)1 << 28;      // new tokens times heads, 32 a workgroup of 256
 constexpr int64_t kPagedElements = (int64_t)1 << 33;  // four a thread of the append

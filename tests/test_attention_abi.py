@@ -251,3 +251,11 @@ def test_norm_rope_gradients_against_differences(interleaved):
         u[0][i] += h
         u[1][i] -= h
         assert abs((loss(x, u[0]) - loss(x, u[1])) / (2 * h) - float(dw.sum(0)[i])) < 1e-8
+
+
+def test_norm_of_more_tokens_than_one_launch_holds_is_refused():
+    # q's and k's workgroups share a launch of fewer than 2^32 threads, four tokens in 256 of them at least
+    for n in (1 << 25, (1 << 25) - 3):
+        for back in (False, True):
+            assert rope({"B": 1, "n": n}, back, ws=1 << 50) == EUNSUPPORTED
+    assert rope({"B": 1 << 10, "n": 1 << 15}) == EUNSUPPORTED

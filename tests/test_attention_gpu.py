@@ -831,3 +831,22 @@ def test_norm_of_small_and_large_vectors(size, eps, per_head, dtype):
         if not per_head:
             rdw, wmag = rdw.sum(0), wmag.sum(0)
         check("dw" + name, dw, rdw, wmag.max() * (e + B * n * H * u) + rdw.abs() * u)
+
+
+def test_norm_of_the_most_tokens_that_a_launch_holds():
+    n, d = (1 << 25) - 4, 264                             # pieces of four elements, four tokens a workgroup
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of GPU memory")
+    x = rnd(1, 1, 1, 2, d).to(DEV)
+    q, k = (x[:, :, i:i + 1].expand(1, n, 1, d) for i in range(2))
+    inv = (10000.0 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).to(DEV)
+    print(f"[gpu] norm of {n} tokens", flush=True)
+    qn, kn = P.qk_norm_rope(q, k, None, None, inv, eps=1e-5)
+    torch.cuda.synchronize()
+    at = torch.tensor([0, 1, 4097, 1 << 22, (1 << 24) + 1, n - 5, n - 1])
+    for t, y in ((q, qn), (k, kn)):
+        want = norm_rope(t[:, :1].expand(1, len(at), 1, d).contiguous(), None, inv, at[None], 1e-5, False)
+        amp = t[0, 0, 0].double().cpu()
+        amp = float(amp.abs().max() / torch.sqrt(amp.square().mean() + 1e-5))
+        # the angle's fp32 fraction of a turn: 2 pi 2^-24, as everywhere
+        check("y", y[:, :, at.to(DEV)], want, want.abs() * HALF[BF] + amp * (d + 32) * 2.0 ** -24)
