@@ -609,8 +609,8 @@ int lact_qk_norm_rope_backward(const lact_rope_desc* desc, const lact_view* q, c
  * at padding). Sums over a group's heads are in a fixed order.
  *
  * d <= 256; n_q, n_kv, |q_start| and q_start + n_q <= 2^29; B * H times n_q,
- * or n_kv, <= 2^30; scale finite and > 0 (1e-12 to 1e12, else
- * LACT_EUNSUPPORTED). Weights and their cotangents are rounded to bf16 for the
+ * or n_kv, rounded up to a multiple of 128, < 2^30; scale finite and > 0 (1e-12
+ * to 1e12, else LACT_EUNSUPPORTED). Weights and their cotangents are rounded to bf16 for the
  * second products with bf16 I/O; scores, maxima, sums and accumulators are fp32.
  * Scores (scale q . k) stay below 2^29 in magnitude, here and over pages: past
  * it the rounding of a row's maximum is larger than an exponent's range. The

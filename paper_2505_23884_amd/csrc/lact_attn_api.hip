@@ -18,7 +18,10 @@ constexpr int64_t kMaxInt = (int64_t)0x7fffffff;
 // of 256 at least (vectors of more than 256 elements by pieces of four).
 constexpr int64_t kRopeRows = ((int64_t)1 << 25) - 4;
 static_assert(2 * (kRopeRows / 4) * 256 < ((int64_t)1 << 32), "threads of a launch");
-constexpr int64_t kAttnRows = (int64_t)1 << 30;       // queries, or keys, over the heads, 128 a workgroup of 512 at most
+// Tiles of 128 queries, or keys, over the heads: workgroups of 512 at most
+// (fp32 heads of more than 128 take twice that a tile of keys, but then 2^22
+// tiles of dk and dv are more than the card holds).
+constexpr int64_t kAttnTiles = (int64_t)1 << 23;
 constexpr int64_t kPagedRows = (int64_t)1 << 28;      // new tokens times heads, 32 a workgroup of 256
 constexpr int64_t kPagedElements = (int64_t)1 << 33;  // four a thread of the append
 
@@ -129,7 +132,7 @@ int check_attn(const lact_attn_desc* s) {
   if (s->n_q > kAttnTokens || s->n_kv > kAttnTokens || s->q_start > kAttnTokens || s->q_start < -kAttnTokens ||
       s->q_start + s->n_q > kAttnTokens)
     return LACT_EUNSUPPORTED;
-  if ((int64_t)s->B * s->H * std::max(s->n_q, s->n_kv) > kAttnRows) return LACT_EUNSUPPORTED;
+  if ((int64_t)s->B * s->H * ((std::max(s->n_q, s->n_kv) + 127) / 128) >= kAttnTiles) return LACT_EUNSUPPORTED;
   return LACT_OK;
 }
 

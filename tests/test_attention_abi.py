@@ -259,3 +259,11 @@ def test_norm_of_more_tokens_than_one_launch_holds_is_refused():
         for back in (False, True):
             assert rope({"B": 1, "n": n}, back, ws=1 << 50) == EUNSUPPORTED
     assert rope({"B": 1 << 10, "n": 1 << 15}) == EUNSUPPORTED
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("desc", [{"B": 1 << 10, "H": 1 << 10, "Hkv": 1 << 10, "n_q": 1, "n_kv": 897},
+                                  {"B": 1 << 10, "H": 1 << 10, "n_q": 1 << 10, "n_kv": 1}, {"B": 2, "H": 1, "Hkv": 1, "n_q": 1 << 29}])
+def test_window_attention_of_more_tiles_than_one_launch_holds_is_refused(desc, back):
+    # 2^23 tiles of 128 in workgroups of 512: 2^32 threads
+    assert attn(desc, back, ws=1 << 50) == EUNSUPPORTED
