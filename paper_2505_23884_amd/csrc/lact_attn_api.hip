@@ -31,7 +31,7 @@ bool finite(float x) { return x - x == 0.0f; }
 // error. `out`: its vectors must not overlap.
 int check_view(const lact_view* v, int64_t batch, int64_t head, int64_t token, int d, int es, bool out) {
   if (!v) return LACT_EINVAL;
-  if (batch * head * token == 0) return LACT_OK;
+  if (!batch || !head || !token) return LACT_OK;
   if (!v->data) return LACT_EINVAL;
   const int64_t ext[3] = {batch, head, token}, st[3] = {v->batch, v->head, v->token};
   for (int i = 0; i < 3; ++i) {
@@ -58,7 +58,7 @@ int check_view(const lact_view* v, int64_t batch, int64_t head, int64_t token, i
 // Strides of extents of 1 are not used: 0, so that no offset can overflow.
 AttnView take(const lact_view* v, int64_t batch, int64_t head, int64_t token) {
   AttnView a{};
-  if (batch * head * token == 0) return a;
+  if (!batch || !head || !token) return a;
   a.p = v->data;
   a.sb = batch > 1 ? v->batch : 0;
   a.sh = head > 1 ? v->head : 0;

@@ -267,3 +267,12 @@ def test_norm_of_more_tokens_than_one_launch_holds_is_refused():
 def test_window_attention_of_more_tiles_than_one_launch_holds_is_refused(desc, back):
     # 2^23 tiles of 128 in workgroups of 512: 2^32 threads
     assert attn(desc, back, ws=1 << 50) == EUNSUPPORTED
+
+
+def test_views_of_more_elements_than_an_integer_counts_are_looked_at():
+    # pages x heads x slots = 2^64, or a multiple of it
+    for pages, heads, page in ((1 << 30, 1 << 20, 1 << 14), (1 << 30, 1 << 19, 1 << 16)):
+        big = {"B": 1, "H": heads, "Hkv": heads, "pages": pages, "page": page, "n_new": 1}
+        for bad in (view(0), view(0x10008)):
+            assert paged(big, ws=1 << 50, k_cache=bad) in (EINVAL, EALIGN)
+            assert paged(big, append=True, k_cache=bad) in (EINVAL, EALIGN)
