@@ -248,15 +248,20 @@ __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwd
     Cp::rows(to + BYTES, row_of<T>(a.v, b, hk, k0), ldv, len - k0, a.d);
   };
   const int pa = a.q_start + r0, pb = a.q_start + min(r0 + QB - 1, last);
-  // The cotangents of the scores of rows RB .. of the tile.
-  auto scores = [&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad, f32x16& s)
+  // The cotangents of the scores of rows RB .. of the tile; with `Sum` the weights are added to `whole`.
+  float whole = 0.0f;
+  auto scores = [&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad, f32x16& s, auto with_sum)
       __attribute__((always_inline)) {
     constexpr int RB = decltype(rb)::value;
-    f32x16 dp;
+    constexpr bool Sum = decltype(with_sum)::value;
+    f32x16 dp, w;
     mma_dot<T, DP, RB>(s, ks, q);
     mma_dot<T, DP, RB>(dp, ks + BYTES, go);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, nlse2)) * (dp[e] + ndelta);
+    for (int e = 0; e < 16; ++e) {
+      w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, nlse2));
+      s[e] = w[e] * (dp[e] + ndelta);
+    }
     if (masked) {
       if (__builtin_expect(bad != 0, 0))   // keys that held an infinity or NaN
 #pragma unroll
@@ -264,8 +269,15 @@ __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwd
           if (bad >> (RB + 8 * (e >> 2) + 4 * half + (e & 3)) & 1) s[e] = __builtin_nanf("");
       const Sight sight(a, p, jhi, k0);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = sight.see(RB + 8 * (e >> 2) + (e & 3)) ? s[e] : 0.0f;
+      for (int e = 0; e < 16; ++e) {
+        const bool see = sight.see(RB + 8 * (e >> 2) + (e & 3));
+        s[e] = see ? s[e] : 0.0f;
+        if (Sum) w[e] = see ? w[e] : 0.0f;
+      }
     }
+    if (Sum)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) whole += w[e];
   };
   // use(tile, k0, RB, masked, bad) for each 32 keys that the wave sees something of
   auto over_tiles = [&](auto use) __attribute__((always_inline)) {
@@ -291,25 +303,33 @@ __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwd
   if (sizeof(T) == 2 && n <= 256 / KT) {
     // delta from a rounded o is off by 2^-8 of its terms, which shows in rows
     // of few keys (their o is large): the cotangents of a row's scores sum to
-    // zero, so a pass over its keys finds what is missing.
+    // zero, so a pass over its keys finds what is missing. Where lse is of more
+    // keys than these (split over calls) the weights here sum to less than 1 and
+    // the cotangents need not cancel: such rows keep delta as it is, also those
+    // whose scores are so large that the weights' own error passes 2^-12.
     float rest = 0.0f;
     over_tiles([&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad) __attribute__((always_inline)) {
       f32x16 s;
-      scores(ks, k0, rb, masked, bad, s);
+      scores(ks, k0, rb, masked, bad, s, std::true_type{});
 #pragma unroll
       for (int e = 0; e < 16; ++e) rest += s[e];
     });
     if constexpr (KS > 1) {
       float* all = reinterpret_cast<float*>(smem_) + lane;
       __syncthreads();
-      all[ks_ * 64] = rest;
+      all[2 * ks_ * 64] = rest;
+      all[(2 * ks_ + 1) * 64] = whole;
       __syncthreads();
-      rest = 0.0f;
-      for (int w = 0; w < KS; ++w) rest += all[w * 64];
+      rest = whole = 0.0f;
+      for (int w = 0; w < KS; ++w) {
+        rest += all[2 * w * 64];
+        whole += all[(2 * w + 1) * 64];
+      }
       __syncthreads();
     }
     rest = half_sum(rest);
-    if (__builtin_isfinite(rest)) ndelta -= rest;   // (an infinite key that weighs nothing leaves the row its delta)
+    const bool all_keys = fabsf(half_sum(whole) - 1.0f) < 0x1p-12f;
+    if (all_keys && __builtin_isfinite(rest)) ndelta -= rest;   // (an infinite key that weighs nothing leaves the row its delta)
   }
   if (i < a.n_q && lane < 32 && ks_ == 0) {
     g.nlse[at] = nlse;
@@ -320,7 +340,7 @@ __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwd
   for (int x = 0; x < DP / 32; ++x) dq[x] = f32x16{};
   over_tiles([&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad) __attribute__((always_inline)) {
     f32x16 s;
-    scores(ks, k0, rb, masked, bad, s);
+    scores(ks, k0, rb, masked, bad, s, std::false_type{});
     // Of two keys a row's cotangents are one number and its negative: their
     // rounding does not average out, so rows of up to 128 keys take what it leaves
     // too (error of dq, heads of 2 to 70 tokens: 1.5 to 1.8 times a plain form's

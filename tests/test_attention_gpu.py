@@ -850,3 +850,22 @@ def test_norm_of_the_most_tokens_that_a_launch_holds():
         amp = float(amp.abs().max() / torch.sqrt(amp.square().mean() + 1e-5))
         # the angle's fp32 fraction of a turn: 2 pi 2^-24, as everywhere
         check("y", y[:, :, at.to(DEV)], want, want.abs() * HALF[BF] + amp * (d + 32) * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("B,H,n,d,cut", [(1, 2, 60, 64, 30), (1, 2, 200, 128, 70), (8, 16, 150, 64, 50), (1, 2, 100, 256, 99)])
+def test_reverse_of_a_part_of_the_keys_with_the_whole_rows_lse(B, H, n, d, cut, dtype):
+    # keys split over calls: each call's reverse takes the rows' o and lse over all keys, and gives its part
+    q, k, v, do = (rnd(950 + x, B, H, n, d, dtype=dtype) for x in range(4))
+    want, tol = attention(q, k, v, lookahead=None, do=do)
+    qd, kd, vd, gd = (t.to(DEV) for t in (q, k, v, do))
+    print(f"[gpu] parts of the keys B={B} H={H} n={n} d={d} cut={cut} {dtype}", flush=True)
+    o, lse = P.window_attention(qd, kd, vd, lookahead=None, with_lse=True)
+    parts = [P.window_attention_backward(qd, kd[:, :, a:b], vd[:, :, a:b], o, lse, gd, lookahead=None)
+             for a, b in ((0, cut), (cut, n))]
+    h = HALF[dtype]
+    for x, name in ((1, "dk"), (2, "dv")):
+        check(name, torch.cat([p[x] for p in parts], 2), want[name], tol[name])
+    # dq: each part is rounded by itself, so the two half steps are of their own sizes
+    dq = sum(p[0].double().cpu() for p in parts)
+    check("dq", dq, want["dq"], tol["dq"] + sum(p[0].double().cpu().abs() for p in parts) * h * 1.01)
