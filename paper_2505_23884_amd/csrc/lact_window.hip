@@ -49,6 +49,39 @@ __device__ __forceinline__ int length_of(const WindowArgs& a, int b) {
   return a.len ? min(max(a.len[b], 0), a.n_kv) : a.n_kv;
 }
 
+// Rows of few keys (16-bit I/O): those that see at most this many. What the
+// reverse does for their sake (k_window_dq) goes by each row's own count, so it
+// is the same in dq and dk, whichever kernels run and whatever rows stand beside.
+constexpr int kFewKeys = 128;
+
+// The number of keys that position p of a sequence of len sees.
+__device__ __forceinline__ int keys_of(const WindowArgs& a, int len, int p) {
+  const int hi = min(p + a.look, len - 1), lo = max(0, p - a.win + 1);
+  return max(0, hi - lo + 1) + max(0, min(min(a.sinks, hi + 1), lo));
+}
+// Which of 32 queries see few keys, for the kernel that holds queries by rows.
+struct FewKeys {
+  int below, above;   // queries i .. i + 31 of below <= i <= above all see more
+  __device__ __forceinline__ FewKeys(const WindowArgs& a, int len) {
+    // they share the keys from the last one's window to the first one's end
+    const bool never = a.look >= kFewKeys + 32 - a.win && len > kFewKeys;   // (look + win may be 2^31)
+    below = never ? kFewKeys - a.look - a.q_start : (1 << 30);
+    above = len + a.win - (kFewKeys + 33) - a.q_start;
+  }
+  __device__ __forceinline__ bool any(int i) const { return (i < below) | (i > above); }
+  // What the rounding to bf16 leaves of the rows of an accumulator (below_bf16)
+  // whose queries, from i on, see few keys.
+  static __device__ __forceinline__ f32x16 below_bf16_of(const WindowArgs& a, int len, int i, const f32x16& s) {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));   // nothing of this is worked out ahead of a loop, for it hardly ever runs
+    const uint32_t few = (uint32_t)__ballot(keys_of(a, len, a.q_start + i + (lane & 31)) <= kFewKeys) >> (lane >> 5) * 4;
+    f32x16 r = below_bf16(s);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) r[e] = few >> (8 * (e >> 2) + (e & 3)) & 1 ? r[e] : 0.0f;
+    return r;
+  }
+};
+
 // Keys a tile: those of a lone wave (of NW = 1) leave room for three more waves' at DP = 128.
 template <typename T, int DP, int NW> constexpr int key_tile() {
   return sizeof(T) == 2 && DP <= (NW > 1 ? 128 : 64) ? 64 : 32;
@@ -300,7 +333,10 @@ __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwd
       Cp::sync();
     }
   };
-  if (sizeof(T) == 2 && n <= 256 / KT) {
+  // the lane's query, some of the wave's and some of the workgroup's
+  const bool few = sizeof(T) == 2 && live && keys_of(a, len, p) <= kFewKeys, few_wave = __any(few);
+  const bool few_block = sizeof(T) == 2 && (NW > 1 ? __syncthreads_or(few) : few_wave);
+  if (few_block) {
     // delta from a rounded o is off by 2^-8 of its terms, which shows in rows
     // of few keys (their o is large): the cotangents of a row's scores sum to
     // zero, so a pass over its keys finds what is missing. Where lse is of more
@@ -329,7 +365,7 @@ __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwd
     }
     rest = half_sum(rest);
     const bool all_keys = fabsf(half_sum(whole) - 1.0f) < 0x1p-12f;
-    if (all_keys && __builtin_isfinite(rest)) ndelta -= rest;   // (an infinite key that weighs nothing leaves the row its delta)
+    if (few && all_keys && __builtin_isfinite(rest)) ndelta -= rest;   // (an infinite key that weighs nothing leaves the row its delta)
   }
   if (i < a.n_q && lane < 32 && ks_ == 0) {
     g.nlse[at] = nlse;
@@ -338,17 +374,27 @@ __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwd
   f32x16 dq[DP / 32];
 #pragma unroll
   for (int x = 0; x < DP / 32; ++x) dq[x] = f32x16{};
-  over_tiles([&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad) __attribute__((always_inline)) {
-    f32x16 s;
-    scores(ks, k0, rb, masked, bad, s, std::false_type{});
-    // Of two keys a row's cotangents are one number and its negative: their
-    // rounding does not average out, so rows of up to 128 keys take what it leaves
-    // too (error of dq, heads of 2 to 70 tokens: 1.5 to 1.8 times a plain form's
-    // that rounds its outputs only, 1.0 so; 1 % of the time of long calls).
-    if (sizeof(T) == 2 && n <= 128 / KT)
-      mma_rows<T, DP, DP / 32, decltype(rb)::value>(dq, RowsB<T>(below_bf16(s)), ks, 0);
-    mma_rows<T, DP, DP / 32, decltype(rb)::value>(dq, RowsB<T>(s), ks, 0);
-  });
+  // The rounding of the cotangents to 16 bits makes the error of dq and dk 1.4
+  // times that of a form which rounds its outputs only, of however many keys. A
+  // second product, of what it leaves, makes it 1.0. Rows of few keys take it: in
+  // long calls they are the first ones and cost nothing that shows; a window of
+  // 128 costs 9 % of the training call ([1, 16 / 4, 8192, 128]: 164 to 179 us).
+  auto products = [&](auto rest) __attribute__((always_inline)) {
+    over_tiles([&](const uint8_t* ks, int k0, auto rb, bool masked, uint64_t bad) __attribute__((always_inline)) {
+      constexpr int RB = decltype(rb)::value;
+      f32x16 s;
+      scores(ks, k0, rb, masked, bad, s, std::false_type{});
+      mma_rows<T, DP, DP / 32, RB>(dq, RowsB<T>(s), ks, 0);
+      if (decltype(rest)::value && few_wave) {
+        s = below_bf16(s);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = few ? s[e] : 0.0f;
+        mma_rows<T, DP, DP / 32, RB>(dq, RowsB<T>(s), ks, 0);
+      }
+    });
+  };
+  if (few_block) products(std::integral_constant<bool, sizeof(T) == 2>{});
+  else products(std::false_type{});
   if constexpr (KS > 1) {
     static_assert(DP / 2 * 64 * 4 <= 4 * BYTES, "sums of a wave");
     if (!join_waves<KS, DP / 32>(dq, reinterpret_cast<float*>(smem_), ks_)) return;
@@ -419,6 +465,7 @@ __global__ __launch_bounds__(64 * NW * QS, (DP == 64 && NW > 1 ? 2 : 1)) void k_
   DkvJob job(a, g.plan, blockIdx.x / ND, gridDim.x / ND);
   const int bk = job.bk, b = bk / a.Hkv, hk = bk % a.Hkv;
   const int len = length_of(a, b);
+  const FewKeys few(a, len);
   job.queries(a, g.plan, len);
   const int kw = job.tile * KB + 32 * wave, j = kw + (lane & 31), jc = min(j, a.n_kv - 1);
   const bool live = j < len;
@@ -501,8 +548,10 @@ __global__ __launch_bounds__(64 * NW * QS, (DP == 64 && NW > 1 ? 2 : 1)) void k_
       }
     }
     mma_rows<T, DP, NB, RB>(dv, RowsB<T>(s), os, dsel * NB);
-    if (sizeof(T) == 2 && a.q_start + i0 + RB < 128)   // rows of few keys, as in dq
-      mma_rows<T, DP, NB, RB>(dk, RowsB<T>(below_bf16(dp)), qs, dsel * NB);
+    if constexpr (sizeof(T) == 2) {
+      if (__builtin_expect(few.any(i0 + RB), 0))
+        mma_rows<T, DP, NB, RB>(dk, RowsB<T>(FewKeys::below_bf16_of(a, len, i0 + RB, dp)), qs, dsel * NB);
+    }
     mma_rows<T, DP, NB, RB>(dk, RowsB<T>(dp), qs, dsel * NB);
   };
   if (Cp::thread() == 0) *found = -1;
@@ -568,6 +617,7 @@ __global__ __launch_bounds__(256 * QH, 2) void k_window_dkv16(const WindowBwdArg
   DkvJob job(a, g.plan, blockIdx.x, gridDim.x);
   const int bk = job.bk, b = bk / a.Hkv, hk = bk % a.Hkv;
   const int len = length_of(a, b);
+  const FewKeys few(a, len);
   job.queries(a, g.plan, len);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
   const int kg = wave & 3, qh = wave >> 2;
@@ -673,10 +723,10 @@ __global__ __launch_bounds__(256 * QH, 2) void k_window_dkv16(const WindowBwdArg
         d[e] *= s[e];
       }
       mma_rows<T, DP, NB, 0>(dv, RowsB<T>(s), ot, 0);
-      // rows of few keys, as in dq (1.5 % of a long call; the weights of dv, which
-      // hold no such pairs, as well: 4 %, by registers)
-      if (__builtin_expect(a.q_start + i0 + r0 < 128, 0))
-        mma_rows<T, DP, NB, 0>(dk, RowsB<T>(below_bf16(d)), qt, 0);
+      // (of dv, whose weights' rounding nothing of the kind corrects, the same would
+      // cost 4 % of a long call, by registers)
+      if (__builtin_expect(few.any(i0 + r0), 0))
+        mma_rows<T, DP, NB, 0>(dk, RowsB<T>(FewKeys::below_bf16_of(a, len, i0 + r0, d)), qt, 0);
       mma_rows<T, DP, NB, 0>(dk, RowsB<T>(d), qt, 0);
     }
 #pragma unroll 1

@@ -869,3 +869,72 @@ def test_reverse_of_a_part_of_the_keys_with_the_whole_rows_lse(B, H, n, d, cut, 
     # dq: each part is rounded by itself, so the two half steps are of their own sizes
     dq = sum(p[0].double().cpu() for p in parts)
     check("dq", dq, want["dq"], tol["dq"] + sum(p[0].double().cpu().abs() for p in parts) * h * 1.01)
+
+
+def few_keys(q, k, v, o, lse, do, **opt):
+    """dq and dk of bf16 calls against 64 bits: rows that see 128 keys at most with the rounding of their outputs and
+    2^-15 of each term (the two bf16 parts of a score's cotangent, delta freed of the rounding of o), the others with
+    a half step of each cotangent and of o."""
+    B, H, n_q, d = q.shape
+    Hkv, n_kv = k.shape[1], k.shape[2]
+    kw = dict(opt)
+    if "lengths" in opt:
+        kw["lengths"] = torch.tensor(opt["lengths"], dtype=torch.int32, device=DEV)
+    got = P.window_attention_backward(q, k, v, o, lse, do, **kw)
+    scale, u, h = d ** -0.5, 2.0 ** -24, HALF[BF]
+    want, tol = ([torch.zeros(t.shape, dtype=torch.float64) for t in got] for _ in range(2))
+    for b in range(B):
+        L = opt["lengths"][b] if "lengths" in opt else n_kv
+        see = visible(n_q, n_kv, L, opt.get("q_start", n_kv - n_q), opt.get("window"), opt.get("sinks", 0), opt.get("lookahead", 0))
+        few = (see.sum(1, keepdim=True) <= 128).double()
+        n = int(see.sum(1).max())
+        for i in range(H):
+            j = i // (H // Hkv)
+            qi, kj, vj, gi = (t.double().cpu() for t in (q[b, i], k[b, j], v[b, j], do[b, i]))
+            r = head(qi, kj, vj, see, scale, gi)
+            t = bounds(r, qi, kj, gi, scale, BF)
+            o_err = (gi.abs() * (t["o"] + r["o"].abs() * h)).sum(1, keepdim=True)
+            e = r["p"] * (r["e"] + 3 * (d + n + 8) * u) * (r["mdp"] + r["mdelta"]) + r["ds"].abs() * (2.0 ** -15 + r["e"])
+            e = e + (1 - few) * (r["p"] * o_err + r["ds"].abs() * h)
+            want[0][b, i] = r["dq"]
+            tol[0][b, i] = e @ kj.abs() * scale
+            want[1][b, j] += r["dk"]
+            tol[1][b, j] += e.t() @ qi.abs() * scale
+    for name, x, w, t in zip(("dq", "dk"), got, want, tol):
+        check(name, x, w, 2 * t + w.abs() * h)      # (twice: the correction of delta carries the same errors)
+
+
+# B, H, Hkv, n_q, n_kv, d, options
+FEW = [
+    (1, 2, 1, 400, 400, 64, dict(window=2)),
+    (1, 2, 2, 400, 400, 128, dict(window=8)),
+    (1, 4, 2, 300, 300, 128, dict(window=60)),
+    (2, 2, 1, 400, 400, 80, dict(window=40, sinks=3)),
+    (1, 2, 2, 400, 400, 64, dict(window=128)),
+    (1, 2, 1, 400, 400, 64, dict(window=129)),                    # all but the first rows see more
+    (1, 2, 1, 300, 300, 128, {}),                                  # the rows around position 128
+    (1, 2, 2, 200, 200, 256, dict(window=30)),
+    (1, 2, 1, 200, 200, 256, {}),
+    (1, 2, 1, 300, 300, 64, dict(window=0, sinks=5)),
+    (1, 2, 2, 300, 300, 128, dict(window=70, sinks=90)),           # few by the window, many by the sinks
+    (1, 2, 1, 100, 500, 64, dict(window=20)),                      # q_start 400
+    (1, 2, 1, 300, 300, 64, dict(window=20, lookahead=15)),
+    (1, 2, 1, 300, 300, 64, dict(window=30, lookahead=None)),      # few at the end only
+    (1, 2, 1, 300, 300, 128, dict(window=None, lookahead=None)),   # nowhere few, the first positions neither
+    (2, 2, 1, 300, 300, 64, dict(window=None, lookahead=None, lengths=[300, 100])),
+    (8, 16, 4, 300, 300, 64, dict(window=16)),                     # 128 queries a workgroup
+    (4, 32, 8, 300, 300, 128, dict(window=40, sinks=2)),
+    (8, 16, 16, 200, 200, 128, {}),
+]
+
+
+@pytest.mark.parametrize("i", range(len(FEW)))
+def test_rows_of_few_keys_wherever_they_stand(i):
+    B, H, Hkv, n_q, n_kv, d, opt = FEW[i]
+    q, k, v, do = (rnd(900 + 10 * i + x, B, h, n, d).to(DEV) for x, h, n in ((0, H, n_q), (1, Hkv, n_kv), (2, Hkv, n_kv), (3, H, n_q)))
+    kw = dict(opt)
+    if "lengths" in opt:
+        kw["lengths"] = torch.tensor(opt["lengths"], dtype=torch.int32, device=DEV)
+    print(f"[gpu] few keys {FEW[i]}", flush=True)
+    o, lse = P.window_attention(q, k, v, with_lse=True, **kw)
+    few_keys(q, k, v, o, lse, do, **opt)
