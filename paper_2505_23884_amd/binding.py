@@ -801,7 +801,7 @@ def _fn(name):
 def _pack(pack, *fields):
     try:
         return pack(*fields)
-    except (struct.error, OverflowError) as e:   # the latter for floats
+    except struct.error as e:
         raise LactError(-1, f"an argument is out of range: {e}") from None
 
 
