@@ -938,3 +938,41 @@ def test_rows_of_few_keys_wherever_they_stand(i):
     print(f"[gpu] few keys {FEW[i]}", flush=True)
     o, lse = P.window_attention(q, k, v, with_lse=True, **kw)
     few_keys(q, k, v, o, lse, do, **opt)
+
+
+# long calls, tiles and parts at every place: each visible pair is counted once
+COUNTED = [
+    (1, 2, 1, 2600, 2600, 64, dict(window=600, sinks=70)),
+    (1, 4, 2, 2100, 2100, 128, dict(window=300, sinks=4)),
+    (1, 2, 2, 1700, 1700, 128, {}),
+    (2, 3, 1, 1000, 1300, 80, dict(window=500, lookahead=100, lengths=[1300, 900])),
+    (1, 2, 1, 1500, 1500, 96, dict(window=None, lookahead=None)),
+    (4, 32, 4, 520, 520, 64, dict(window=130, sinks=3)),
+    (1, 2, 1, 900, 900, 256, dict(window=200)),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("i", range(len(COUNTED)))
+def test_every_visible_pair_is_counted_once(i, dtype):
+    # Where every score is 0 a row's weights are one number, and with rows of the unit matrix
+    # for values, cotangents, keys or queries an element of an output is a sum of equal signs over
+    # every d-th pair: its bound is relative to itself, and one pair less or twice is past it.
+    B, H, Hkv, n_q, n_kv, d, opt = COUNTED[i]
+    opt = dict(opt)
+    unit = lambda h, n: torch.eye(d, dtype=dtype)[torch.arange(n) % d].expand(B, h, n, d).contiguous()
+    zero = lambda h, n: torch.zeros(B, h, n, d, dtype=dtype)
+    first = lambda h, n: torch.zeros(B, h, n, d, dtype=dtype).index_fill(3, torch.tensor([0]), 1.0)
+    sign = lambda h, n: first(h, n) * (1.0 - 2.0 * (torch.arange(n) % 2))[:, None].to(dtype)
+    ln = opt.get("lengths")
+    for q, k, v, do, names in ((zero(H, n_q), unit(Hkv, n_kv), unit(Hkv, n_kv), unit(H, n_q), ("o", "dv")),
+                               (zero(H, n_q), unit(Hkv, n_kv), sign(Hkv, n_kv), first(H, n_q), ("dq",)),
+                               (unit(H, n_q), zero(Hkv, n_kv), sign(Hkv, n_kv), first(H, n_q), ("dk",))):
+        want, tol = attention(q, k, v, do=do, **opt)
+        kw = dict(opt, lengths=torch.tensor(ln, dtype=torch.int32, device=DEV)) if ln else opt
+        q, k, v, do = (t.to(DEV) for t in (q, k, v, do))
+        print(f"[gpu] pairs {COUNTED[i]} {names} {dtype}", flush=True)
+        o, lse = P.window_attention(q, k, v, with_lse=True, **kw)
+        got = dict(zip(("dq", "dk", "dv"), P.window_attention_backward(q, k, v, o, lse, do, **kw)), o=o)
+        for x in names:
+            check(x, got[x], want[x], tol[x])
