@@ -613,8 +613,12 @@ int lact_qk_norm_rope_backward(const lact_rope_desc* desc, const lact_view* q, c
  *
  * d <= 256; n_q, n_kv, |q_start| and q_start + n_q <= 2^29; B * H times n_q,
  * or n_kv, rounded up to a multiple of 128, < 2^30; scale finite and > 0 (1e-12
- * to 1e12, else LACT_EUNSUPPORTED). Weights and their cotangents are rounded to bf16 for the
- * second products with bf16 I/O; scores, maxima, sums and accumulators are fp32.
+ * to 1e12, else LACT_EUNSUPPORTED). Scores, maxima, sums and accumulators are
+ * fp32. With bf16 I/O the weights and their cotangents are rounded to bf16 for
+ * the second products: outputs are off by about 0.0023 of their norm, where the
+ * rounding of the outputs alone makes 0.0017. dq and dk of rows that see at most
+ * 128 keys, and the output of few new tokens over pages (tokens times H / Hkv up
+ * to 32 a sequence on average), take what that rounding leaves too.
  * Scores (scale q . k) stay below 2^29 in magnitude, here and over pages: past
  * it the rounding of a row's maximum is larger than an exponent's range. The
  * reverse takes the weights from lse, so they are off by |lse| 2^-24 of

@@ -976,3 +976,21 @@ def test_every_visible_pair_is_counted_once(i, dtype):
         got = dict(zip(("dq", "dk", "dv"), P.window_attention_backward(q, k, v, o, lse, do, **kw)), o=o)
         for x in names:
             check(x, got[x], want[x], tol[x])
+
+
+@pytest.mark.parametrize("lens,new,H,Hkv,d,page,opt", [
+    ([40, 333], [1, 1], 16, 2, 128, 16, {}), ([700], [1], 4, 4, 64, 24, dict(window=500, sinks=3)), ([300, 90], [4, 2], 4, 1, 80, 16, {}),
+    ([200], [3], 2, 2, 256, 32, {}), ([5003], [1], 16, 4, 128, 64, dict(window=2048, sinks=4)), ([1], [1], 2, 1, 64, 16, {})])
+def test_tokens_over_pages_are_rounded_once(lens, new, H, Hkv, d, page, opt):
+    # up to 32 rows (tokens times heads of a group) a sequence: beside the output's own half step
+    # there is 2^-15 of each weight (its two bf16 parts) and the fp32 arithmetic, no more
+    q, kc, vc, table, ln, cu_new, K, V, cu = paged_setup(lens, new, H, Hkv, d, page, BF, seed=400 + d)
+    print(f"[gpu] tokens {lens} {new} {H} {Hkv} {d}", flush=True)
+    o = P.paged_attention(q, kc, vc, table, ln, cu_new, **opt)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lens):
+        see = visible(new[b], n, n, n - new[b], opt.get("window"), opt.get("sinks", 0), 0)
+        for h in range(H):
+            x, j = q[cu[b]:cu[b + 1], h].cpu(), h // (H // Hkv)
+            r = head(x, K[b][0, j], V[b][0, j], see, d ** -0.5)
+            check(f"{b} {h}", o[cu[b]:cu[b + 1], h], r["o"], r["o_mag"] * (r["e"] + 2.0 ** -15 + n * 2.0 ** -24) * 1.01 + r["o"].abs() * HALF[BF])
