@@ -12,11 +12,14 @@
 //   wide    128 rows, 32 a wave; the tiles pass through LDS for all waves,
 //           copied there without registers between.
 // Measured, bf16, heads of 128, 16 over 4: decoding of 64 sequences of up to
-// 16384 tokens, 1.59 GB, 334 us or 4.8 TB/s (a large copy moves 4.9); one
-// token over a window of 2048, 8.4 us and 4 for the joining of 20 parts; six
-// chunks of up to 700 tokens over 4096 to 8192, 201 GF, 350 us or 0.57 PF
-// (matrix cores busy 24 % of the cycles, vector instructions 26 %, the rest
-// waits for LDS and for the slots' addresses).
+// 16384 tokens, 1.59 GB, 323 to 349 us by the card's clock, 4.9 to 4.6 TB/s (a
+// large copy moves 4.9); one token over a window of 2048, 8.4 us and 4 for the
+// joining of 20 parts; six chunks of up to 700 tokens over 4096 to 8192, 201 GF,
+// 314 to 354 us, 0.64 to 0.57 PF (matrix cores busy 26 % of the cycles, vector
+// instructions 28 %, the rest waits for LDS and for the slots' addresses); 63
+// tokens and a chunk of 700, each over 8192, 302 us, where the tokens alone take
+// 231 and the chunk 95. Heads of 256 spill 99 registers of the narrow kernel, in
+// its loop too: 32 sequences of up to 16384, 1.58 GB, 502 us or 3.1 TB/s.
 // Where the row tiles alone would leave the chip idle, the tiles of keys are
 // cut into `splits` parts; each leaves its maximum, sum and unnormalised
 // output, and k_paged_join adds them in order.
@@ -500,7 +503,9 @@ hipError_t run(const PagedArgs& a, hipStream_t s) {
 
 void paged_plan(PagedArgs& a, bool bf16) {
   // rows a sequence on average: more than one narrow tile's, and the keys
-  // are better shared by four waves
+  // are better shared by four waves (16 / 4 heads of 128, 64 sequences of 4096:
+  // 24 rows 118 us narrow and 117 wide, 36 rows 154 and 122, 72 rows 218 and 134;
+  // of 16 sequences, which leave CUs idle, 24 rows 50 and 36)
   a.wide = (int64_t)a.T * a.G > 32 * (int64_t)a.B || (!bf16 && a.d > 128);
   const int64_t groups = (int64_t)row_tiles(a, a.wide) * a.Hkv;
   const int64_t most = std::max<int64_t>(1, ((int64_t)a.max_pages * a.page + kKT - 1) / kKT / (2 * kWaves));

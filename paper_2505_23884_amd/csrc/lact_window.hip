@@ -97,8 +97,8 @@ template <typename T, int DP, int NW> constexpr int key_tile() {
 // 128 queries share each tile that comes from L2, and 64 keys a step leave two
 // workgroups a CU (D = 128; four at 64): one's vector work and LDS reads run
 // beside the other's products. bf16, heads of 128: [1, 16, 16384], window 2048:
-// 347 to 410 us by the card's clock, 0.74 to 0.63 PF; [2, 40, 3120], all keys:
-// 483 to 517, 0.82 to 0.77 (a library product of 8192 x 8192 x 8192: 1.15).
+// 337 to 424 us by the card's clock, 0.76 to 0.61 PF; [2, 40, 3120], all keys:
+// 468 to 592, 0.85 to 0.67 (a library product of 8192 x 8192 x 8192: 1.15).
 // Heads of 64, [2, 32 / 8, 8192], causal: 0.76. Matrix instructions take 31 % of
 // the cycles (1.9 GHz), vector ones 37 % and a quarter more for exponentials.
 // Weaving the halves of a tile in one wave (one's scores beside the other's
@@ -230,7 +230,10 @@ __device__ __forceinline__ float dot_half(const u32x4 (&x)[N], const u32x4 (&y)[
 // dq: queries stay in registers with their cotangents, keys and values pass
 // through LDS as in the forward (NW, KS as there). Leaves -lse / scale and -delta of its queries
 // for dk and dv, whose accumulators start from them. Three products a pair with
-// one exponential: [1, 16 / 4, 8192, 128] bf16, window 2048, 4 sinks: 215 us, 0.84 PF.
+// one exponential: [1, 16 / 4, 8192, 128] bf16, window 2048, 4 sinks: 214 to 231
+// us by the card's clock, 0.84 to 0.78 PF. Registers: what spills at heads of 128
+// (44) stays out of the products; fp32 heads of 256 spill 173, read back among
+// theirs too.
 template <typename T, int DP, int NW, int KS, int OCC>
 __global__ __launch_bounds__(64 * NW * KS, OCC) void k_window_dq(const WindowBwdArgs g) {
   const WindowArgs& a = g.f;
@@ -601,7 +604,8 @@ __global__ __launch_bounds__(64 * NW * QS, (DP == 64 && NW > 1 ? 2 : 1)) void k_
 // matrix products. The values wait in LDS instead of registers. Four products
 // a pair, 40 KB of fragments from LDS for 32 matrix instructions: bound by
 // those reads and their waits ([1, 16 / 4, 8192, 128], window 2048, 4 sinks:
-// 430 us, 0.56 PF, matrix cores busy 24 %).
+// 421 to 462 us by the card's clock, 0.57 to 0.52 PF, matrix cores busy 24 %; 9
+// registers spill).
 template <int DP, int QH>
 __global__ __launch_bounds__(256 * QH, 2) void k_window_dkv16(const WindowBwdArgs g) {
   typedef __bf16 T;
@@ -811,7 +815,9 @@ constexpr int sharers(bool bf16, int DP) { return DP <= (bf16 ? 128 : 64) ? 4 : 
 // waves take turns at the other side's tiles and join their sums: more CUs and
 // a shorter chain of tiles. Their LDS holds one workgroup a CU, so past 64
 // times four of them they come in rounds, each a W-th as long; fp32's longer
-// products forgive more of these. This and workgroups of 128, in us:
+// products forgive more of these. (Heads of more than 128 in bf16 have two such
+// waves and would gain past their limit of 48 too.) This and workgroups of 128,
+// in us:
 //   training  [1, 2, 256, 64] fp32, window 64 (4 workgroups of 128)      43   94
 //             [1, 8 / 4, 2048, 64] fp32, window 512 (128)               165  260
 //             [1, 12 / 4, 2048, 64] fp32, window 512 (192)              238  262
@@ -820,6 +826,14 @@ constexpr int sharers(bool bf16, int DP) { return DP <= (bf16 ? 128 : 64) ? 4 : 
 //             [1, 8 / 4, 1536, 128] bf16, window 512 (96)                27   25
 //             [1, 8 / 4, 2048, 64] bf16, window 512 (128)                19   19
 //             [1, 12 / 4, 2048, 64] bf16, window 512 (192)               27   18
+//             [1, 4 / 2, 1024, 256] bf16, window 512 (32)                34   50
+//             [1, 4 / 2, 2048, 256] bf16, window 512 (64)                36   51
+//   dq        [1, 8 / 4, 1024, 128] bf16, window 512 (64)                17   28
+//             [1, 8 / 4, 1536, 128] bf16, window 512 (96)                30   29
+//             [1, 8 / 4, 1024, 64] bf16, window 512 (64)                 13   22
+//             [1, 8 / 4, 1536, 64] bf16, window 512 (96)                 23   22
+//             [1, 4 / 2, 1024, 256] bf16, window 512 (32)                29   49
+//             [1, 4 / 2, 2048, 256] bf16, window 512 (64)                30   49
 bool few_blocks(const WindowArgs& a, bool bf16, int n) {
   const int W = sharers(bf16, a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256);
   return W > 1 && (int64_t)a.B * a.H * cdiv(n, 128) < (bf16 ? 24 : 64) * W;
