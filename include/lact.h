@@ -609,7 +609,8 @@ int lact_qk_norm_rope_backward(const lact_rope_desc* desc, const lact_view* q, c
  * at padding). Sums over a group's heads are in a fixed order. Where the keys
  * of a row are split over calls (its position below n_kv in each), o and lse are
  * those of the whole row, and each call gives dk and dv of its keys and its part
- * of the sum dq.
+ * of the sum dq. Infinities at visible places of q or k make cotangents that
+ * meet them NaN, also where the pair weighs nothing.
  *
  * d <= 256; n_q, n_kv, |q_start| and q_start + n_q <= 2^29; B * H times n_q,
  * or n_kv, rounded up to a multiple of 128, < 2^30; scale finite and > 0 (1e-12
