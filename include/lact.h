@@ -688,6 +688,86 @@ int lact_paged_attention(const lact_paged_desc* desc, const lact_view* q, const 
                          const lact_view* o, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * A cache in 8 bits. A slot's vector of one head is held as e4m3 numbers c_i
+ * (sign, 4 bits of exponent, 3 of significand, bias 7; 0x7f and 0xff are NaN,
+ * there are no infinities) and one byte x for all of them, and stands for
+ *
+ *   c_i 2^(x - 127)
+ *
+ * which bf16 and fp32 hold exactly: nothing is rounded when it is read.
+ * lact_paged_append_e4m3 is lact_paged_append into such a cache: with a the
+ * largest |element| of a vector, x - 127 is the smallest e with a <= 448 2^e,
+ * within [-117, 119], and the elements are rounded to the nearest number, ties
+ * to the even one (so they are off by 2^-4 of themselves, or by 2^(e - 10) where
+ * that is more: elements below 2^-14 of the largest). Magnitudes over 448 2^119
+ * become that. Infinities and NaN become NaN (0x7f) and do not count for a. Vectors
+ * of zeros have x = 10.
+ *
+ *   k_cache, v_cache   views of bytes [page][head][slot][d], strides in
+ *                      multiples of 16 bytes, the same of both
+ *   k_scale, v_scale   views of bytes [page][head][slot] (a vector is one byte;
+ *                      any alignment), the same strides of both
+ *
+ * lact_paged_read_e4m3 is its reverse: rows cu_new[b] .. cu_new[b + 1] - 1 of k
+ * and v (io_dtype) get what the cache holds for the last positions of sequence
+ * b (with cu_new the sums of lens: all of them), zeros for positions that
+ * hold nothing. lact_paged_attention_e4m3 is lact_paged_attention over such a
+ * cache. Values read are exact for x in [10, 246], all that the append writes;
+ * with other bytes in a slot they may be zero, infinite or NaN.
+ *
+ * d a multiple of 16 (else LACT_EUNSUPPORTED); the other limits and refusals of
+ * lact_paged_append and lact_paged_attention.
+ */
+int lact_paged_append_e4m3(const lact_paged_desc* desc, const lact_view* k, const lact_view* v,
+                           const lact_view* k_cache, const lact_view* v_cache, const lact_view* k_scale,
+                           const lact_view* v_scale, const int32_t* table, const int32_t* lens, const int32_t* cu_new,
+                           void* stream);
+int lact_paged_read_e4m3(const lact_paged_desc* desc, const lact_view* k_cache, const lact_view* v_cache,
+                         const lact_view* k_scale, const lact_view* v_scale, const int32_t* table, const int32_t* lens,
+                         const int32_t* cu_new, const lact_view* k, const lact_view* v, void* stream);
+size_t lact_paged_attention_e4m3_workspace_bytes(const lact_paged_desc* desc, int* err);
+int lact_paged_attention_e4m3(const lact_paged_desc* desc, const lact_view* q, const lact_view* k_cache,
+                              const lact_view* v_cache, const lact_view* k_scale, const lact_view* v_scale,
+                              const int32_t* table, const int32_t* lens, const int32_t* cu_new, const lact_view* o,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of new tokens of sequences that share a prefix, in groups: the
+ * prefix's keys and values are read once for all rows of its group.
+ *
+ * Group g is sequences cu_seq[g] .. cu_seq[g + 1] - 1 (cu_seq ascending); its
+ * prefix is lens[g] positions, position j on page table[g][j / page] of the
+ * same cache. The sequences' own tables, lens and cu_new are those of
+ * lact_paged_attention and count from the prefix's end: a token that stands at
+ * p among its sequence's own keys has position lens[g] + p, sees the prefix's
+ * key j as key j and its sequence's key j as key lens[g] + j, with the window
+ * and sinks over these positions. So a call gives what lact_paged_attention
+ * gives for sequences whose tables begin with the prefix's pages (where the
+ * prefix fills them). Sequences of no group have no prefix; a token that its
+ * sequence does not hold (more new tokens than lens[b]) sees nothing. Device
+ * data out of range is clamped, as there.
+ *
+ * k_scale and v_scale NULL: a cache of io_dtype elements; else both, and the
+ * cache is one of e4m3 numbers.
+ *
+ * groups >= 1 (else LACT_EINVAL); groups * Hkv <= 2^20; the pages of a
+ * prefix and of a sequence together hold at most 2^29 positions; the other
+ * limits of lact_paged_attention.
+ */
+typedef struct lact_prefix {
+  int32_t groups, max_pages;
+  const int32_t *table;     /* int32 [groups][max_pages]                        */
+  const int32_t *lens;      /* int32 [groups]                                   */
+  const int32_t *cu_seq;    /* int32 [groups + 1]                               */
+} lact_prefix;
+size_t lact_paged_prefix_attention_workspace_bytes(const lact_paged_desc* desc, const lact_prefix* prefix, int* err);
+int lact_paged_prefix_attention(const lact_paged_desc* desc, const lact_prefix* prefix, const lact_view* q,
+                                const lact_view* k_cache, const lact_view* v_cache, const lact_view* k_scale,
+                                const lact_view* v_scale, const int32_t* table, const int32_t* lens,
+                                const int32_t* cu_new, const lact_view* o, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/*
  * Kernel timing (instrumentation for benchmarks). While enabled, lact_forward
  * brackets every kernel launch with HIP events on its stream, grouped by
  * kernel class (LACT_KCLASS_*). lact_timing_read synchronises on the recorded
@@ -707,8 +787,9 @@ int lact_paged_attention(const lact_paged_desc* desc, const lact_view* q, const 
                                /* as BWD, its row and token steps as UPDATE, its  */
                                /* transposed copies as PREP)                      */
 #define LACT_KCLASS_ATTN 6     /* lact_window_attention and its reverse,          */
-                               /* lact_paged_attention (lact_qk_norm_rope, its    */
-                               /* reverse and lact_paged_append count as IO)      */
+                               /* lact_paged_attention and its kin                */
+                               /* (lact_qk_norm_rope, its reverse, the appends    */
+                               /* and the reading back count as IO)               */
 #define LACT_KCLASS_COUNT 7
 int lact_timing_enable(int enable);
 int lact_timing_reset(void);

@@ -69,6 +69,11 @@ class LactPagedDesc(ctypes.Structure):
                 ("scale", ctypes.c_float), ("io_dtype", ctypes.c_int32)]
 
 
+class LactPrefix(ctypes.Structure):
+    _fields_ = [("groups", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("cu_seq", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -129,12 +134,21 @@ def load_library(path: str | None = None):
     L.lact_window_attention_backward.argtypes = [ap, vw, vw, vw, vw, vp, vw, vp, vw, vw, vw, vp, sz, vp]
     L.lact_paged_append.argtypes = [pp, vw, vw, vw, vw, vp, vp, vp, vp]
     L.lact_paged_attention.argtypes = [pp, vw, vw, vw, vp, vp, vp, vw, vp, sz, vp]
+    xp = ctypes.POINTER(LactPrefix)
+    L.lact_paged_append_e4m3.argtypes = [pp] + [vw] * 6 + [vp] * 4
+    L.lact_paged_read_e4m3.argtypes = [pp] + [vw] * 4 + [vp] * 3 + [vw, vw, vp]
+    L.lact_paged_attention_e4m3.argtypes = [pp] + [vw] * 5 + [vp] * 3 + [vw, vp, sz, vp]
+    L.lact_paged_prefix_attention.argtypes = [pp, xp] + [vw] * 5 + [vp] * 3 + [vw, vp, sz, vp]
+    L.lact_paged_prefix_attention_workspace_bytes.argtypes = [pp, xp, ip]
+    L.lact_paged_prefix_attention_workspace_bytes.restype = sz
     for f in ("lact_qk_norm_rope", "lact_qk_norm_rope_backward", "lact_window_attention",
-              "lact_window_attention_backward", "lact_paged_append", "lact_paged_attention"):
+              "lact_window_attention_backward", "lact_paged_append", "lact_paged_attention", "lact_paged_append_e4m3",
+              "lact_paged_read_e4m3", "lact_paged_attention_e4m3", "lact_paged_prefix_attention"):
         getattr(L, f).restype = i32
     for f, desc in (("lact_qk_norm_rope_backward_workspace_bytes", rp),
                     ("lact_window_attention_backward_workspace_bytes", ap),
-                    ("lact_paged_attention_workspace_bytes", pp)):
+                    ("lact_paged_attention_workspace_bytes", pp),
+                    ("lact_paged_attention_e4m3_workspace_bytes", pp)):
         getattr(L, f).argtypes = [desc, ip]
         getattr(L, f).restype = sz
     L.lact_timing_enable.argtypes = [i32]
@@ -782,6 +796,7 @@ _pack_view = struct.Struct("Pqqq").pack
 _pack_rope = struct.Struct("4i2q4ifi").pack
 _pack_attn = struct.Struct("4i6qfi").pack
 _pack_paged = struct.Struct("4i2q2i2qfi").pack
+_pack_prefix = struct.Struct("2i3P").pack
 _packed = {}
 
 
@@ -843,6 +858,14 @@ def _view_n(t, name, shape, dtype, dev):
     _refuse(t, name, shape, dtype, dev)
 
 
+def _view_s(t, name, shape, dtype, dev):
+    """The same of scales [page, slot, head], one element each."""
+    if t is not None and t.shape == shape and t.dtype is dtype and t.get_device() == dev >= 0:
+        s = t.stride()
+        return _pack_view(t.data_ptr(), s[0], s[2], s[1])
+    raise LactError(-1, f"{name} must be a {dtype} tensor {list(shape)}, on the first one's device")
+
+
 def _aux(t, name, shape, dtype, dev):
     """The address of a contiguous tensor of that shape, type and device, or None."""
     if t is None:
@@ -884,12 +907,12 @@ def _new(like, shape, stream, torch, dtype=None):
         return like.new_empty(shape, dtype=dtype or like.dtype)
 
 
-def _workspace(name, desc, workspace, like, stream, torch):
+def _workspace(name, desc, workspace, like, stream, torch, *more):
     """(tensor that stays alive, address, bytes) of the caller's workspace, or of
     a new one of the size that the call needs (0 too where the descriptor is
     refused, which the call itself then says)."""
     if workspace is None:
-        n = _fn(name)(desc, None)
+        n = (_packed.get(name) or _fn(name))(desc, *more, None)
         if not n:
             return None, None, 0
         workspace = _new(like, n, stream, torch, torch.uint8)
@@ -1069,6 +1092,117 @@ def paged_attention(q, k_cache, v_cache, table, lens, cu_new, *, window=None, si
     o = _new(q, s, stream, torch) if out is None else out
     workspace, wp, nb = _workspace("lact_paged_attention_workspace_bytes", desc, workspace, q, stream, torch)
     _call("lact_paged_attention", dev, stream, torch, desc, qv, *tail, _view_n(o, "o", s, dt, dev), wp, nb)
+    return o
+
+
+def _code_args(x, H, n, dtype, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, window, sinks, scale, torch):
+    """As _paged_args() for a cache of e4m3 numbers: x is a tensor of the call's device, n its new tokens."""
+    if k_cache.dim() != 4 or table.dim() != 2:
+        raise LactError(-1, "new tokens are [n_new, heads, d], caches [pages, page, Hkv, d], table [B, max_pages]")
+    sc = pages, page, Hkv, d = k_cache.shape
+    B, max_pages = table.shape
+    dev, i32, u8, f8 = x.get_device(), torch.int32, torch.uint8, torch.float8_e4m3fn
+    io = IO_BF16 if dtype is torch.bfloat16 else IO_FP32 if dtype is torch.float32 else None
+    if io is None:
+        raise LactError(-1, f"unsupported dtype {dtype}")
+    desc = _pack(_pack_paged, B, H, Hkv, d, n, pages, page, max_pages, -1 if window is None else int(window),
+                 int(sinks), d ** -0.5 if scale is None else float(scale), io)
+    return d, dev, desc, (_view_t(k_cache, "k_cache", sc, f8, dev), _view_t(v_cache, "v_cache", sc, f8, dev),
+                          _view_s(k_scale, "k_scale", sc[:3], u8, dev), _view_s(v_scale, "v_scale", sc[:3], u8, dev),
+                          _aux(table, "table", (B, max_pages), i32, dev), _aux(lens, "lens", (B,), i32, dev),
+                          _aux(cu_new, "cu_new", (B + 1,), i32, dev))
+
+
+def paged_append_e4m3(k, v, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, *, stream=None):
+    """paged_append() into a cache in 8 bits (lact_paged_append_e4m3): k_cache,
+    v_cache float8_e4m3fn [pages, page, Hkv, d] (d a multiple of 16) and
+    k_scale, v_scale uint8 [pages, page, Hkv], in place. A vector is held as
+    numbers c and a byte x, and stands for c 2^(x - 127), the smallest power of
+    two that takes its largest element."""
+    import torch
+    if k.dim() != 3 or k_cache.dim() != 4:
+        raise LactError(-1, "k and v are [n_new, Hkv, d], caches [pages, page, Hkv, d]")
+    n, Hkv, dt = k.shape[0], k_cache.shape[2], k.dtype
+    d, dev, desc, tail = _code_args(k, Hkv, n, dt, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, None, 0, 1.0,
+                                    torch)
+    s = (n, Hkv, d)
+    _call("lact_paged_append_e4m3", dev, stream, torch, desc, _view_n(k, "k", s, dt, dev), _view_n(v, "v", s, dt, dev),
+          *tail)
+
+
+def paged_read_e4m3(k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, n_new, *, dtype=None, out=None, stream=None):
+    """What the cache of paged_append_e4m3() holds for the last positions of
+    sequences (lact_paged_read_e4m3): returns (k, v) [n_new, Hkv, d] of
+    ``dtype`` (bf16 or fp32; bf16), exactly, where rows cu_new[b] ..
+    cu_new[b + 1] - 1 are sequence b's last positions (with cu_new the sums of
+    lens: whole sequences); rows of no sequence are left as they were,
+    positions that hold nothing are zeros. ``out`` may hold that pair."""
+    import torch
+    if k_cache.dim() != 4:
+        raise LactError(-1, "caches are [pages, page, Hkv, d]")
+    Hkv = k_cache.shape[2]
+    dt = dtype if dtype is not None else torch.bfloat16 if out is None else out[0].dtype
+    n = int(n_new)
+    d, dev, desc, tail = _code_args(k_cache, Hkv, n, dt, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, None, 0,
+                                    1.0, torch)
+    s = (n, Hkv, d)
+    if n < 0:
+        raise LactError(-1, "n_new must not be negative")
+    k, v = (_new(k_cache, s, stream, torch, dt), _new(k_cache, s, stream, torch, dt)) if out is None else out
+    _call("lact_paged_read_e4m3", dev, stream, torch, desc, *tail, _view_n(k, "k", s, dt, dev),
+          _view_n(v, "v", s, dt, dev))
+    return k, v
+
+
+def paged_attention_e4m3(q, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, *, window=None, sinks=0, scale=None,
+                         out=None, workspace=None, stream=None):
+    """paged_attention() over the cache of paged_append_e4m3()
+    (lact_paged_attention_e4m3)."""
+    import torch
+    if q.dim() != 3:
+        raise LactError(-1, "q must be [n_new, H, d]")
+    T, H, _ = q.shape
+    dt = q.dtype
+    d, dev, desc, tail = _code_args(q, H, T, dt, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, window, sinks,
+                                    scale, torch)
+    s = (T, H, d)
+    qv = _view_n(q, "q", s, dt, dev)
+    o = _new(q, s, stream, torch) if out is None else out
+    workspace, wp, nb = _workspace("lact_paged_attention_e4m3_workspace_bytes", desc, workspace, q, stream, torch)
+    _call("lact_paged_attention_e4m3", dev, stream, torch, desc, qv, *tail, _view_n(o, "o", s, dt, dev), wp, nb)
+    return o
+
+
+def paged_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, cu_seq, table, lens, cu_new, *, k_scale=None,
+                           v_scale=None, window=None, sinks=0, scale=None, out=None, workspace=None, stream=None):
+    """paged_attention() of sequences that share prefixes, each read once for
+    its group (lact_paged_prefix_attention): group g is sequences cu_seq[g] ..
+    cu_seq[g + 1] - 1 (int32 [groups + 1]), its prefix the first prefix_lens[g]
+    (int32 [groups]) positions on pages prefix_table[g] (int32 [groups,
+    max_pages]) of the same cache. table and lens of a sequence begin at the
+    prefix's end; window and sinks go by the positions from the prefix's
+    start. With k_scale and v_scale the cache is one of paged_append_e4m3()."""
+    import torch
+    if q.dim() != 3 or prefix_table.dim() != 2:
+        raise LactError(-1, "q must be [n_new, H, d], prefix_table [groups, max_pages]")
+    T, H, _ = q.shape
+    dt, i32 = q.dtype, torch.int32
+    if (k_scale is None) != (v_scale is None):
+        raise LactError(-1, "k_scale and v_scale are given both or not at all")
+    if k_scale is None:
+        d, _, dev, desc, tail = _paged_args(q, H, k_cache, v_cache, table, lens, cu_new, window, sinks, scale, torch)
+        tail = (*tail[:2], None, None, *tail[2:])
+    else:
+        d, dev, desc, tail = _code_args(q, H, T, dt, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, window,
+                                        sinks, scale, torch)
+    groups, width = prefix_table.shape
+    prefix = _pack(_pack_prefix, groups, width, _aux(prefix_table, "prefix_table", (groups, width), i32, dev) or 0,
+                   _aux(prefix_lens, "prefix_lens", (groups,), i32, dev) or 0, _aux(cu_seq, "cu_seq", (groups + 1,), i32, dev) or 0)
+    s = (T, H, d)
+    qv = _view_n(q, "q", s, dt, dev)
+    o = _new(q, s, stream, torch) if out is None else out
+    workspace, wp, nb = _workspace("lact_paged_prefix_attention_workspace_bytes", desc, workspace, q, stream, torch, prefix)
+    _call("lact_paged_prefix_attention", dev, stream, torch, desc, prefix, qv, *tail, _view_n(o, "o", s, dt, dev), wp, nb)
     return o
 
 

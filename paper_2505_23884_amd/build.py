@@ -12,7 +12,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liblact.so")
 SOURCES = ["lact_api.hip", "lact_kernels.hip", "lact_io.hip", "lact_attn_api.hip", "lact_window.hip", "lact_paged.hip",
-           "lact_rope.hip"]
+           "lact_rope.hip", "lact_codes.hip", "lact_prefix.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,6 +1,6 @@
 // Host side of the attention entry points: validation (before any HIP call),
 // workspaces and launches. All arithmetic runs in lact_window.hip,
-// lact_paged.hip and lact_rope.hip.
+// lact_paged.hip, lact_rope.hip, lact_codes.hip and lact_prefix.hip.
 #include <algorithm>
 
 #include "lact.h"
@@ -28,7 +28,7 @@ constexpr int64_t kPagedElements = (int64_t)1 << 33;  // four a thread of the ap
 bool finite(float x) { return x - x == 0.0f; }
 
 // A view of [batch][head][token] vectors of `es`-byte elements: LACT_OK or an
-// error. `out`: its vectors must not overlap.
+// error. `out`: its vectors must not overlap. `es` 0: bytes, without alignment.
 int check_view(const lact_view* v, int64_t batch, int64_t head, int64_t token, int d, int es, bool out) {
   if (!v) return LACT_EINVAL;
   if (!batch || !head || !token) return LACT_OK;
@@ -48,7 +48,7 @@ int check_view(const lact_view* v, int64_t batch, int64_t head, int64_t token, i
       span += (__int128)(ext[i] - 1) * st[i];
     }
   }
-  if ((uintptr_t)v->data & 15) return LACT_EALIGN;
+  if (es && ((uintptr_t)v->data & 15)) return LACT_EALIGN;
   for (int i = 0; i < 3; ++i)
     if (ext[i] > 1 && st[i] * es % 16) return LACT_EALIGN;
   if (token > 1 && v->token > kMaxTokenStride) return LACT_EUNSUPPORTED;
@@ -179,14 +179,16 @@ int check_paged(const lact_paged_desc* s, bool attend) {
   return LACT_OK;
 }
 
-int check_cache(const lact_paged_desc* s, const lact_view* kc, const lact_view* vc, const int32_t* table,
+bool same_strides(const lact_paged_desc* s, const lact_view* x, const lact_view* y) {
+  return s->pages == 0 || ((s->pages == 1 || x->batch == y->batch) && (s->Hkv == 1 || x->head == y->head) &&
+                           (s->page == 1 || x->token == y->token));
+}
+
+int check_cache(const lact_paged_desc* s, int es, const lact_view* kc, const lact_view* vc, const int32_t* table,
                 const int32_t* lens, const int32_t* cu, bool out) {
-  const int es = elem(s->io_dtype);
   LACT_TRY(check_view(kc, s->pages, s->Hkv, s->page, s->d, es, out));
   LACT_TRY(check_view(vc, s->pages, s->Hkv, s->page, s->d, es, out));
-  if (s->pages > 0 && ((s->pages > 1 && kc->batch != vc->batch) || (s->Hkv > 1 && kc->head != vc->head) ||
-                       (s->page > 1 && kc->token != vc->token)))
-    return LACT_EINVAL;
+  if (!same_strides(s, kc, vc)) return LACT_EINVAL;
   if (!lens || !cu || (s->max_pages > 0 && !table)) return LACT_EINVAL;
   if (((uintptr_t)table & 3) || ((uintptr_t)lens & 3) || ((uintptr_t)cu & 3)) return LACT_EALIGN;
   return LACT_OK;
@@ -200,9 +202,8 @@ void divider(int d, uint32_t* mul, uint32_t* shift) {
   *mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << s) - d)) / d + 1);
 }
 
-PagedArgs paged_args(const lact_paged_desc* s) {
+void fill_paged(PagedArgs& a, const lact_paged_desc* s) {
   const int64_t far = (int64_t)1 << 30;
-  PagedArgs a{};
   a.B = s->B;
   a.H = s->H;
   a.Hkv = s->Hkv;
@@ -217,12 +218,82 @@ PagedArgs paged_args(const lact_paged_desc* s) {
   a.sinks = (int)std::min(s->sinks, kAttnTokens);
   a.scale = s->scale;
   divider(s->page, &a.mul, &a.shift);
+}
+PagedArgs paged_args(const lact_paged_desc* s) {
+  PagedArgs a{};
+  fill_paged(a, s);
   paged_plan(a, s->io_dtype == LACT_IO_BF16);
   return a;
 }
 
 size_t paged_bytes(const PagedArgs& a) {
   return a.splits > 1 ? ws_round((size_t)a.splits * a.T * a.H * (a.d + 2) * 4) : 0;
+}
+
+// ---------------------------------------------------------------- pages of e4m3 numbers, prefixes
+// A cache of e4m3 numbers: vectors of d bytes, which the kernels move 16 at a
+// time, and a byte for each.
+int check_codes(const lact_paged_desc* s, const lact_view* kc, const lact_view* vc, const lact_view* ks,
+                const lact_view* vs, const int32_t* table, const int32_t* lens, const int32_t* cu, bool out) {
+  if (s->d % 16) return LACT_EUNSUPPORTED;
+  LACT_TRY(check_cache(s, 1, kc, vc, table, lens, cu, out));
+  LACT_TRY(check_view(ks, s->pages, s->Hkv, s->page, 1, 0, out));
+  LACT_TRY(check_view(vs, s->pages, s->Hkv, s->page, 1, 0, out));
+  return same_strides(s, ks, vs) ? LACT_OK : LACT_EINVAL;
+}
+
+int check_prefix(const lact_paged_desc* s, const lact_prefix* p) {
+  LACT_TRY(check_paged(s, true));
+  if (!p || p->groups < 1 || p->max_pages < 0) return LACT_EINVAL;
+  // (positions behind a prefix count its keys)
+  if ((int64_t)p->groups * s->Hkv > (1 << 20) || ((int64_t)p->max_pages + s->max_pages) * s->page > kAttnTokens)
+    return LACT_EUNSUPPORTED;
+  return LACT_OK;
+}
+
+PrefixArgs prefix_args(const lact_paged_desc* s, const lact_prefix* p) {
+  PrefixArgs a{};
+  fill_paged(a, s);
+  if (p) {
+    a.P = p->groups;
+    a.p_pages = s->pages > 0 ? p->max_pages : 0;
+    a.ptable = p->table;
+    a.plen = p->lens;
+    a.cu_seq = p->cu_seq;
+  }
+  prefix_plan(a, s->io_dtype == LACT_IO_BF16);
+  return a;
+}
+
+size_t prefix_bytes(const PrefixArgs& a) {
+  const int parts = a.psplits + a.splits;
+  return parts > 1 ? ws_round((size_t)parts * a.T * a.H * (a.d + 2) * 4) : 0;
+}
+
+CodeArgs code_args(const lact_paged_desc* s, const lact_view* k, const lact_view* v, const lact_view* kc,
+                   const lact_view* vc, const lact_view* ks, const lact_view* vs, const int32_t* table,
+                   const int32_t* lens, const int32_t* cu) {
+  CodeArgs a{};
+  a.k = take(k, 1, s->Hkv, s->n_new);
+  a.v = take(v, 1, s->Hkv, s->n_new);
+  a.c = take(kc, s->pages, s->Hkv, s->page);
+  a.cs = take(ks, s->pages, s->Hkv, s->page);
+  a.kc = static_cast<uint8_t*>(kc->data);
+  a.vc = static_cast<uint8_t*>(vc->data);
+  a.ks = static_cast<uint8_t*>(ks->data);
+  a.vs = static_cast<uint8_t*>(vs->data);
+  a.table = table;
+  a.len = lens;
+  a.cu = cu;
+  a.B = s->B;
+  a.Hkv = s->Hkv;
+  a.d = s->d;
+  a.T = (int)s->n_new;
+  a.page = s->page;
+  a.max_pages = s->pages > 0 ? s->max_pages : 0;
+  a.pages = (int)s->pages;
+  divider(s->page, &a.mul, &a.shift);
+  return a;
 }
 
 int check_workspace(size_t need, const void* workspace, size_t bytes) {
@@ -245,6 +316,31 @@ int go(int kclass, const A& a, bool bf16, void* stream) {
         return F(x->a, x->bf16, x->s);
       },
       &c);
+}
+
+int check_rows(const lact_paged_desc* s, const lact_view* q, const lact_view* o) {
+  const int es = elem(s->io_dtype);
+  LACT_TRY(check_view(q, 1, s->H, s->n_new, s->d, es, false));
+  return check_view(o, 1, s->H, s->n_new, s->d, es, true);
+}
+
+// The launch of a checked call; `a` has its plan, its prefixes and its scales.
+int attend(const lact_paged_desc* s, PrefixArgs& a, bool codes, const lact_view* q, const lact_view* kc, const lact_view* vc,
+           const int32_t* table, const int32_t* lens, const int32_t* cu, const lact_view* o, void* workspace,
+           size_t bytes, void* stream) {
+  LACT_TRY(check_workspace(prefix_bytes(a), workspace, bytes));
+  if (s->n_new == 0) return LACT_OK;
+  a.codes = codes;
+  a.q = take(q, 1, s->H, s->n_new);
+  a.o = take(o, 1, s->H, s->n_new);
+  a.c = take(kc, s->pages, s->Hkv, s->page);
+  a.kc = kc->data;
+  a.vc = vc->data;
+  a.table = table;
+  a.len = lens;
+  a.cu = cu;
+  a.part = static_cast<float*>(workspace);
+  return go<PrefixArgs, launch_prefix>(LACT_KCLASS_ATTN, a, s->io_dtype == LACT_IO_BF16, stream);
 }
 
 }  // namespace
@@ -393,7 +489,7 @@ int lact_paged_append(const lact_paged_desc* desc, const lact_view* k, const lac
   const int es = elem(s.io_dtype);
   LACT_TRY(check_view(k, 1, s.Hkv, s.n_new, s.d, es, false));
   LACT_TRY(check_view(v, 1, s.Hkv, s.n_new, s.d, es, false));
-  LACT_TRY(check_cache(desc, k_cache, v_cache, table, lens, cu_new, true));
+  LACT_TRY(check_cache(desc, es, k_cache, v_cache, table, lens, cu_new, true));
   if (s.n_new == 0 || s.pages == 0 || s.max_pages == 0) return LACT_OK;
   AppendArgs a{};
   a.k = take(k, 1, s.Hkv, s.n_new);
@@ -429,7 +525,7 @@ int lact_paged_attention(const lact_paged_desc* desc, const lact_view* q, const 
   const int es = elem(s.io_dtype);
   LACT_TRY(check_view(q, 1, s.H, s.n_new, s.d, es, false));
   LACT_TRY(check_view(o, 1, s.H, s.n_new, s.d, es, true));
-  LACT_TRY(check_cache(desc, k_cache, v_cache, table, lens, cu_new, false));
+  LACT_TRY(check_cache(desc, es, k_cache, v_cache, table, lens, cu_new, false));
   PagedArgs a = paged_args(desc);
   LACT_TRY(check_workspace(paged_bytes(a), workspace, workspace_bytes));
   if (s.n_new == 0) return LACT_OK;
@@ -443,6 +539,84 @@ int lact_paged_attention(const lact_paged_desc* desc, const lact_view* q, const 
   a.cu = cu_new;
   a.part = static_cast<float*>(workspace);
   return go<PagedArgs, launch_paged>(LACT_KCLASS_ATTN, a, s.io_dtype == LACT_IO_BF16, stream);
+}
+
+int lact_paged_append_e4m3(const lact_paged_desc* desc, const lact_view* k, const lact_view* v,
+                           const lact_view* k_cache, const lact_view* v_cache, const lact_view* k_scale,
+                           const lact_view* v_scale, const int32_t* table, const int32_t* lens, const int32_t* cu_new,
+                           void* stream) {
+  LACT_TRY(check_paged(desc, false));
+  const lact_paged_desc& s = *desc;
+  const int es = elem(s.io_dtype);
+  LACT_TRY(check_view(k, 1, s.Hkv, s.n_new, s.d, es, false));
+  LACT_TRY(check_view(v, 1, s.Hkv, s.n_new, s.d, es, false));
+  LACT_TRY(check_codes(desc, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, true));
+  if (s.n_new == 0 || s.pages == 0 || s.max_pages == 0) return LACT_OK;
+  const CodeArgs a = code_args(desc, k, v, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new);
+  return go<CodeArgs, launch_append_e4m3>(LACT_KCLASS_IO, a, s.io_dtype == LACT_IO_BF16, stream);
+}
+
+int lact_paged_read_e4m3(const lact_paged_desc* desc, const lact_view* k_cache, const lact_view* v_cache,
+                         const lact_view* k_scale, const lact_view* v_scale, const int32_t* table, const int32_t* lens,
+                         const int32_t* cu_new, const lact_view* k, const lact_view* v, void* stream) {
+  LACT_TRY(check_paged(desc, false));
+  const lact_paged_desc& s = *desc;
+  const int es = elem(s.io_dtype);
+  LACT_TRY(check_codes(desc, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, false));
+  LACT_TRY(check_view(k, 1, s.Hkv, s.n_new, s.d, es, true));
+  LACT_TRY(check_view(v, 1, s.Hkv, s.n_new, s.d, es, true));
+  if (s.n_new == 0) return LACT_OK;
+  const CodeArgs a = code_args(desc, k, v, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new);
+  return go<CodeArgs, launch_read_e4m3>(LACT_KCLASS_IO, a, s.io_dtype == LACT_IO_BF16, stream);
+}
+
+size_t lact_paged_attention_e4m3_workspace_bytes(const lact_paged_desc* desc, int* err) {
+  int rc = check_paged(desc, true);
+  if (!rc && desc->d % 16) rc = LACT_EUNSUPPORTED;
+  if (err) *err = rc;
+  return rc ? 0 : prefix_bytes(prefix_args(desc, nullptr));
+}
+
+int lact_paged_attention_e4m3(const lact_paged_desc* desc, const lact_view* q, const lact_view* k_cache,
+                              const lact_view* v_cache, const lact_view* k_scale, const lact_view* v_scale,
+                              const int32_t* table, const int32_t* lens, const int32_t* cu_new, const lact_view* o,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  LACT_TRY(check_paged(desc, true));
+  LACT_TRY(check_rows(desc, q, o));
+  LACT_TRY(check_codes(desc, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, false));
+  PrefixArgs a = prefix_args(desc, nullptr);
+  a.ks = static_cast<const uint8_t*>(k_scale->data);
+  a.vs = static_cast<const uint8_t*>(v_scale->data);
+  a.cs = take(k_scale, desc->pages, desc->Hkv, desc->page);
+  return attend(desc, a, true, q, k_cache, v_cache, table, lens, cu_new, o, workspace, workspace_bytes, stream);
+}
+
+size_t lact_paged_prefix_attention_workspace_bytes(const lact_paged_desc* desc, const lact_prefix* prefix, int* err) {
+  const int rc = check_prefix(desc, prefix);
+  if (err) *err = rc;
+  return rc ? 0 : prefix_bytes(prefix_args(desc, prefix));
+}
+
+int lact_paged_prefix_attention(const lact_paged_desc* desc, const lact_prefix* prefix, const lact_view* q,
+                                const lact_view* k_cache, const lact_view* v_cache, const lact_view* k_scale,
+                                const lact_view* v_scale, const int32_t* table, const int32_t* lens,
+                                const int32_t* cu_new, const lact_view* o, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  LACT_TRY(check_prefix(desc, prefix));
+  LACT_TRY(check_rows(desc, q, o));
+  const bool codes = k_scale || v_scale;
+  LACT_TRY(codes ? check_codes(desc, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, false)
+                 : check_cache(desc, elem(desc->io_dtype), k_cache, v_cache, table, lens, cu_new, false));
+  if (!prefix->lens || !prefix->cu_seq || (prefix->max_pages > 0 && !prefix->table)) return LACT_EINVAL;
+  if (((uintptr_t)prefix->table & 3) || ((uintptr_t)prefix->lens & 3) || ((uintptr_t)prefix->cu_seq & 3))
+    return LACT_EALIGN;
+  PrefixArgs a = prefix_args(desc, prefix);
+  if (codes) {
+    a.ks = static_cast<const uint8_t*>(k_scale->data);
+    a.vs = static_cast<const uint8_t*>(v_scale->data);
+    a.cs = take(k_scale, desc->pages, desc->Hkv, desc->page);
+  }
+  return attend(desc, a, codes, q, k_cache, v_cache, table, lens, cu_new, o, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

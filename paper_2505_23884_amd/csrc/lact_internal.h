@@ -573,6 +573,35 @@ struct PagedArgs {
 void paged_plan(PagedArgs& a, bool bf16);   // splits and wide, from the sizes
 hipError_t launch_paged(const PagedArgs& a, bool bf16, hipStream_t s);
 
+// The same over a cache of any kind, with sequences in groups that share a
+// prefix: group g is sequences cu_seq[g] .. cu_seq[g + 1] - 1, behind plen[g]
+// keys on pages of its own. Workgroups of two roles in one launch: the first
+// `pjobs` take the rows of groups over the prefixes, the others those of
+// sequences over their own keys.
+struct PrefixArgs : PagedArgs {
+  const uint8_t *ks, *vs;    // e4m3: exponents of the scales (page, head, slot) by cs
+  AttnView cs;
+  const int32_t *ptable, *plen, *cu_seq;
+  int P, p_pages;            // groups (0: none), pages of a prefix's row in ptable
+  int psplits, pjobs;        // parts of the prefixes (0: none); `splits` are those of the sequences' own keys
+  bool pwide, codes;         // codes: a cache of e4m3 numbers
+};
+void prefix_plan(PrefixArgs& a, bool bf16);
+hipError_t launch_prefix(const PrefixArgs& a, bool bf16, hipStream_t s);
+
+// Keys and values to and from a cache of e4m3 numbers (append: k, v read;
+// read back: k, v written).
+struct CodeArgs {
+  AttnView k, v;             // [token][head] rows
+  uint8_t *kc, *vc, *ks, *vs;
+  AttnView c, cs;
+  const int32_t *table, *len, *cu;
+  int B, Hkv, d, T, page, max_pages, pages;
+  uint32_t mul, shift;
+};
+hipError_t launch_append_e4m3(const CodeArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_read_e4m3(const CodeArgs& a, bool bf16, hipStream_t s);
+
 struct AppendArgs {
   AttnView k, v;         // [token][head] rows
   void *kc, *vc;

@@ -30,151 +30,12 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "lact_attn.h"
-#include "lact_internal.h"
+#include "lact_paged.h"
 
 namespace lact {
 namespace {
 
 using namespace attn;
-
-constexpr int kWaves = 4;
-constexpr int kKT = 32;   // keys a tile
-
-// The rows of sequence b: `rows` of them, of tokens t0 .., the first at position p0.
-struct Seq {
-  int b, t0, rows, p0, len;
-};
-
-__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
-
-template <class Args>
-__device__ __forceinline__ int seq_len(const Args& a, int b) {
-  return clampi(a.len[b], 0, a.max_pages * a.page);
-}
-
-// Row tile `t` of R rows. Up to 64 sequences stand a lane each, in the order of
-// the keys they see, most first: what is left for the end, or comes as a
-// second workgroup to a CU, is short. More than that stand in their own order,
-// sequence b from tile cu[b] G / R + b on (rounded down, so that each has room
-// for its last partial tile). Tiles past the last one are empty.
-__device__ __forceinline__ bool find_rows(const PagedArgs& a, int t, int R, Seq& s, int& r0) {
-  int count, k;
-  if (a.B <= 64) {
-    const int lane = threadIdx.x & 63, b = min(lane, a.B - 1);
-    const int t0 = clampi(a.cu[b], 0, a.T), t1 = a.cu[b + 1], len = seq_len(a, b);
-    const int n = lane < a.B ? clampi(t1, t0, a.T) - t0 : 0, tiles = (int)(((int64_t)n * a.G + R - 1) / R);
-    const int keys = min(len, a.win);
-    int start = 0;
-    for (int j = 0; j < a.B; ++j) {
-      const int kj = __builtin_amdgcn_readlane(keys, j), nj = __builtin_amdgcn_readlane(tiles, j);
-      start += (kj > keys) | ((kj == keys) & (j < lane)) ? nj : 0;
-    }
-    const uint64_t mine = __ballot(t >= start && t - start < tiles);
-    if (!mine) return false;
-    s.b = __builtin_ctzll(mine);
-    s.t0 = __builtin_amdgcn_readlane(t0, s.b);
-    s.len = __builtin_amdgcn_readlane(len, s.b);
-    count = __builtin_amdgcn_readlane(n, s.b);
-    k = t - __builtin_amdgcn_readlane(start, s.b);
-  } else {
-    int lo = 0, hi = a.B - 1;
-    auto first = [&](int b) { return (int)((int64_t)clampi(a.cu[b], 0, a.T) * a.G / R) + b; };
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (first(mid) <= t) lo = mid;
-      else hi = mid - 1;
-    }
-    s.b = lo;
-    s.t0 = clampi(a.cu[lo], 0, a.T);
-    s.len = seq_len(a, lo);
-    count = clampi(a.cu[lo + 1], s.t0, a.T) - s.t0;
-    k = t - first(lo);
-  }
-  s.rows = count * a.G;
-  s.p0 = s.len - count;
-  if (k < 0 || (int64_t)k * R >= s.rows) return false;
-  r0 = k * R;
-  return true;
-}
-
-__device__ __forceinline__ int page_of(int key, uint32_t mul, uint32_t shift) {
-  return (int)((__umulhi((uint32_t)key, mul) + (uint32_t)key) >> shift);
-}
-
-// Where lane l's key k0 + l lies: its offset in elements, < 0 if it is past
-// the length or its page is no page of the cache.
-template <class Args>
-__device__ __forceinline__ int64_t slot_of(const Args& a, const int32_t* table, int key, int len) {
-  if (key < 0 || key >= len) return -1;
-  const int pi = page_of(key, a.mul, a.shift), pg = table[pi];
-  if (pg < 0 || pg >= a.pages) return -1;
-  return pg * a.c.sb + (key - pi * a.page) * a.c.st;
-}
-
-__device__ __forceinline__ int64_t shfl64(int64_t x, int lane) {
-  const int lo = __shfl((int)x, lane, 64), hi = __shfl((int)(x >> 32), lane, 64);
-  return ((int64_t)hi << 32) | (uint32_t)lo;
-}
-
-// A tile of kKT keys and values through the registers of NT threads; `at` is
-// each wave's slot_of() of the tile's keys (lane = key).
-template <typename T, int DP, int NT>
-struct PagedStage {
-  using L = Tile<T, DP>;
-  static constexpr int N = kKT * L::CPR / NT, STEP = NT / L::CPR;
-  static_assert(N >= 1 && kKT * L::CPR % NT == 0 && NT % L::CPR == 0, "tile split");
-  u32x4 k[N], v[N];
-  __device__ __forceinline__ void load(const T* kb, const T* vb, int64_t at, int d) {
-    const int row = threadIdx.x % NT / L::CPR, e = threadIdx.x % L::CPR * L::E;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int64_t o = shfl64(at, row + i * STEP);
-      const bool ok = o >= 0 && e < d;
-      k[i] = ok ? *reinterpret_cast<const u32x4*>(kb + o + e) : u32x4{};
-      v[i] = ok ? *reinterpret_cast<const u32x4*>(vb + o + e) : u32x4{};
-    }
-  }
-  // an infinity or NaN among the values; the values without them
-  __device__ __forceinline__ bool any_nonfinite() const {
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < N; ++i) bad |= nonfinite<T>(v[i]);
-    return bad;
-  }
-  __device__ __forceinline__ void scrub() {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) v[i][x] = finite_or_zero<T>(v[i][x]);
-  }
-  __device__ __forceinline__ void store(uint8_t* kt, uint8_t* vt) const {
-    const int row = threadIdx.x % NT / L::CPR, c = threadIdx.x % L::CPR;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      *reinterpret_cast<u32x4*>(kt + L::off(row + i * STEP, c)) = k[i];
-      *reinterpret_cast<u32x4*>(vt + L::off(row + i * STEP, c)) = v[i];
-    }
-  }
-};
-
-__device__ __forceinline__ void wave_fence() {   // LDS of one wave: its instructions run in order
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
-// The infinities and NaN of a scrubbed tile (offsets `at` of its keys, a lane
-// each) to the rows that see them: the sight counts from the lane's first row
-// of the tile, key j is row j - 4 (lane / 32) there, which may be below 0.
-template <typename T, int DP>
-__device__ __forceinline__ void restore_nonfinite(Softmax<DP / 32>& st, const T* vb, int64_t at, int d,
-                                                  const Sight& sight) {
-#pragma unroll 1
-  for (int j = 0; j < kKT; ++j) {
-    const int64_t o = shfl64(at, j);
-    if (o >= 0) add_nonfinite<T, DP / 32>(st.o, vb + o, sight.see(j - 4 * (int)((threadIdx.x >> 5) & 1)), 0, d);
-  }
-}
 
 // What a workgroup and its lane work on.
 struct RowOf {
@@ -205,9 +66,6 @@ __device__ __forceinline__ void finish(const PagedArgs& a, const RowOf& row, int
   if (row.ok && lane < 32)
     *reinterpret_cast<f32x2*>(a.part + (int64_t)a.splits * rows * a.d + at * 2) = f32x2{st.m, l};
 }
-
-// 16 bytes of zeros for the lanes of a copy that have nothing to read.
-__device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
 
 template <typename T, int DP, int KT, int OCC>
 __global__ __launch_bounds__(64 * kWaves, OCC) void k_paged_wide(const PagedArgs a) {
