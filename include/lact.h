@@ -760,7 +760,8 @@ typedef struct lact_prefix {
   const int32_t *lens;      /* int32 [groups]                                   */
   const int32_t *cu_seq;    /* int32 [groups + 1]                               */
 } lact_prefix;
-size_t lact_paged_prefix_attention_workspace_bytes(const lact_paged_desc* desc, const lact_prefix* prefix, int* err);
+size_t lact_paged_prefix_attention_workspace_bytes(const lact_paged_desc* desc, const lact_prefix* prefix, int e4m3,
+                                                   int* err);   /* e4m3: whether the cache is one of e4m3 numbers */
 int lact_paged_prefix_attention(const lact_paged_desc* desc, const lact_prefix* prefix, const lact_view* q,
                                 const lact_view* k_cache, const lact_view* v_cache, const lact_view* k_scale,
                                 const lact_view* v_scale, const int32_t* table, const int32_t* lens,

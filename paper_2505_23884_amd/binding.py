@@ -139,7 +139,7 @@ def load_library(path: str | None = None):
     L.lact_paged_read_e4m3.argtypes = [pp] + [vw] * 4 + [vp] * 3 + [vw, vw, vp]
     L.lact_paged_attention_e4m3.argtypes = [pp] + [vw] * 5 + [vp] * 3 + [vw, vp, sz, vp]
     L.lact_paged_prefix_attention.argtypes = [pp, xp] + [vw] * 5 + [vp] * 3 + [vw, vp, sz, vp]
-    L.lact_paged_prefix_attention_workspace_bytes.argtypes = [pp, xp, ip]
+    L.lact_paged_prefix_attention_workspace_bytes.argtypes = [pp, xp, i32, ip]
     L.lact_paged_prefix_attention_workspace_bytes.restype = sz
     for f in ("lact_qk_norm_rope", "lact_qk_norm_rope_backward", "lact_window_attention",
               "lact_window_attention_backward", "lact_paged_append", "lact_paged_attention", "lact_paged_append_e4m3",
@@ -1201,7 +1201,8 @@ def paged_prefix_attention(q, k_cache, v_cache, prefix_table, prefix_lens, cu_se
     s = (T, H, d)
     qv = _view_n(q, "q", s, dt, dev)
     o = _new(q, s, stream, torch) if out is None else out
-    workspace, wp, nb = _workspace("lact_paged_prefix_attention_workspace_bytes", desc, workspace, q, stream, torch, prefix)
+    workspace, wp, nb = _workspace("lact_paged_prefix_attention_workspace_bytes", desc, workspace, q, stream, torch, prefix,
+                                   int(k_scale is not None))
     _call("lact_paged_prefix_attention", dev, stream, torch, desc, prefix, qv, *tail, _view_n(o, "o", s, dt, dev), wp, nb)
     return o
 

@@ -12,7 +12,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liblact.so")
 SOURCES = ["lact_api.hip", "lact_kernels.hip", "lact_io.hip", "lact_attn_api.hip", "lact_window.hip", "lact_paged.hip",
-           "lact_rope.hip", "lact_codes.hip", "lact_prefix.hip"]
+           "lact_rope.hip", "lact_codes.hip", "lact_prefix.hip", "lact_prefix_bf16.hip",
+           "lact_prefix_e4m3.hip", "lact_prefix_e4m3_fp32.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -32,7 +33,7 @@ def hipcc() -> str:
 def build(verbose: bool = False) -> str:
     """Compile every HIP source (side by side) and link liblact.so next to this file; returns its path."""
     tmp = LIB + ".tmp"
-    with tempfile.TemporaryDirectory() as objs, ThreadPoolExecutor(max_workers=4) as pool:
+    with tempfile.TemporaryDirectory() as objs, ThreadPoolExecutor(max_workers=8) as pool:
         def run(cmd):
             if verbose:
                 print(" ".join(cmd), flush=True)

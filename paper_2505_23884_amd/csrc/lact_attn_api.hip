@@ -251,7 +251,7 @@ int check_prefix(const lact_paged_desc* s, const lact_prefix* p) {
   return LACT_OK;
 }
 
-PrefixArgs prefix_args(const lact_paged_desc* s, const lact_prefix* p) {
+PrefixArgs prefix_args(const lact_paged_desc* s, const lact_prefix* p, bool codes) {
   PrefixArgs a{};
   fill_paged(a, s);
   if (p) {
@@ -261,7 +261,8 @@ PrefixArgs prefix_args(const lact_paged_desc* s, const lact_prefix* p) {
     a.plen = p->lens;
     a.cu_seq = p->cu_seq;
   }
-  prefix_plan(a, s->io_dtype == LACT_IO_BF16);
+  a.codes = codes;
+  prefix_plan(a, s->io_dtype == LACT_IO_BF16, codes);
   return a;
 }
 
@@ -325,12 +326,11 @@ int check_rows(const lact_paged_desc* s, const lact_view* q, const lact_view* o)
 }
 
 // The launch of a checked call; `a` has its plan, its prefixes and its scales.
-int attend(const lact_paged_desc* s, PrefixArgs& a, bool codes, const lact_view* q, const lact_view* kc, const lact_view* vc,
+int attend(const lact_paged_desc* s, PrefixArgs& a, const lact_view* q, const lact_view* kc, const lact_view* vc,
            const int32_t* table, const int32_t* lens, const int32_t* cu, const lact_view* o, void* workspace,
            size_t bytes, void* stream) {
   LACT_TRY(check_workspace(prefix_bytes(a), workspace, bytes));
   if (s->n_new == 0) return LACT_OK;
-  a.codes = codes;
   a.q = take(q, 1, s->H, s->n_new);
   a.o = take(o, 1, s->H, s->n_new);
   a.c = take(kc, s->pages, s->Hkv, s->page);
@@ -574,7 +574,7 @@ size_t lact_paged_attention_e4m3_workspace_bytes(const lact_paged_desc* desc, in
   int rc = check_paged(desc, true);
   if (!rc && desc->d % 16) rc = LACT_EUNSUPPORTED;
   if (err) *err = rc;
-  return rc ? 0 : prefix_bytes(prefix_args(desc, nullptr));
+  return rc ? 0 : prefix_bytes(prefix_args(desc, nullptr, true));
 }
 
 int lact_paged_attention_e4m3(const lact_paged_desc* desc, const lact_view* q, const lact_view* k_cache,
@@ -584,17 +584,18 @@ int lact_paged_attention_e4m3(const lact_paged_desc* desc, const lact_view* q, c
   LACT_TRY(check_paged(desc, true));
   LACT_TRY(check_rows(desc, q, o));
   LACT_TRY(check_codes(desc, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, false));
-  PrefixArgs a = prefix_args(desc, nullptr);
+  PrefixArgs a = prefix_args(desc, nullptr, true);
   a.ks = static_cast<const uint8_t*>(k_scale->data);
   a.vs = static_cast<const uint8_t*>(v_scale->data);
   a.cs = take(k_scale, desc->pages, desc->Hkv, desc->page);
-  return attend(desc, a, true, q, k_cache, v_cache, table, lens, cu_new, o, workspace, workspace_bytes, stream);
+  return attend(desc, a, q, k_cache, v_cache, table, lens, cu_new, o, workspace, workspace_bytes, stream);
 }
 
-size_t lact_paged_prefix_attention_workspace_bytes(const lact_paged_desc* desc, const lact_prefix* prefix, int* err) {
+size_t lact_paged_prefix_attention_workspace_bytes(const lact_paged_desc* desc, const lact_prefix* prefix, int e4m3,
+                                                   int* err) {
   const int rc = check_prefix(desc, prefix);
   if (err) *err = rc;
-  return rc ? 0 : prefix_bytes(prefix_args(desc, prefix));
+  return rc ? 0 : prefix_bytes(prefix_args(desc, prefix, e4m3 != 0));
 }
 
 int lact_paged_prefix_attention(const lact_paged_desc* desc, const lact_prefix* prefix, const lact_view* q,
@@ -610,13 +611,13 @@ int lact_paged_prefix_attention(const lact_paged_desc* desc, const lact_prefix* 
   if (!prefix->lens || !prefix->cu_seq || (prefix->max_pages > 0 && !prefix->table)) return LACT_EINVAL;
   if (((uintptr_t)prefix->table & 3) || ((uintptr_t)prefix->lens & 3) || ((uintptr_t)prefix->cu_seq & 3))
     return LACT_EALIGN;
-  PrefixArgs a = prefix_args(desc, prefix);
+  PrefixArgs a = prefix_args(desc, prefix, codes);
   if (codes) {
     a.ks = static_cast<const uint8_t*>(k_scale->data);
     a.vs = static_cast<const uint8_t*>(v_scale->data);
     a.cs = take(k_scale, desc->pages, desc->Hkv, desc->page);
   }
-  return attend(desc, a, codes, q, k_cache, v_cache, table, lens, cu_new, o, workspace, workspace_bytes, stream);
+  return attend(desc, a, q, k_cache, v_cache, table, lens, cu_new, o, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

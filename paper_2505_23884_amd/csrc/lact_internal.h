@@ -584,10 +584,14 @@ struct PrefixArgs : PagedArgs {
   const int32_t *ptable, *plen, *cu_seq;
   int P, p_pages;            // groups (0: none), pages of a prefix's row in ptable
   int psplits, pjobs;        // parts of the prefixes (0: none); `splits` are those of the sequences' own keys
-  bool pwide, codes;         // codes: a cache of e4m3 numbers
+  int shape, pshape;         // of the workgroups of the two roles
+  bool codes;                // a cache of e4m3 numbers
 };
-void prefix_plan(PrefixArgs& a, bool bf16);
+void prefix_plan(PrefixArgs& a, bool bf16, bool codes);
 hipError_t launch_prefix(const PrefixArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_prefix_bf16(const PrefixArgs& a, hipStream_t s);
+hipError_t launch_prefix_e4m3(const PrefixArgs& a, hipStream_t s);
+hipError_t launch_prefix_e4m3_fp32(const PrefixArgs& a, hipStream_t s);
 
 // Keys and values to and from a cache of e4m3 numbers (append: k, v read;
 // read back: k, v written).
