@@ -51,37 +51,91 @@ struct Row {
   }
 };
 
-// The groups of a call, as find_rows() takes them.
-struct Groups {
+// The offsets of a call's sequences, clamped, are brought to LDS first (those
+// of up to kOffsets sequences; of more they are read where they lie): everything that
+// a workgroup has to find then takes one round trip to memory, with the
+// offsets, lengths and groups on their way together.
+constexpr int kOffsets = 511;
+struct Offsets {
   const PrefixArgs& a;
-  __device__ __forceinline__ int count() const { return a.P; }
-  __device__ __forceinline__ int first(int g) const { return clampi(a.cu[clampi(a.cu_seq[g], 0, a.B)], 0, a.T); }
-  __device__ __forceinline__ int len(int g) const { return clampi(a.plen[g], 0, a.p_pages * a.page); }
+  const int* lds;
+  __device__ __forceinline__ Offsets(const PrefixArgs& a_, int* to) : a(a_), lds(to) {
+    if (a.B <= kOffsets)
+      for (int i = threadIdx.x; i <= a.B; i += 64 * kWaves) to[i] = clampi(a.cu[i], 0, a.T);
+  }
+  __device__ __forceinline__ int operator()(int b) const { return a.B <= kOffsets ? lds[b] : clampi(a.cu[b], 0, a.T); }
 };
 
-// The position of a token among its sequence's own keys (< 0 for one that its
-// sequence does not hold). All 64 lanes take part. Up to 64 sequences stand a
-// lane each.
-__device__ __forceinline__ int own_position(const PrefixArgs& a, int token) {
-  int b = 0, t1, len;
-  if (a.B <= 64) {
-    const int mine = min((int)(threadIdx.x & 63), a.B - 1), t0 = clampi(a.cu[mine], 0, a.T);
-    b = -1;
-    for (int j = 0; j < a.B; ++j) b += __builtin_amdgcn_readlane(t0, j) <= token;
-    b = max(b, 0);
-    t1 = __shfl(clampi(a.cu[mine + 1], 0, a.T), b, 64);
-    len = __shfl(seq_len(a, mine), b, 64);
+// What a role's rows come from: sequences, or groups of them. Its count, and
+// of item i the first token and the keys that it has.
+struct Items {
+  const PrefixArgs& a;
+  const Offsets& off;
+  bool groups;
+  __device__ __forceinline__ int count() const { return groups ? a.P : a.B; }
+  __device__ __forceinline__ int at(int i) const { return groups ? clampi(a.cu_seq[i], 0, a.B) : i; }
+  __device__ __forceinline__ int first(int i) const { return off(at(i)); }
+  __device__ __forceinline__ int len(int i) const { return groups ? clampi(a.plen[i], 0, a.p_pages * a.page) : seq_len(a, i); }
+};
+
+// Row tile `t` of R rows, as find_rows() has them: up to 64 items in the order
+// of their keys, most first; of more, item i from tile first(i) G / R + i on.
+template <bool GROUPS>
+__device__ __forceinline__ bool find_tile(const PrefixArgs& a, const Offsets& off, int t, int R, Seq& s, int& r0) {
+  const Items it{a, off, GROUPS};
+  const int n = it.count();
+  int count, k;
+  if (n <= 64) {
+    const int lane = threadIdx.x & 63, i = min(lane, n - 1);
+    const int b0 = it.at(i), b1 = it.at(i + 1), len = it.len(i);   // (loads before the offsets are waited for)
+    // rank by keys; the lane in its low bits makes each one's its own
+    const int mine = min(len, a.win) >> 5 << 6 | (63 - lane);
+    __syncthreads();
+    const int t0 = off(b0), c = lane < n ? max(off(b1), t0) - t0 : 0, tiles = (int)(((int64_t)c * a.G + R - 1) / R);
+    int start = 0;
+    for (int j = 0; j < n; ++j) {
+      const int nj = __builtin_amdgcn_readlane(tiles, j);
+      start += __builtin_amdgcn_readlane(mine, j) > mine ? nj : 0;
+    }
+    const uint64_t found = __ballot(t >= start && t - start < tiles);
+    if (!found) return false;
+    s.b = __builtin_ctzll(found);
+    s.t0 = __builtin_amdgcn_readlane(t0, s.b);
+    s.len = __builtin_amdgcn_readlane(len, s.b);
+    count = __builtin_amdgcn_readlane(c, s.b);
+    k = t - __builtin_amdgcn_readlane(start, s.b);
   } else {
-    int hi = a.B - 1;
-    while (b < hi) {
-      const int mid = (b + hi + 1) >> 1;
-      if (clampi(a.cu[mid], 0, a.T) <= token) b = mid;
+    __syncthreads();
+    int lo = 0, hi = n - 1;
+    auto first = [&](int i) { return (int)((int64_t)it.first(i) * a.G / R) + i; };
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first(mid) <= t) lo = mid;
       else hi = mid - 1;
     }
-    t1 = clampi(a.cu[b + 1], 0, a.T);
-    len = seq_len(a, b);
+    s.b = lo;
+    s.t0 = it.first(lo);
+    s.len = it.len(lo);
+    count = max(it.first(lo + 1), s.t0) - s.t0;
+    k = t - first(lo);
   }
-  return len - (t1 - token);
+  s.rows = count * a.G;
+  s.p0 = s.len - count;
+  if (k < 0 || (int64_t)k * R >= s.rows) return false;
+  r0 = k * R;
+  return true;
+}
+
+// The position of a token among its sequence's own keys (< 0 for one that its
+// sequence does not hold).
+__device__ __forceinline__ int own_position(const PrefixArgs& a, const Offsets& off, int token) {
+  int b = 0, hi = a.B - 1;
+  while (b < hi) {
+    const int mid = (b + hi + 1) >> 1;
+    if (off(mid) <= token) b = mid;
+    else hi = mid - 1;
+  }
+  return seq_len(a, b) - (off(b + 1) - token);
 }
 
 // The group of sequence b, or -1.
@@ -96,27 +150,62 @@ __device__ __forceinline__ int group_of(const PrefixArgs& a, int b) {
   return a.cu_seq[lo] <= b && b < a.cu_seq[lo + 1] ? lo : -1;
 }
 
-// Where a key lies: offsets of its vectors and of its scales, `at` < 0 if there is none.
+// A key's page, as the table has it (not looked at: the load stays in flight),
+// and its place there, < 0 if it is past the length.
+struct Place {
+  int page, at;
+  Place() = default;
+  // (only where there are keys: entry 0 of the table is read for those past them)
+  __device__ __forceinline__ Place(const PrefixArgs& a, const int32_t* table, int key, int len) {
+    const bool ok = key < len;
+    const int pi = page_of(ok ? key : 0, a.mul, a.shift);
+    page = table[pi];
+    at = ok ? key - pi * a.page : -1;
+  }
+};
+
+// Where it lies: offsets of its vectors and of its scales, `at` < 0 if there is none.
 template <class C>
 struct Slot {
   int64_t at;
-  template <class Args>
-  __device__ __forceinline__ void find(const Args& a, const int32_t* table, int key, int len) {
-    at = slot_of(a, table, key, len);
-  }
+  Slot() = default;
+  __device__ __forceinline__ Slot(const PrefixArgs& a, const Place& p)
+      : at(p.at >= 0 && p.page >= 0 && p.page < a.pages ? p.page * a.c.sb + p.at * a.c.st : -1) {}
 };
 template <>
 struct Slot<Code> {
   int64_t at, scale;
-  template <class Args>
-  __device__ __forceinline__ void find(const Args& a, const int32_t* table, int key, int len) {
-    int pg, i;
-    at = -1;
-    if (!find_slot(a, table, key, len, pg, i)) return;
-    at = pg * a.c.sb + i * a.c.st;
-    scale = pg * a.cs.sb + i * a.cs.st;
+  Slot() = default;
+  __device__ __forceinline__ Slot(const PrefixArgs& a, const Place& p) {
+    const bool ok = p.at >= 0 && p.page >= 0 && p.page < a.pages;
+    at = ok ? p.page * a.c.sb + p.at * a.c.st : -1;
+    scale = ok ? p.page * a.cs.sb + p.at * a.cs.st : 0;
   }
 };
+
+// Loads that lanes have nothing to read with go to zeros instead of around a
+// branch, behind which the compiler could not tell what is in flight and would wait
+// for all of it.
+__device__ __forceinline__ u32x4 load16(bool ok, const void* p) {
+  typedef __attribute__((address_space(1))) const u32x4 global;   // (a choice of generic pointers would count as LDS too)
+  return *(ok ? (global*)p : (global*)kZeros);
+}
+__device__ __forceinline__ int load_byte(bool ok, const uint8_t* p) {
+  typedef __attribute__((address_space(1))) const uint8_t global;
+  return *(ok ? (global*)p : (global*)kZeros);
+}
+
+// Has the compiler wait here for what is loaded in these registers, so that a
+// loop that uses them does not (it would wait for its own loads with them).
+template <class X>
+__device__ __forceinline__ void arrived(X& x) {
+  if constexpr (std::is_array<X>::value) {
+#pragma unroll
+    for (auto& y : x) arrived(y);
+  } else {
+    asm volatile("" : "+v"(x));
+  }
+}
 
 // The caches of one key head.
 template <class C>
@@ -157,17 +246,14 @@ struct Stage<T, Code, DP, KT, NT> {
   static __device__ __forceinline__ int row(int i) { return threadIdx.x % NT / CPR + i * STEP; }
   __device__ __forceinline__ void load(const Heads<Code>& h, const Slot<Code>& s, int d) {
     const int e = threadIdx.x % CPR * 16;
-    kb = vb = 127;
-    if (s.at >= 0) {
-      kb = h.ks[s.scale];
-      vb = h.vs[s.scale];
-    }
+    kb = load_byte(s.at >= 0, h.ks + s.scale);
+    vb = load_byte(s.at >= 0, h.vs + s.scale);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int64_t o = shfl64(s.at, row(i) & 63);
       const bool ok = o >= 0 && e < d && (ALL >= NT || row(i) < KT);
-      k[i] = ok ? *reinterpret_cast<const u32x4*>(h.k + o + e) : u32x4{};
-      v[i] = ok ? *reinterpret_cast<const u32x4*>(h.v + o + e) : u32x4{};
+      k[i] = load16(ok, h.k + o + e);
+      v[i] = load16(ok, h.v + o + e);
     }
   }
   // a NaN among the values, or a scale that can make an infinity of one
@@ -257,45 +343,40 @@ __device__ __forceinline__ Sights own_sights(const PrefixArgs& a, const Job& j, 
 
 // Rows of a group over its prefix: the positions are those of their sequences,
 // behind all keys. A row that its sequence does not hold stands before them.
-__device__ __forceinline__ Sights group_sights(const PrefixArgs& a, const Job& j, const Row& row, int R) {
+// wa .. wb are those of the wave's rows (of which lane l has row l % N).
+template <int N>
+__device__ __forceinline__ Sights group_sights(const PrefixArgs& a, const Offsets& off, const Job& j, const Row& row) {
   Sights s;
-  auto at = [&](int token) __attribute__((always_inline)) {
-    const int p = own_position(a, token);
-    return p < 0 ? -1 : j.len + p;
-  };
-  s.p = at(row.token);
-  s.jhi = row.ok && s.p >= 0 ? j.len - 1 : -1;
-  const int lane = threadIdx.x & 63;
+  const int p = own_position(a, off, row.token);
+  s.p = p < 0 ? -1 : j.len + p;
+  s.jhi = row.ok && p >= 0 ? j.len - 1 : -1;
   int lo = row.ok ? s.p : 1 << 30, hi = row.ok ? s.p : -1;
 #pragma unroll
-  for (int x = 1; x < 32; x *= 2) {
+  for (int x = 1; x < N; x *= 2) {
     lo = min(lo, __shfl_xor(lo, x, 64));
     hi = max(hi, __shfl_xor(hi, x, 64));
   }
   const bool some = __any(row.ok);
-  s.wa = some ? __builtin_amdgcn_readfirstlane(lo) : 1;
-  s.wb = some ? __builtin_amdgcn_readfirstlane(hi) : 0;
-  s.pa = s.wa;
-  s.pb = s.wb;
-  if (R > 32) {   // the workgroup's rows, each wave by itself
-    lo = 1 << 30;
-    hi = -1;
-    for (int r = j.r0 + lane; r - lane < min(j.r0 + R, j.rows); r += 64) {
-      const int p = at(j.t0 + min(r, j.rows - 1) / a.G);
-      if (r < j.rows) {
-        lo = min(lo, p);
-        hi = max(hi, p);
-      }
-    }
-#pragma unroll
-    for (int x = 1; x < 64; x *= 2) {
-      lo = min(lo, __shfl_xor(lo, x, 64));
-      hi = max(hi, __shfl_xor(hi, x, 64));
-    }
-    s.pa = __builtin_amdgcn_readfirstlane(lo);
-    s.pb = __builtin_amdgcn_readfirstlane(hi);
-  }
+  s.pa = s.wa = some ? __builtin_amdgcn_readfirstlane(lo) : 1;
+  s.pb = s.wb = some ? __builtin_amdgcn_readfirstlane(hi) : 0;
   return s;
+}
+// The same over the waves of a workgroup, through LDS (eight words).
+__device__ __forceinline__ void join_sights(Sights& s, int* lds) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((threadIdx.x & 63) == 0) {
+    lds[2 * wave] = s.wa <= s.wb ? s.wa : 1 << 30;
+    lds[2 * wave + 1] = s.wa <= s.wb ? s.wb : -1;
+  }
+  __syncthreads();
+  int lo = lds[0], hi = lds[1];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    lo = min(lo, lds[2 * w]);
+    hi = max(hi, lds[2 * w + 1]);
+  }
+  s.pa = __builtin_amdgcn_readfirstlane(lo);
+  s.pb = __builtin_amdgcn_readfirstlane(hi);
 }
 
 // Part `part` of a row's sums, or the output.
@@ -339,12 +420,33 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
   Softmax<DP / 32> st;
   st.init();
   const float c = a.scale * kLog2e;
-  // slots (a lane a key) run two tiles ahead of the products, the copies one
-  auto slot = [&](int x) __attribute__((always_inline)) {
-    Slot<C> s;
-    s.at = -1;
-    if (x < x1 && lane < KT) s.find(a, jb.table, kt.tile(x) * KT + lane, jb.len);
-    return s;
+  arrived(q);
+  constexpr bool PIPED = CODES && sizeof(T) == 2 && DP <= 128;
+  // (addresses as in mma_dot_add() and mma_rows(): chunks by flipping bits of the first one's)
+  typedef __attribute__((address_space(3))) const u32x4 lds_u4;
+  typedef __attribute__((address_space(3))) s16x4 lds_s4;
+  const int sl = lane & 15, vrow = 4 * (lane >> 5) + (sl >> 2), vchunk = 2 * (lane >> 4 & 1) + (sl >> 1 & 1);
+  const uint32_t kat = L::off(lane & 31, lane >> 5), vlo = L::off(vrow, vchunk) + ((sl & 1) << 3),
+                 vhi = L::off(vrow + 8, vchunk) + ((sl & 1) << 3);
+  auto read_keys = [&](u32x4 (&f)[L::KS], uint32_t t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < L::KS; ++i) f[i] = *(lds_u4*)(uintptr_t)((t + kat) ^ (uint32_t)(i << 5));
+  };
+  auto read_values = [&](u32x2 (&f)[4 * L::DB], uint32_t t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < L::DB; ++b)
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const uint32_t at = ((t + (h & 1 ? vhi : vlo)) ^ (uint32_t)(b << 6)) + (h >> 1) * 16 * L::PITCH;
+        f[4 * b + h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(uintptr_t)at));
+      }
+  };
+  // pages (a lane a key) run two tiles ahead of the products, the copies one
+  auto place = [&](int x) __attribute__((always_inline)) {
+    Place p{};
+    p.at = -1;
+    if (x < x1) p = Place(a, jb.table, lane < KT ? kt.tile(x) * KT + lane : jb.len, jb.len);
+    return p;
   };
   auto tile_of = [&](int x) __attribute__((always_inline)) { return smem + ((x - x0) & 1) * 2 * BYTES; };
   Stage<T, Code, DP, KT, NT> stage;
@@ -371,7 +473,8 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
   auto arrive = [&](int x) __attribute__((always_inline)) {
     if constexpr (CODES) stage.put(tile_of(x), tile_of(x) + BYTES, false);
   };
-  Slot<C> here = slot(x0), next = slot(x0 + 1);
+  Slot<C> here(a, place(x0));
+  Place next = place(x0 + 1);
   if (threadIdx.x == 0) *found = -1;
   if (x0 < x1) {
     copy(x0, here);
@@ -387,24 +490,71 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
     if ((!whole || sees(jb.band, jb.len, sg.pa, sg.pb, k0, KT) != 2) &&
         __builtin_expect(Cp::holds_nonfinite(ks + BYTES, x, found), 0))
       bad = Cp::scrub(ks + BYTES, mask);
-    if (x + 1 < x1) copy(x + 1, next);
-    const Slot<C> after = slot(x + 2);
+    const Slot<C> then(a, next);
+    if (x + 1 < x1) copy(x + 1, then);
+    next = place(x + 2);
     const Sight sight(jb.band, sg.p, sg.jhi, k0);
     const uint64_t mine = there >> (4 * (lane >> 5));
     auto see = [&](int r) __attribute__((always_inline)) { return sight.see(r) && (mine >> r & 1); };
-    auto step = [&](auto rb) __attribute__((always_inline)) {
-      constexpr int RB = decltype(rb)::value;
-      const int what = sees(jb.band, jb.len, sg.wa, sg.wb, k0 + RB, 32);
-      if (what) softmax_step<T, DP, RB>(st, q, ks, ks + BYTES, c, what == 1 || !whole, see);
-    };
-    step(std::integral_constant<int, 0>{});
-    if constexpr (KT == 64) step(std::integral_constant<int, 32>{});
+    if constexpr (PIPED) {
+      // keys of the first 32, then in turn: values of a step while its scores are
+      // worked out, keys of the next one while its weights are
+      u32x4 kf[L::KS];
+      read_keys(kf, lds_addr(ks));
+#pragma unroll
+      for (int rb = 0; rb < KT; rb += 32) {
+        const int what = sees(jb.band, jb.len, sg.wa, sg.wb, k0 + rb, 32);
+        u32x2 vf[4 * L::DB];
+        read_values(vf, lds_addr(ks) + BYTES + rb * L::PITCH);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 s = {};
+#pragma unroll
+        for (int i = 0; i < L::KS; ++i) mma_chunk<T>(s, kf[i], q[i]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (rb + 32 < KT) read_keys(kf, lds_addr(ks) + (rb + 32) * L::PITCH);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!what) continue;
+        if (what == 1 || !whole) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!see(rb + 8 * (i >> 2) + (i & 3))) s[i] = neg_inf();
+        }
+        float mx = neg_inf();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        if (__any(mx * c > st.m + 8.0f)) st.grow(half_max(mx) * c);
+        const float m = st.m == neg_inf() ? 0.0f : st.m;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -m));
+          sum += s[i];
+        }
+        st.l += sum;
+        const RowsB<T> w(s);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int b = 0; b < L::DB; ++b) {
+            const u32x2 lo = vf[4 * b + 2 * h], hi = vf[4 * b + 2 * h + 1];
+            mma_chunk<T>(st.o[b], u32x4{lo[0], lo[1], hi[0], hi[1]}, w.v[h]);
+          }
+      }
+    } else {
+      auto step = [&](auto rb) __attribute__((always_inline)) {
+        constexpr int RB = decltype(rb)::value;
+        const int what = sees(jb.band, jb.len, sg.wa, sg.wb, k0 + RB, 32);
+        if (what) softmax_step<T, DP, RB>(st, q, ks, ks + BYTES, c, what == 1 || !whole, see);
+      };
+      step(std::integral_constant<int, 0>{});
+      if constexpr (KT == 64) step(std::integral_constant<int, 32>{});
+    }
 #pragma unroll 1
     for (; __builtin_expect(bad != 0, 0); bad &= bad - 1)
       restore_key<T, C, DP>(st, hd, here, __builtin_ctzll(bad), a.d, sight);
     if (x + 1 < x1) arrive(x + 1);
-    here = next;
-    next = after;
+    here = then;
     __syncthreads();
   }
   const float l = half_sum(st.l);
@@ -435,19 +585,20 @@ __device__ __forceinline__ void narrow(const PrefixArgs& a, const Job& jb, const
   const float c = a.scale * kLog2e;
   uint8_t* ks = smem + wave * WAVE;
   Stage<T, C, DP, kKT, 64> stage;
-  auto slot = [&](int x) __attribute__((always_inline)) {
-    Slot<C> s;
-    s.at = -1;
-    if (x < x1 && lane < kKT) s.find(a, jb.table, kt.tile(x) * kKT + lane, jb.len);
-    return s;
+  auto place = [&](int x) __attribute__((always_inline)) {
+    Place p{};
+    p.at = -1;
+    if (x < x1) p = Place(a, jb.table, lane < kKT ? kt.tile(x) * kKT + lane : jb.len, jb.len);
+    return p;
   };
   int x = x0 + wave;
-  Slot<C> at = slot(x);
+  Slot<C> at(a, place(x));
+  Place next = place(x + kWaves);
   if (x < x1) stage.load(hd, at, a.d);
   for (; x < x1; x += kWaves) {
     const Slot<C> here = at;
     const uint32_t there = (uint32_t)__ballot(here.at >= 0);
-    at = slot(x + kWaves);
+    at = Slot<C>(a, next);
     const int k0 = kt.tile(x) * kKT;
     const int what = there == 0xffffffffu ? sees(jb.band, jb.len, sg.wa, sg.wb, k0, kKT) : 1;
     const bool scrubbed = what == 1 && __any(stage.any_nonfinite());
@@ -455,6 +606,7 @@ __device__ __forceinline__ void narrow(const PrefixArgs& a, const Job& jb, const
     stage.put(ks, ks + BYTES, scrubbed);
     wave_fence();
     if (x + kWaves < x1) stage.load(hd, at, a.d);
+    next = place(x + 2 * kWaves);
     const Sight sight(jb.band, sg.p, sg.jhi, k0);
     const uint32_t mine = there >> (4 * (lane >> 5));
     auto see = [&](int r) __attribute__((always_inline)) { return sight.see(r) && (mine >> r & 1); };
@@ -521,16 +673,21 @@ __device__ __forceinline__ void narrow(const PrefixArgs& a, const Job& jb, const
 //
 // With fp32 queries (over e4m3 numbers, which are numbers of bf16) queries and
 // weights are three bf16 parts each, which hold all their bits.
-template <typename T, class C, int DP, int NR>
+//
+// HP key heads stand beside each other in a workgroup's tiles: two of 64 e4m3
+// numbers, which share lines of memory where heads lie behind slots (decoding of 64
+// sequences of up to 16384, heads of 64: 149 us one by one, PAIRED_US in pairs).
+template <typename T, class C, int DP, int NR, int HP>
 struct Slim {
   static constexpr bool CODES = std::is_same<C, Code>::value;
   static constexpr int ES = CODES ? 1 : 2, CH = 16 / ES;       // bytes an element, elements a chunk of 16 bytes
-  static constexpr int PITCH = DP * ES, CPR = DP / CH, LK = CPR / 4;   // chunks a row, and of a key a lane
+  static constexpr int CPH = DP / CH, LK = CPH / 4;            // chunks of a head's key, and of that a lane
+  static constexpr int PITCH = HP * DP * ES, CPR = HP * CPH, NY = NR * HP;
   static constexpr int ST = DP / 32, DB = DP / 16;
   static constexpr int NQ = sizeof(T) == 4 ? 3 : 1, NP = sizeof(T) == 4 ? 3 : 2;
-  static constexpr int VB = 32 * PITCH, WAVE = 2 * VB + 256, SUMS = NR * (4 * DB + 2) * 256;
+  static constexpr int VB = 32 * PITCH, WAVE = 2 * VB + 256 * HP, SUMS = NY * (4 * DB + 2) * 256;
   static constexpr int SMEM = kWaves * WAVE > 2 * SUMS ? kWaves * WAVE : 2 * SUMS;
-  static_assert(CPR >= 4, "four chunks a row at least");
+  static_assert(CPH >= 4, "four chunks a head at least");
 
   // The row of LDS that a key's values have, and its chunks' order: the 16
   // lanes of a transposing read (8 rows of one chunk, or 4 rows of two), and 8
@@ -612,29 +769,29 @@ struct Slim {
   }
 
   struct Sums {
-    f32x4 o[NR][DB];
-    float m[NR], l[NR];
+    f32x4 o[NY][DB];
+    float m[NY], l[NY];
     __device__ __forceinline__ void put(float* to) const {
       to += threadIdx.x & 63;
 #pragma unroll
-      for (int y = 0; y < NR; ++y) {
+      for (int y = 0; y < NY; ++y) {
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) to[((y * DB + b) * 4 + i) * 64] = o[y][b][i];
-        to[(NR * DB * 4 + 2 * y) * 64] = m[y];
-        to[(NR * DB * 4 + 2 * y + 1) * 64] = l[y];
+        to[(NY * DB * 4 + 2 * y) * 64] = m[y];
+        to[(NY * DB * 4 + 2 * y + 1) * 64] = l[y];
       }
     }
     __device__ __forceinline__ void join(const float* from) {
       from += threadIdx.x & 63;
 #pragma unroll
-      for (int y = 0; y < NR; ++y) {
-        const float m2 = from[(NR * DB * 4 + 2 * y) * 64], up = fmaxf(m[y], m2);
+      for (int y = 0; y < NY; ++y) {
+        const float m2 = from[(NY * DB * 4 + 2 * y) * 64], up = fmaxf(m[y], m2);
         const float f = m[y] == up ? 1.0f : __builtin_amdgcn_exp2f(m[y] - up);
         const float g = m2 == up ? 1.0f : __builtin_amdgcn_exp2f(m2 - up);
         m[y] = up;
-        l[y] = l[y] * f + from[(NR * DB * 4 + 2 * y + 1) * 64] * g;
+        l[y] = l[y] * f + from[(NY * DB * 4 + 2 * y + 1) * 64] * g;
 #pragma unroll
         for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -650,16 +807,20 @@ struct Slim {
   struct Tile32 {
     static constexpr int N = CPR / 2, STEP = 64 / CPR;
     u32x4 k[N], v[N];
-    int scale;                     // the byte of the lane's key (lanes 0 to 31) or value
-    __device__ __forceinline__ void load(const Heads<C>& h, const Slot<C>& s, int d) {
-      const int lane = threadIdx.x & 63, e = lane % CPR * CH;
-      if constexpr (CODES) scale = s.at < 0 ? 127 : (lane < 32 ? h.ks : h.vs)[s.scale];
+    int scale[HP];                 // bytes of the lane's key (lanes 0 to 31) or value, of each head
+    __device__ __forceinline__ void load(const PrefixArgs& a, const Heads<C>& h, const Slot<C>& s) {
+      const int lane = threadIdx.x & 63, c = lane % CPR, e = c % CPH * CH;
+      const int64_t more = e + (HP > 1 ? c / CPH * a.c.sh : 0);
+      if constexpr (CODES) {
+#pragma unroll
+        for (int y = 0; y < HP; ++y) scale[y] = load_byte(s.at >= 0, (lane < 32 ? h.ks : h.vs) + s.scale + y * a.cs.sh);
+      }
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int64_t o = shfl64(s.at, lane / CPR + i * STEP);
-        const bool ok = o >= 0 && e < d;
-        k[i] = ok ? *reinterpret_cast<const u32x4*>(h.k + o + e) : u32x4{};
-        v[i] = ok ? *reinterpret_cast<const u32x4*>(h.v + o + e) : u32x4{};
+        const bool ok = o >= 0 && e < a.d;
+        k[i] = load16(ok, h.k + o + more);
+        v[i] = load16(ok, h.v + o + more);
       }
     }
     __device__ __forceinline__ bool any_nonfinite() const {
@@ -698,12 +859,15 @@ struct Slim {
         *reinterpret_cast<u32x4*>(kt + off(row, chunk)) = k[i];
         *reinterpret_cast<u32x4*>(kt + VB + off(row_of(row), chunk)) = v[i];
       }
-      if constexpr (CODES)   // the factors of a key's score and of its weight
-        reinterpret_cast<float*>(kt + 2 * VB)[2 * (lane & 31) + (lane >> 5)] = lane < 32 ? scale_of(scale) * c : scale_of(scale);
+      if constexpr (CODES) {   // the factors of a key's scores and of its weights
+#pragma unroll
+        for (int y = 0; y < HP; ++y)
+          reinterpret_cast<float*>(kt + 2 * VB)[64 * y + 2 * (lane & 31) + (lane >> 5)] = scale_of(scale[y]) * (lane < 32 ? c : 1.0f);
+      }
     }
   };
 
-  static __device__ __forceinline__ void run(const PrefixArgs& a, const Job& jb, const Row (&row)[NR], const Sights (&sg)[NR],
+  static __device__ __forceinline__ void run(const PrefixArgs& a, const Job& jb, const Row (&row)[NY], const Sights (&sg)[NR],
                                              int hk, uint8_t* smem) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
     const int wa = sg[0].wa, wb = sg[0].wb;
@@ -712,28 +876,27 @@ struct Slim {
     const Heads<C> hd(a, hk);
     const float c = a.scale * kLog2e;
     uint8_t *ks = smem + wave * WAVE, *vt = ks + VB;
-    auto slot = [&](int x) __attribute__((always_inline)) {   // of key lane % 32
-      Slot<C> s;
-      s.at = -1;
-      if (x < x1) s.find(a, jb.table, kt.tile(x) * 32 + (lane & 31), jb.len);
-      return s;
+    auto place = [&](int x) __attribute__((always_inline)) {   // of key lane % 32
+      Place p{};
+      p.at = -1;
+      if (x < x1) p = Place(a, jb.table, kt.tile(x) * 32 + (lane & 31), jb.len);
+      return p;
     };
-    Tile32 t;
     int x = x0 + wave;
-    Slot<C> here = slot(x), next = slot(x + kWaves);
-    if (x < x1) t.load(hd, here, a.d);
-    bf16x8 q[NR][NQ][ST];
+    const Place at0 = place(x);
+    Place next = place(x + kWaves);
+    bf16x8 q[NY][NQ][ST];
 #pragma unroll
-    for (int y = 0; y < NR; ++y)
+    for (int y = 0; y < NY; ++y)
 #pragma unroll
       for (int s = 0; s < ST; ++s) {
         const int e = query_at(s);
         const T* at = reinterpret_cast<const T*>(a.q.p) + row[y].token * a.q.st + row[y].head * a.q.sh + e;
         const bool ok = row[y].ok && e < a.d;
         if constexpr (sizeof(T) == 2) {
-          q[y][0][s] = __builtin_bit_cast(bf16x8, ok ? *reinterpret_cast<const u32x4*>(at) : u32x4{});
+          q[y][0][s] = __builtin_bit_cast(bf16x8, load16(ok, at));
         } else {
-          const f32x4 lo = ok ? *reinterpret_cast<const f32x4*>(at) : f32x4{}, hi = ok ? *reinterpret_cast<const f32x4*>(at + 4) : f32x4{};
+          const f32x4 lo = __builtin_bit_cast(f32x4, load16(ok, at)), hi = __builtin_bit_cast(f32x4, load16(ok, at + 4));
           const float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
           bf16x8 p[NQ];
           parts<NQ, false>(f, p);
@@ -741,9 +904,13 @@ struct Slim {
           for (int k = 0; k < NQ; ++k) q[y][k][s] = p[k];
         }
       }
+    Slot<C> here(a, at0);
+    Tile32 t;
+    if (x < x1) t.load(a, hd, here);
+    arrived(q);
     Sums st;
 #pragma unroll
-    for (int y = 0; y < NR; ++y) {
+    for (int y = 0; y < NY; ++y) {
 #pragma unroll
       for (int b = 0; b < DB; ++b) st.o[y][b] = f32x4{};
       st.m[y] = neg_inf();
@@ -760,52 +927,55 @@ struct Slim {
       wave_fence();
       // the next tile
       const Slot<C> old = here;
-      here = next;
-      if (x + kWaves < x1) t.load(hd, here, a.d);
-      next = slot(x + 2 * kWaves);
+      here = Slot<C>(a, next);
+      if (x + kWaves < x1) t.load(a, hd, here);
+      next = place(x + 2 * kWaves);
       // scores
-      f32x4 s[NR][2];
+      f32x4 s[NY][2];
 #pragma unroll
-      for (int y = 0; y < NR; ++y) s[y][0] = s[y][1] = f32x4{};
+      for (int y = 0; y < NY; ++y) s[y][0] = s[y][1] = f32x4{};
 #pragma unroll
-      for (int i = 0; i < LK; ++i)
+      for (int i = 0; i < LK * HP; ++i)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const u32x4 chunk = *reinterpret_cast<const u32x4*>(ks + off(16 * u + n, g + 4 * i));
+          const int hp = i / LK, ih = i % LK;
+          const u32x4 chunk = *reinterpret_cast<const u32x4*>(ks + off(16 * u + n, hp * CPH + g + 4 * ih));
 #pragma unroll
           for (int h = 0; h < (CODES ? 2 : 1); ++h) {
             const bf16x8 kr = rows(chunk, h);
 #pragma unroll
-            for (int y = 0; y < NR; ++y)
+            for (int y = hp * NR; y < (hp + 1) * NR; ++y)
 #pragma unroll
               for (int p = NQ - 1; p >= 0; --p)
-                s[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr, q[y][p][CODES ? 2 * i + h : i], s[y][u], 0, 0, 0);
+                s[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr, q[y][p][CODES ? 2 * ih + h : ih], s[y][u], 0, 0, 0);
           }
         }
-      float kf[2][4], vf[2][4];
+      float kf[HP][2][4], vf[HP][2][4];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if constexpr (CODES) {
-          const f32x4* f = reinterpret_cast<const f32x4*>(ks + 2 * VB + (16 * u + 4 * g) * 8);
-          const f32x4 lo = f[0], hi = f[1];
-          kf[u][0] = lo[0], vf[u][0] = lo[1], kf[u][1] = lo[2], vf[u][1] = lo[3];
-          kf[u][2] = hi[0], vf[u][2] = hi[1], kf[u][3] = hi[2], vf[u][3] = hi[3];
-        } else {
+      for (int hp = 0; hp < HP; ++hp)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) kf[u][i] = c, vf[u][i] = 1.0f;
+        for (int u = 0; u < 2; ++u) {
+          if constexpr (CODES) {
+            const f32x4* f = reinterpret_cast<const f32x4*>(ks + 2 * VB + 256 * hp + (16 * u + 4 * g) * 8);
+            const f32x4 lo = f[0], hi = f[1];
+            kf[hp][u][0] = lo[0], vf[hp][u][0] = lo[1], kf[hp][u][1] = lo[2], vf[hp][u][1] = lo[3];
+            kf[hp][u][2] = hi[0], vf[hp][u][2] = hi[1], kf[hp][u][3] = hi[2], vf[hp][u][3] = hi[3];
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) kf[hp][u][i] = c, vf[hp][u][i] = 1.0f;
+          }
         }
-      }
       if (what) {
-        bf16x8 w[NR][NP];
+        bf16x8 w[NY][NP];
 #pragma unroll
-        for (int y = 0; y < NR; ++y) {
+        for (int y = 0; y < NY; ++y) {
           float z[2][4], mx = neg_inf();
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[u][i] = s[y][u][i] * kf[u][i];
+            for (int i = 0; i < 4; ++i) z[u][i] = s[y][u][i] * kf[y / NR][u][i];
           if (what == 1) {
-            const int jlo = sg[y].p - jb.band.win + 1, jhi = sg[y].jhi, sink = min(jb.band.sinks, jhi + 1);
+            const int jlo = sg[y % NR].p - jb.band.win + 1, jhi = sg[y % NR].jhi, sink = min(jb.band.sinks, jhi + 1);
             const int lo = jhi < jlo ? 1 << 30 : jlo;
             const uint32_t span = (uint32_t)max(jhi - jlo, 0);
 #pragma unroll
@@ -839,18 +1009,18 @@ struct Slim {
             for (int i = 0; i < 4; ++i) {
               const float e = __builtin_amdgcn_exp2f(z[u][i] - m);
               st.l[y] += e;
-              p[4 * u + i] = CODES ? (what == 1 && e == 0.0f ? 0.0f : e * vf[u][i]) : e;
+              p[4 * u + i] = CODES ? (what == 1 && e == 0.0f ? 0.0f : e * vf[y / NR][u][i]) : e;
             }
           parts<NP, true>(p, w[y]);
         }
 #pragma unroll
-        for (int b = 0; b < DB; ++b) {
+        for (int b = 0; b < DB * HP; ++b) {
           const bf16x8 vc = columns(vt, b);
 #pragma unroll
-          for (int y = 0; y < NR; ++y)
+          for (int y = b / DB * NR; y < (b / DB + 1) * NR; ++y)
 #pragma unroll
             for (int p = NP - 1; p >= 0; --p)
-              st.o[y][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vc, w[y][p], st.o[y][b], 0, 0, 0);
+              st.o[y][b % DB] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vc, w[y][p], st.o[y][b % DB], 0, 0, 0);
         }
       }
       if (__builtin_expect(scrubbed, 0)) {
@@ -858,12 +1028,12 @@ struct Slim {
         for (int r = 0; r < 32; ++r) {
           const int64_t o = shfl64(old.at, r);
           if (o < 0) continue;
-          restore(st, hd, jb, sg, o, k0 + r, a.d);
+          restore(st, a, hd, jb, sg, o, k0 + r);
         }
       }
     }
 #pragma unroll
-    for (int y = 0; y < NR; ++y) {
+    for (int y = 0; y < NY; ++y) {
       st.l[y] += __shfl_xor(st.l[y], 16, 64);
       st.l[y] += __shfl_xor(st.l[y], 32, 64);
     }
@@ -879,7 +1049,7 @@ struct Slim {
     if (wave) return;
     st.join(sums);
 #pragma unroll
-    for (int y = 0; y < NR; ++y) {
+    for (int y = 0; y < NY; ++y) {
       if (!row[y].ok) continue;
       const int64_t to = part_row(a, max(jb.part, 0), row[y]);
       const float inv = st.l[y] == 0.0f ? 0.0f : 1.0f / st.l[y];
@@ -901,65 +1071,87 @@ struct Slim {
   }
 
   // (as add_nonfinite()) key j at offset o, whose values were scrubbed
-  static __device__ __forceinline__ void restore(Sums& st, const Heads<C>& hd, const Job& jb, const Sights (&sg)[NR], int64_t o,
-                                                 int j, int d) {
+  static __device__ __forceinline__ void restore(Sums& st, const PrefixArgs& a, const Heads<C>& hd, const Job& jb,
+                                                 const Sights (&sg)[NR], int64_t o, int j) {
     int g = (threadIdx.x & 63) >> 4;
     asm volatile("" : "+v"(g));
 #pragma unroll
-    for (int y = 0; y < NR; ++y) {
-      const int jlo = sg[y].p - jb.band.win + 1, jhi = sg[y].jhi;
+    for (int y = 0; y < NY; ++y) {
+      const int jlo = sg[y % NR].p - jb.band.win + 1, jhi = sg[y % NR].jhi;
       if (!((j >= jlo && j <= jhi) || j < min(jb.band.sinks, jhi + 1))) continue;
 #pragma unroll
       for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int e = 16 * b + 4 * g + i;
-          if (e >= d) continue;
+          if (e >= a.d) continue;
+          const int64_t at = o + y / NR * a.c.sh + e;
           float x;
-          if constexpr (CODES) x = (hd.v[o + e] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
-          else x = (float)hd.v[o + e];
+          if constexpr (CODES) x = (hd.v[at] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
+          else x = (float)hd.v[at];
           if (!(fabsf(x) < __builtin_inff())) st.o[y][b][i] += x;
         }
     }
   }
 };
 
-// The shapes of a role's workgroups: 16 or 32 rows whose waves take turns at the keys, or 128.
-enum Shape { kNone, kRows16, kRows32, kRows128 };
+// The shapes of a role's workgroups: 16 or 32 rows whose waves take turns at
+// the keys, of one key head or of two, or 128 of one.
+enum Shape { kNone, kRows16, kRows32, kRows128, kPairs16, kPairs32 };
 
 template <typename T, class C, int DP, int SHAPE>
 struct Role {
   static constexpr bool PAGED32 = sizeof(T) == 4 && !std::is_same<C, Code>::value;   // an fp32 cache
-  static constexpr int R = SHAPE == kRows128 ? 128 : SHAPE == kRows16 ? 16 : 32;
+  static constexpr int R = SHAPE == kRows128 ? 128 : SHAPE == kRows16 || SHAPE == kPairs16 ? 16 : 32;
   static constexpr int NR = R / 16;
+  static constexpr int HP = SHAPE == kPairs16 || SHAPE == kPairs32 ? 2 : 1;   // key heads a workgroup
   static constexpr int smem() {
     if constexpr (SHAPE == kNone) return 0;
     else if constexpr (SHAPE == kRows128) return Shapes<T, C, DP>::WIDE;
     else if constexpr (PAGED32) return kWaves * Shapes<T, C, DP>::WAVE;
-    else return Slim<T, C, DP, NR>::SMEM;
+    else return Slim<T, C, DP, NR, HP>::SMEM;
   }
 };
 
+// Workgroups a CU that the registers are to allow.
+template <typename T, class C, int DP, int PS, int OS>
+constexpr int occupancy() {
+  constexpr bool few = PS != kRows128 && OS != kRows128 && !Role<T, C, DP, OS>::PAGED32;   // rows
+  return DP <= 128 && (sizeof(T) == 2 || few) ? 2 : 1;
+}
+
+// LDS that all shapes have: flags of the wide one, positions of the waves' rows, offsets.
+struct Words {
+  uint32_t mask[2];
+  int found, sights[2 * kWaves], offsets[kOffsets + 1];
+};
+
 template <typename T, class C, int DP, int SHAPE, bool GROUP>
-__device__ __forceinline__ void work(const PrefixArgs& a, const Job& jb, int p0, int hk, uint8_t* smem, uint32_t* mask, int* found) {
+__device__ __forceinline__ void work(const PrefixArgs& a, const Offsets& off, const Job& jb, int p0, int hk, uint8_t* smem,
+                                     Words& words) {
   using Ro = Role<T, C, DP, SHAPE>;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if constexpr (SHAPE == kRows128 || Ro::PAGED32) {
     const int wr = jb.r0 + (SHAPE == kRows128 ? 32 * wave : 0);
     const Row row(a, jb, hk, wr + (lane & 31));
     Sights sg;
-    if constexpr (GROUP) sg = group_sights(a, jb, row, Ro::R);
-    else sg = own_sights(a, jb, p0, row, wr, Ro::R);
-    if constexpr (SHAPE == kRows128) wide<T, C, DP>(a, jb, row, sg, hk, smem, mask, found);
+    if constexpr (GROUP) {
+      sg = group_sights<32>(a, off, jb, row);
+      if (SHAPE == kRows128) join_sights(sg, words.sights);
+    } else {
+      sg = own_sights(a, jb, p0, row, wr, Ro::R);
+    }
+    if constexpr (SHAPE == kRows128) wide<T, C, DP>(a, jb, row, sg, hk, smem, words.mask, &words.found);
     else narrow<T, C, DP>(a, jb, row, sg, hk, smem);
   } else {
-    constexpr int NR = Ro::NR;
-    Row row[NR];
+    constexpr int NR = Ro::NR, HP = Ro::HP;
+    Row row[NR * HP];
     Sights sg[NR];
 #pragma unroll
-    for (int y = 0; y < NR; ++y) {
-      row[y] = Row(a, jb, hk, jb.r0 + 16 * y + (lane & 15));
-      if constexpr (GROUP) sg[y] = group_sights(a, jb, row[y], 16);
+    for (int y = 0; y < NR * HP; ++y) {
+      row[y] = Row(a, jb, hk + y / NR, jb.r0 + 16 * (y % NR) + (lane & 15));
+      if (y >= NR) continue;
+      if constexpr (GROUP) sg[y] = group_sights<16>(a, off, jb, row[y]);
       else sg[y] = own_sights(a, jb, p0, row[y], jb.r0, Ro::R);
     }
     if constexpr (GROUP)
@@ -968,51 +1160,52 @@ __device__ __forceinline__ void work(const PrefixArgs& a, const Job& jb, int p0,
           sg[0].wa = min(sg[0].wa, sg[y].wa);
           sg[0].wb = max(sg[0].wb, sg[y].wb);
         }
-    Slim<T, C, DP, NR>::run(a, jb, row, sg, hk, smem);
+    Slim<T, C, DP, NR, HP>::run(a, jb, row, sg, hk, smem);
   }
 }
 
 // PS, OS: the shapes of the rows over prefixes (or kNone) and over a sequence's own keys.
 template <typename T, class C, int DP, int PS, int OS>
-__global__ __launch_bounds__(64 * kWaves, (DP <= 128 && (sizeof(T) == 2 || (PS != kRows128 && OS != kRows128 && !Role<T, C, DP, OS>::PAGED32)) ? 2 : 1)) void k_prefix(const PrefixArgs a) {
+__global__ __launch_bounds__(64 * kWaves, (occupancy<T, C, DP, PS, OS>())) void k_prefix(const PrefixArgs a) {
   using P = Role<T, C, DP, PS>;
   using O = Role<T, C, DP, OS>;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[P::smem() > O::smem() ? P::smem() : O::smem()];
-  __shared__ uint32_t mask[2];
-  __shared__ int found;
+  __shared__ Words words;
+  const Offsets off(a, words.offsets);
   Seq s;
   Job jb;
+  jb.band = Band{a.win, 0, a.sinks};
   if constexpr (PS != kNone) {
     if ((int)blockIdx.x < a.pjobs) {
-      const int heads = a.Hkv * a.psplits, t = (int)blockIdx.x / heads, y = (int)blockIdx.x - t * heads, hk = y % a.Hkv;
-      if (!find_rows(a, Groups{a}, t, P::R, s, jb.r0)) return;
+      const int n = a.Hkv / P::HP, heads = n * a.psplits, t = (int)blockIdx.x / heads, y = (int)blockIdx.x - t * heads;
+      if (!find_tile<true>(a, off, t, P::R, s, jb.r0)) return;
       jb.table = a.ptable + (int64_t)s.b * a.p_pages;
       jb.t0 = s.t0;
       jb.rows = s.rows;
       jb.len = s.len;
-      jb.split = jb.part = y / a.Hkv;
+      jb.split = jb.part = y / n;
       jb.splits = a.psplits;
-      jb.band = Band{a.win, 0, a.sinks};
-      work<T, C, DP, PS, true>(a, jb, 0, hk, smem, mask, &found);
+      work<T, C, DP, PS, true>(a, off, jb, 0, y % n * P::HP, smem, words);
       return;
     }
   }
-  const int job = (int)blockIdx.x - (PS != kNone ? a.pjobs : 0), heads = a.Hkv * a.splits;
-  const int t = job / heads, y = job - t * heads, hk = y % a.Hkv;
-  if (!find_rows(a, Sequences{a}, t, O::R, s, jb.r0)) return;
+  const int job = (int)blockIdx.x - (PS != kNone ? a.pjobs : 0), n = a.Hkv / O::HP, heads = n * a.splits;
+  const int t = job / heads, y = job - t * heads;
+  if (!find_tile<false>(a, off, t, O::R, s, jb.r0)) return;
   jb.table = a.table + (int64_t)s.b * a.max_pages;
   jb.t0 = s.t0;
   jb.rows = s.rows;
   jb.len = s.len;
-  jb.split = y / a.Hkv;
+  jb.split = y / n;
   jb.splits = a.splits;
   jb.part = PS != kNone || a.splits > 1 ? a.psplits + jb.split : -1;
-  jb.band = Band{a.win, 0, a.sinks};
   if constexpr (PS != kNone) {
-    const int g = group_of(a, s.b);
-    if (g >= 0) jb.band.sinks = max(0, a.sinks - Groups{a}.len(g));
+    if (a.sinks) {   // those that its group's prefix leaves
+      const int g = group_of(a, s.b);
+      if (g >= 0) jb.band.sinks = max(0, a.sinks - clampi(a.plen[g], 0, a.p_pages * a.page));
+    }
   }
-  work<T, C, DP, OS, false>(a, jb, s.p0, hk, smem, mask, &found);
+  work<T, C, DP, OS, false>(a, off, jb, s.p0, y % n * O::HP, smem, words);
 }
 
 // The parts of each (token, head), joined in a fixed order: those over its
@@ -1029,7 +1222,10 @@ __global__ __launch_bounds__(256) void k_prefix_join(const PrefixArgs a, int G, 
   const int token = (int)(r / a.H), head = (int)(r % a.H), e = lg * 4, all = a.psplits + a.splits;
   const bool ok = r < rows && token >= clampi(a.cu[0], 0, a.T) && token < clampi(a.cu[a.B], 0, a.T);
   int s0 = a.psplits;
-  if (a.P && token >= Groups{a}.first(0) && token < Groups{a}.first(a.P)) s0 = 0;
+  if (a.P) {
+    auto first = [&](int g) { return clampi(a.cu[clampi(a.cu_seq[g], 0, a.B)], 0, a.T); };
+    if (token >= first(0) && token < first(a.P)) s0 = 0;
+  }
   float m = neg_inf(), sum = 0.0f;
   f32x4 o = {};
   auto add = [&](f32x2 x, f32x4 y) __attribute__((always_inline)) {
@@ -1070,12 +1266,16 @@ __global__ __launch_bounds__(256) void k_prefix_join(const PrefixArgs a, int G, 
     *reinterpret_cast<f32x4*>(dst) = o * inv;
 }
 
-int shape_rows(int shape) { return shape == kRows128 ? 128 : shape == kRows16 ? 16 : 32; }
-int row_tiles(const PrefixArgs& a, int shape, int n) { return (int)((int64_t)a.T * a.G / shape_rows(shape)) + n; }
+int shape_rows(int shape) { return shape == kRows128 ? 128 : shape == kRows16 || shape == kPairs16 ? 16 : 32; }
+// Workgroups of one part of the keys: row tiles of n sequences or groups, times (pairs of) key heads.
+int row_jobs(const PrefixArgs& a, int shape, int n) {
+  const int tiles = (int)((int64_t)a.T * a.G / shape_rows(shape)) + n;
+  return tiles * (shape >= kPairs16 ? a.Hkv / 2 : a.Hkv);
+}
 
 template <typename T, class C, int DP, int PS, int OS>
 void start(const PrefixArgs& a, hipStream_t s) {
-  const unsigned jobs = (unsigned)(a.pjobs + row_tiles(a, OS, a.B) * a.Hkv * a.splits);
+  const unsigned jobs = (unsigned)(a.pjobs + row_jobs(a, OS, a.B) * a.splits);
   k_prefix<T, C, DP, PS, OS><<<jobs, 64 * kWaves, 0, s>>>(a);
 }
 
@@ -1085,19 +1285,28 @@ hipError_t run(const PrefixArgs& a, hipStream_t s) {
   if constexpr (FP32 && DP == 256) {                // a wave's own tile would not fit
     start<T, C, DP, kRows128, kRows128>(a, s);
   } else {
+    constexpr bool PAIRS = CODES && DP == 64;
     constexpr int k16 = FP32 ? kRows32 : kRows16;   // (an fp32 cache has one shape of few rows)
+    constexpr int p16 = PAIRS ? kPairs16 : k16, p32 = PAIRS ? kPairs32 : kRows32;
     if (!a.P) {
       if constexpr (CODES) {                        // (the other kinds have their own entry point)
         if (a.shape == kRows128) start<T, C, DP, kNone, kRows128>(a, s);
         else if (a.shape == kRows32) start<T, C, DP, kNone, kRows32>(a, s);
-        else start<T, C, DP, kNone, kRows16>(a, s);
+        else if (a.shape == kRows16) start<T, C, DP, kNone, kRows16>(a, s);
+        else if (a.shape == kPairs32) start<T, C, DP, kNone, p32>(a, s);
+        else start<T, C, DP, kNone, p16>(a, s);
       }
     } else if (a.shape == kRows128) {
       start<T, C, DP, kRows128, kRows128>(a, s);
     } else if (a.shape == kRows32) {
       start<T, C, DP, kRows128, kRows32>(a, s);
+    } else if (a.shape == kPairs32) {
+      start<T, C, DP, kRows128, p32>(a, s);
     } else if (a.pshape == kRows128) {
-      start<T, C, DP, kRows128, k16>(a, s);
+      if (a.shape == kPairs16) start<T, C, DP, kRows128, p16>(a, s);
+      else start<T, C, DP, kRows128, k16>(a, s);
+    } else if (a.shape == kPairs16) {
+      start<T, C, DP, p32, p16>(a, s);
     } else {
       start<T, C, DP, kRows32, k16>(a, s);
     }
