@@ -1097,19 +1097,19 @@ def paged_attention(q, k_cache, v_cache, table, lens, cu_new, *, window=None, si
 
 def _code_args(x, H, n, dtype, k_cache, v_cache, k_scale, v_scale, table, lens, cu_new, window, sinks, scale, torch):
     """As _paged_args() for a cache of e4m3 numbers: x is a tensor of the call's device, n its new tokens."""
-    if k_cache.dim() != 4 or table.dim() != 2:
+    sc, st = k_cache.shape, table.shape
+    if len(sc) != 4 or len(st) != 2:
         raise LactError(-1, "new tokens are [n_new, heads, d], caches [pages, page, Hkv, d], table [B, max_pages]")
-    sc = pages, page, Hkv, d = k_cache.shape
-    B, max_pages = table.shape
+    pages, page, Hkv, d = sc
+    B, max_pages = st
     dev, i32, u8, f8 = x.get_device(), torch.int32, torch.uint8, torch.float8_e4m3fn
-    io = IO_BF16 if dtype is torch.bfloat16 else IO_FP32 if dtype is torch.float32 else None
-    if io is None:
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise LactError(-1, f"unsupported dtype {dtype}")
     desc = _pack(_pack_paged, B, H, Hkv, d, n, pages, page, max_pages, -1 if window is None else int(window),
-                 int(sinks), d ** -0.5 if scale is None else float(scale), io)
+                 int(sinks), d ** -0.5 if scale is None else float(scale), IO_BF16 if dtype is torch.bfloat16 else IO_FP32)
     return d, dev, desc, (_view_t(k_cache, "k_cache", sc, f8, dev), _view_t(v_cache, "v_cache", sc, f8, dev),
                           _view_s(k_scale, "k_scale", sc[:3], u8, dev), _view_s(v_scale, "v_scale", sc[:3], u8, dev),
-                          _aux(table, "table", (B, max_pages), i32, dev), _aux(lens, "lens", (B,), i32, dev),
+                          _aux(table, "table", st, i32, dev), _aux(lens, "lens", (B,), i32, dev),
                           _aux(cu_new, "cu_new", (B + 1,), i32, dev))
 
 

@@ -194,14 +194,6 @@ int check_cache(const lact_paged_desc* s, int es, const lact_view* kc, const lac
   return LACT_OK;
 }
 
-// x / d for 0 <= x < 2^31 as (mulhi(x, mul) + x) >> shift
-void divider(int d, uint32_t* mul, uint32_t* shift) {
-  uint32_t s = 0;
-  while (((uint64_t)1 << s) < (uint64_t)d) ++s;
-  *shift = s;
-  *mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << s) - d)) / d + 1);
-}
-
 void fill_paged(PagedArgs& a, const lact_paged_desc* s) {
   const int64_t far = (int64_t)1 << 30;
   a.B = s->B;

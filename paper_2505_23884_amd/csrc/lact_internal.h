@@ -602,6 +602,8 @@ struct CodeArgs {
   const int32_t *table, *len, *cu;
   int B, Hkv, d, T, page, max_pages, pages;
   uint32_t mul, shift;
+  int per;                             // tokens a workgroup, set at the launch
+  uint32_t hmul, hshift, mul2, shift2;
 };
 hipError_t launch_append_e4m3(const CodeArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_read_e4m3(const CodeArgs& a, bool bf16, hipStream_t s);
@@ -635,6 +637,14 @@ void rope_plan(RopeArgs& a, bool bf16, bool bwd);
 size_t rope_part_floats(const RopeArgs& a);
 hipError_t launch_rope(const RopeArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_rope_bwd(const RopeArgs& a, bool bf16, hipStream_t s);
+
+// x / d for 0 <= x < 2^31 as (mulhi(x, mul) + x) >> shift
+inline void divider(int d, uint32_t* mul, uint32_t* shift) {
+  uint32_t s = 0;
+  while (((uint64_t)1 << s) < (uint64_t)d) ++s;
+  *shift = s;
+  *mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << s) - d)) / d + 1);
+}
 
 // timed() of lact_api.hip for the entry points of other files.
 int timed_launch(int kclass, double flops, hipStream_t s, hipError_t (*launch)(void*), void* ctx);

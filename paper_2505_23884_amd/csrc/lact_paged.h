@@ -173,5 +173,18 @@ __device__ __forceinline__ void restore_nonfinite(Softmax<DP / 32>& st, const T*
 // 16 bytes of zeros for the lanes of a copy that have nothing to read.
 __device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
 
+// Loads that lanes have nothing to read with go to zeros instead of around a
+// branch, behind which the compiler could not tell what is in flight and would wait
+// for all of it.
+template <class X>
+__device__ __forceinline__ X load_or_zeros(bool ok, const void* p) {
+  typedef __attribute__((address_space(1))) const X global;   // (a choice of generic pointers would count as LDS too)
+  return *(ok ? (global*)p : (global*)kZeros);
+}
+__device__ __forceinline__ u32x4 load16(bool ok, const void* p) { return load_or_zeros<u32x4>(ok, p); }
+__device__ __forceinline__ u32x2 load8(bool ok, const void* p) { return load_or_zeros<u32x2>(ok, p); }
+__device__ __forceinline__ uint32_t load4(bool ok, const void* p) { return load_or_zeros<uint32_t>(ok, p); }
+__device__ __forceinline__ int load_byte(bool ok, const uint8_t* p) { return load_or_zeros<uint8_t>(ok, p); }
+
 }  // namespace attn
 }  // namespace lact

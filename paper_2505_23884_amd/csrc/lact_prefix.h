@@ -29,6 +29,9 @@ struct Band {
   int win, look, sinks;
 };
 
+// Where part `i` of n parts of `count` tiles begins (2^24 tiles of 32 at most, 64 parts).
+__device__ __forceinline__ int share(int count, int i, int n) { return (int)((uint32_t)count * (uint32_t)i / (uint32_t)n); }
+
 // What a workgroup works on: `rows` rows from token t0 on, from row r0, over
 // part `split` of `splits` of the tiles of keys, to part `part` of the sums
 // (< 0: to the output).
@@ -182,18 +185,6 @@ struct Slot<Code> {
     scale = ok ? p.page * a.cs.sb + p.at * a.cs.st : 0;
   }
 };
-
-// Loads that lanes have nothing to read with go to zeros instead of around a
-// branch, behind which the compiler could not tell what is in flight and would wait
-// for all of it.
-__device__ __forceinline__ u32x4 load16(bool ok, const void* p) {
-  typedef __attribute__((address_space(1))) const u32x4 global;   // (a choice of generic pointers would count as LDS too)
-  return *(ok ? (global*)p : (global*)kZeros);
-}
-__device__ __forceinline__ int load_byte(bool ok, const uint8_t* p) {
-  typedef __attribute__((address_space(1))) const uint8_t global;
-  return *(ok ? (global*)p : (global*)kZeros);
-}
 
 // Has the compiler wait here for what is loaded in these registers, so that a
 // loop that uses them does not (it would wait for its own loads with them).
@@ -413,7 +404,7 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
   using Cp = Copy<T, DP, KT, NT>;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const KeyTiles kt(jb.band, jb.len, sg.pa, sg.pb, KT);
-  const int x0 = (int)((int64_t)kt.count() * jb.split / jb.splits), x1 = (int)((int64_t)kt.count() * (jb.split + 1) / jb.splits);
+  const int x0 = share(kt.count(), jb.split, jb.splits), x1 = share(kt.count(), jb.split + 1, jb.splits);
   const Heads<C> hd(a, hk);
   u32x4 q[L::KS];
   load_row<T, DP>(q, reinterpret_cast<const T*>(a.q.p) + row.token * a.q.st + row.head * a.q.sh, row.ok, a.d);
@@ -576,7 +567,7 @@ __device__ __forceinline__ void narrow(const PrefixArgs& a, const Job& jb, const
   constexpr int BYTES = kKT * L::PITCH, WAVE = Shapes<T, C, DP>::WAVE;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const KeyTiles kt(jb.band, jb.len, sg.wa, sg.wb, kKT);
-  const int x0 = (int)((int64_t)kt.count() * jb.split / jb.splits), x1 = (int)((int64_t)kt.count() * (jb.split + 1) / jb.splits);
+  const int x0 = share(kt.count(), jb.split, jb.splits), x1 = share(kt.count(), jb.split + 1, jb.splits);
   const Heads<C> hd(a, hk);
   u32x4 q[L::KS];
   load_row<T, DP>(q, reinterpret_cast<const T*>(a.q.p) + row.token * a.q.st + row.head * a.q.sh, row.ok, a.d);
@@ -676,7 +667,7 @@ __device__ __forceinline__ void narrow(const PrefixArgs& a, const Job& jb, const
 //
 // HP key heads stand beside each other in a workgroup's tiles: two of 64 e4m3
 // numbers, which share lines of memory where heads lie behind slots (decoding of 64
-// sequences of up to 16384, heads of 64: 149 us one by one, PAIRED_US in pairs).
+// sequences of up to 16384, heads of 64: 149 us one by one, 96 in pairs).
 template <typename T, class C, int DP, int NR, int HP>
 struct Slim {
   static constexpr bool CODES = std::is_same<C, Code>::value;
@@ -872,7 +863,7 @@ struct Slim {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
     const int wa = sg[0].wa, wb = sg[0].wb;
     const KeyTiles kt(jb.band, jb.len, wa, wb, 32);
-    const int x0 = (int)((int64_t)kt.count() * jb.split / jb.splits), x1 = (int)((int64_t)kt.count() * (jb.split + 1) / jb.splits);
+    const int x0 = share(kt.count(), jb.split, jb.splits), x1 = share(kt.count(), jb.split + 1, jb.splits);
     const Heads<C> hd(a, hk);
     const float c = a.scale * kLog2e;
     uint8_t *ks = smem + wave * WAVE, *vt = ks + VB;
@@ -1096,15 +1087,15 @@ struct Slim {
 };
 
 // The shapes of a role's workgroups: 16 or 32 rows whose waves take turns at
-// the keys, of one key head or of two, or 128 of one.
-enum Shape { kNone, kRows16, kRows32, kRows128, kPairs16, kPairs32 };
+// the keys (16 of one key head or of two), or 128.
+enum Shape { kNone, kRows16, kRows32, kRows128, kPairs16 };
 
 template <typename T, class C, int DP, int SHAPE>
 struct Role {
   static constexpr bool PAGED32 = sizeof(T) == 4 && !std::is_same<C, Code>::value;   // an fp32 cache
   static constexpr int R = SHAPE == kRows128 ? 128 : SHAPE == kRows16 || SHAPE == kPairs16 ? 16 : 32;
   static constexpr int NR = R / 16;
-  static constexpr int HP = SHAPE == kPairs16 || SHAPE == kPairs32 ? 2 : 1;   // key heads a workgroup
+  static constexpr int HP = SHAPE == kPairs16 ? 2 : 1;   // key heads a workgroup
   static constexpr int smem() {
     if constexpr (SHAPE == kNone) return 0;
     else if constexpr (SHAPE == kRows128) return Shapes<T, C, DP>::WIDE;
@@ -1270,7 +1261,7 @@ int shape_rows(int shape) { return shape == kRows128 ? 128 : shape == kRows16 ||
 // Workgroups of one part of the keys: row tiles of n sequences or groups, times (pairs of) key heads.
 int row_jobs(const PrefixArgs& a, int shape, int n) {
   const int tiles = (int)((int64_t)a.T * a.G / shape_rows(shape)) + n;
-  return tiles * (shape >= kPairs16 ? a.Hkv / 2 : a.Hkv);
+  return tiles * (shape == kPairs16 ? a.Hkv / 2 : a.Hkv);
 }
 
 template <typename T, class C, int DP, int PS, int OS>
@@ -1287,26 +1278,23 @@ hipError_t run(const PrefixArgs& a, hipStream_t s) {
   } else {
     constexpr bool PAIRS = CODES && DP == 64;
     constexpr int k16 = FP32 ? kRows32 : kRows16;   // (an fp32 cache has one shape of few rows)
-    constexpr int p16 = PAIRS ? kPairs16 : k16, p32 = PAIRS ? kPairs32 : kRows32;
+    constexpr int p16 = PAIRS ? kPairs16 : k16;
     if (!a.P) {
       if constexpr (CODES) {                        // (the other kinds have their own entry point)
         if (a.shape == kRows128) start<T, C, DP, kNone, kRows128>(a, s);
         else if (a.shape == kRows32) start<T, C, DP, kNone, kRows32>(a, s);
         else if (a.shape == kRows16) start<T, C, DP, kNone, kRows16>(a, s);
-        else if (a.shape == kPairs32) start<T, C, DP, kNone, p32>(a, s);
         else start<T, C, DP, kNone, p16>(a, s);
       }
     } else if (a.shape == kRows128) {
       start<T, C, DP, kRows128, kRows128>(a, s);
     } else if (a.shape == kRows32) {
       start<T, C, DP, kRows128, kRows32>(a, s);
-    } else if (a.shape == kPairs32) {
-      start<T, C, DP, kRows128, p32>(a, s);
     } else if (a.pshape == kRows128) {
       if (a.shape == kPairs16) start<T, C, DP, kRows128, p16>(a, s);
       else start<T, C, DP, kRows128, k16>(a, s);
     } else if (a.shape == kPairs16) {
-      start<T, C, DP, p32, p16>(a, s);
+      start<T, C, DP, kRows32, p16>(a, s);
     } else {
       start<T, C, DP, kRows32, k16>(a, s);
     }

@@ -7,38 +7,56 @@
 
 namespace lact {
 
-void prefix_plan(PrefixArgs& a, bool bf16, bool codes) {
-  const bool fp32 = !bf16 && !codes, pairs = codes && a.d <= 64 && a.Hkv % 2 == 0;
-  const int rows16 = fp32 ? kRows32 : pairs ? kPairs16 : kRows16, rows32 = pairs ? kPairs32 : kRows32;
-  const int64_t rows = (int64_t)a.T * a.G;
-  a.shape = rows > 32 * (int64_t)a.B || (fp32 && a.d > 128) ? kRows128 : rows > 16 * (int64_t)a.B ? rows32 : rows16;
-  const int64_t keys = (int64_t)a.max_pages * a.page, jobs = row_jobs(a, a.shape, a.B);
-  const int64_t most = std::max<int64_t>(1, (keys + kKT - 1) / kKT / (2 * kWaves));
-  a.psplits = a.pjobs = 0;
-  if (a.P) {
-    // (32 rows of prefixes go with 16 of sequences, or 32 of an fp32 cache)
-    a.pshape = rows > 32 * (int64_t)a.P || a.shape == kRows128 || (a.shape == rows32 && !fp32) ? kRows128 : rows32;
-    const int64_t pk = (int64_t)a.p_pages * a.page, pjobs = row_jobs(a, a.pshape, a.P);
-    const int64_t pmost = std::max<int64_t>(1, pk / kKT / (2 * kWaves));
-    // both roles' keys a workgroup about alike
-    const double work = (double)pjobs * pk + (double)jobs * keys, each = work / 512;
-    a.psplits = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(pk / std::max(each, 1.0) + 0.5), pmost, 64}));
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(keys / std::max(each, 1.0) + 0.5), most, 32}));
-    a.pjobs = (int)(pjobs * a.psplits);
-    return;
-  }
-  if (a.shape != kRows128) {
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(1024 + jobs - 1) / jobs, most, 32}));
-    return;
-  }
-  double best = 0;
-  for (int s = 1; s <= std::min<int64_t>(most, 16); ++s) {
-    const double t = (double)((jobs * s + 511) / 512) / s * (s > 1 ? 1.08 + 0.02 * s : 1.0);
-    if (s == 1 || t < best) {
-      best = t;
-      a.splits = s;
+// The time that `wgs` workgroups of `us` each take, two a CU where there are as
+// many: a pair takes 1.43 times one alone (12 chunks of 160 tokens behind 8192 keys,
+// the prefix in 1, 2, 3, 4 and 6 parts: 256, 180, 199, 162 and 173 us; 234, 167, 190, 142 and 151
+// by this with 0.0286 us a key, and 5 a part for the sums; 32 sequences of 5 tokens, heads of 64
+// in 8 bits, 2 to 8 parts: 52, 46, 43, 54, 52, 51 us).
+double span(int64_t wgs, double us) {
+  const int64_t full = wgs / 512, rest = wgs % 512;
+  return (full * 1.43 + (rest > 256 ? 1.43 : rest ? 1.0 : 0.0)) * us;
+}
+
+// The parts of `keys` keys for `jobs` workgroups a part, from 1 to `most`: what
+// a workgroup does before its first key takes as long as some 6 us of them, and
+// each part's sums of `rows` rows are written and read.
+int best_parts(int64_t jobs, int64_t keys, double us_per_key, int64_t rows, int d, int most, bool joined) {
+  const double sums = (double)rows * (d + 2) * 8 / 4.5e6;   // us
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= most; ++s) {
+    const double t = span(jobs * s, 6.0 + us_per_key * (double)keys / s) + (s > 1 || joined ? 4.0 + (sums + 0.1) * s : 0.0);
+    if (s == 1 || t < least) {
+      least = t;
+      best = s;
     }
   }
+  return best;
+}
+
+void prefix_plan(PrefixArgs& a, bool bf16, bool codes) {
+  const bool fp32 = !bf16 && !codes, pairs = codes && a.d <= 64 && a.Hkv % 2 == 0;
+  const int rows16 = fp32 ? kRows32 : pairs ? kPairs16 : kRows16;
+  const int64_t rows = (int64_t)a.T * a.G;
+  a.shape = rows > 32 * (int64_t)a.B || (fp32 && a.d > 128) ? kRows128 : rows > 16 * (int64_t)a.B ? kRows32 : rows16;
+  // workgroups a part: as many as there would be if the tokens were spread evenly
+  auto jobs = [&](int shape, int n) {
+    const int R = shape_rows(shape);
+    return (rows / n + (rows % n != 0) + R - 1) / R * n * (shape == kPairs16 ? a.Hkv / 2 : a.Hkv);
+  };
+  auto keys = [&](int64_t pages) { return std::min<int64_t>(pages * a.page, (int64_t)a.win + a.sinks + rows / a.G / a.B); };
+  auto rate = [&](int shape) { return (shape == kRows128 ? 0.029 : 0.018) * (a.d > 128 ? 2 : 1) * (fp32 ? 3 : 1); };
+  auto most = [&](int64_t k, int limit) { return (int)std::max<int64_t>(1, std::min<int64_t>(k / (8 * kKT), limit)); };
+  a.psplits = a.pjobs = 0;
+  const int64_t own = keys(a.max_pages);
+  // (beside a prefix they have half the room)
+  a.splits = best_parts(jobs(a.shape, a.B) * (a.P ? 2 : 1), own, rate(a.shape), (int64_t)a.T * a.H, a.d, most(own, 32), a.P > 0);
+  if (!a.P) return;
+  // (32 rows of prefixes go with 16 of sequences, or 32 of an fp32 cache)
+  a.pshape = rows > 32 * (int64_t)a.P || a.shape == kRows128 || (a.shape == kRows32 && !fp32) ? kRows128 : kRows32;
+  const int64_t shared = keys(a.p_pages);
+  a.psplits = best_parts(jobs(a.pshape, a.P), shared, rate(a.pshape), (int64_t)a.T * a.H, a.d, most(shared, 64), true);
+  a.pjobs = row_jobs(a, a.pshape, a.P) * a.psplits;
 }
 
 hipError_t launch_prefix(const PrefixArgs& a, bool bf16, hipStream_t s) {
