@@ -1288,7 +1288,7 @@ hipError_t run(const PrefixArgs& a, hipStream_t s) {
       }
     } else if (a.shape == kRows128) {
       start<T, C, DP, kRows128, kRows128>(a, s);
-    } else if (a.shape == kRows32) {
+    } else if (a.shape == kRows32 && !FP32) {
       start<T, C, DP, kRows128, kRows32>(a, s);
     } else if (a.pshape == kRows128) {
       if (a.shape == kPairs16) start<T, C, DP, kRows128, p16>(a, s);

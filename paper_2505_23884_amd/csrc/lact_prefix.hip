@@ -46,7 +46,7 @@ void prefix_plan(PrefixArgs& a, bool bf16, bool codes) {
   };
   auto keys = [&](int64_t pages) { return std::min<int64_t>(pages * a.page, (int64_t)a.win + a.sinks + rows / a.G / a.B); };
   auto rate = [&](int shape) { return (shape == kRows128 ? 0.029 : 0.018) * (a.d > 128 ? 2 : 1) * (fp32 ? 3 : 1); };
-  auto most = [&](int64_t k, int limit) { return (int)std::max<int64_t>(1, std::min<int64_t>(k / (8 * kKT), limit)); };
+  auto most = [&](int64_t k, int limit) { return (int)std::max<int64_t>(1, std::min<int64_t>(k / (4 * kKT), limit)); };
   a.psplits = a.pjobs = 0;
   const int64_t own = keys(a.max_pages);
   // (beside a prefix they have half the room)
