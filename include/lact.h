@@ -701,7 +701,8 @@ int lact_paged_attention(const lact_paged_desc* desc, const lact_view* q, const 
  * to the even one (so they are off by 2^-4 of themselves, or by 2^(e - 10) where
  * that is more: elements below 2^-14 of the largest). Magnitudes over 448 2^119
  * become that. Infinities and NaN become NaN (0x7f) and do not count for a. Vectors
- * of zeros have x = 10.
+ * of zeros have x = 10. If an append of one call writes a slot twice, any 8 numbers
+ * of it, and its byte, may be of either.
  *
  *   k_cache, v_cache   views of bytes [page][head][slot][d], strides in
  *                      multiples of 16 bytes, the same of both

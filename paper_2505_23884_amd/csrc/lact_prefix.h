@@ -324,7 +324,7 @@ __device__ __forceinline__ Sights own_sights(const PrefixArgs& a, const Job& j, 
   Sights s;
   s.p = p0 + (row.token - j.t0);
   s.jhi = row.ok ? s.p : -1;
-  const int rl = min(j.r0 + R, j.rows) - 1, wl = min(wr + 32, j.rows) - 1;
+  const int rl = min(j.r0 + R, j.rows) - 1, wl = min(wr + min(R, 32), j.rows) - 1;
   s.pa = p0 + j.r0 / a.G;
   s.pb = p0 + rl / a.G;
   s.wa = p0 + wr / a.G;

@@ -290,6 +290,21 @@ def test_prefix_attention_matches_the_formula(i, codes, dtype):
     same(again, out)
 
 
+@types
+@pytest.mark.parametrize("d", [8, 24, 72, 200])
+def test_prefix_attention_of_heads_of_eights(d, dtype):
+    plen, lens = [70, 33], [40, 3, 90]
+    for new in ([1, 1, 1], [4, 3, 9], [40, 3, 80]):
+        c = Cache(lens, 2, d, 16, dtype, False, d, prefixes=plen)
+        cu = offsets(new)
+        q = rnd(d, cu[-1], 4, d, dtype=dtype).to(DEV)
+        out = torch.full_like(q, 7.0)
+        print(f"[gpu] prefix d {d} {new} {dtype}", flush=True)
+        prefix_call(c, q, out, plen, [0, 2, 3], lens, cu, window=100, sinks=5)
+        torch.cuda.synchronize()
+        check_prefix(out, q, c, plen, [0, 2, 3], lens, cu, dict(window=100, sinks=5))
+
+
 @pytest.mark.parametrize("codes", [False, True], ids=["plain", "e4m3"])
 @pytest.mark.parametrize("B,groups,opt", [(63, 2, {}), (64, 64, dict(window=30, sinks=2)), (65, 3, {}), (130, 70, dict(window=25)), (130, 1, {})])
 def test_many_sequences_and_groups(B, groups, opt, codes):
