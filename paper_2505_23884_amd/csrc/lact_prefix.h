@@ -477,16 +477,17 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
     const int k0 = kt.tile(x) * KT;
     const uint64_t there = __ballot(here.at >= 0);
     const bool whole = there == (KT == 64 ? ~0ull : 0xffffffffull);
+    // (most tiles are seen by all rows, which is found out once)
+    const bool inner = whole && sees(jb.band, jb.len, sg.pa, sg.pb, k0, KT) == 2;
     uint64_t bad = 0;   // keys whose values were scrubbed
-    if ((!whole || sees(jb.band, jb.len, sg.pa, sg.pb, k0, KT) != 2) &&
-        __builtin_expect(Cp::holds_nonfinite(ks + BYTES, x, found), 0))
-      bad = Cp::scrub(ks + BYTES, mask);
+    if (!inner && __builtin_expect(Cp::holds_nonfinite(ks + BYTES, x, found), 0)) bad = Cp::scrub(ks + BYTES, mask);
     const Slot<C> then(a, next);
     if (x + 1 < x1) copy(x + 1, then);
     next = place(x + 2);
-    const Sight sight(jb.band, sg.p, sg.jhi, k0);
-    const uint64_t mine = there >> (4 * (lane >> 5));
-    auto see = [&](int r) __attribute__((always_inline)) { return sight.see(r) && (mine >> r & 1); };
+    auto see = [&](int r) __attribute__((always_inline)) {
+      const Sight sight(jb.band, sg.p, sg.jhi, k0);
+      return sight.see(r) && (there >> (4 * (lane >> 5)) >> r & 1);
+    };
     if constexpr (PIPED) {
       // keys of the first 32, then in turn: values of a step while its scores are
       // worked out, keys of the next one while its weights are
@@ -494,7 +495,7 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
       read_keys(kf, lds_addr(ks));
 #pragma unroll
       for (int rb = 0; rb < KT; rb += 32) {
-        const int what = sees(jb.band, jb.len, sg.wa, sg.wb, k0 + rb, 32);
+        const int what = inner ? 2 : sees(jb.band, jb.len, sg.wa, sg.wb, k0 + rb, 32);
         u32x2 vf[4 * L::DB];
         read_values(vf, lds_addr(ks) + BYTES + rb * L::PITCH);
         __builtin_amdgcn_sched_barrier(0);
@@ -505,7 +506,7 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
         if (rb + 32 < KT) read_keys(kf, lds_addr(ks) + (rb + 32) * L::PITCH);
         __builtin_amdgcn_sched_barrier(0);
         if (!what) continue;
-        if (what == 1 || !whole) {
+        if (!inner) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             if (!see(rb + 8 * (i >> 2) + (i & 3))) s[i] = neg_inf();
@@ -535,15 +536,15 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
     } else {
       auto step = [&](auto rb) __attribute__((always_inline)) {
         constexpr int RB = decltype(rb)::value;
-        const int what = sees(jb.band, jb.len, sg.wa, sg.wb, k0 + RB, 32);
-        if (what) softmax_step<T, DP, RB>(st, q, ks, ks + BYTES, c, what == 1 || !whole, see);
+        const int what = inner ? 2 : sees(jb.band, jb.len, sg.wa, sg.wb, k0 + RB, 32);
+        if (what) softmax_step<T, DP, RB>(st, q, ks, ks + BYTES, c, !inner, see);
       };
       step(std::integral_constant<int, 0>{});
       if constexpr (KT == 64) step(std::integral_constant<int, 32>{});
     }
 #pragma unroll 1
     for (; __builtin_expect(bad != 0, 0); bad &= bad - 1)
-      restore_key<T, C, DP>(st, hd, here, __builtin_ctzll(bad), a.d, sight);
+      restore_key<T, C, DP>(st, hd, here, __builtin_ctzll(bad), a.d, Sight(jb.band, sg.p, sg.jhi, k0));
     if (x + 1 < x1) arrive(x + 1);
     here = then;
     __syncthreads();
@@ -1210,12 +1211,27 @@ __global__ __launch_bounds__(256) void k_prefix_join(const PrefixArgs a, int G, 
   __shared__ f32x2 sm[256];
   const int lg = threadIdx.x & (G - 1), w = threadIdx.x / G & (W - 1);
   const int64_t rows = (int64_t)a.T * a.H, r = (int64_t)blockIdx.x * (256 / (G * W)) + threadIdx.x / (G * W);
-  const int token = (int)(r / a.H), head = (int)(r % a.H), e = lg * 4, all = a.psplits + a.splits;
-  const bool ok = r < rows && token >= clampi(a.cu[0], 0, a.T) && token < clampi(a.cu[a.B], 0, a.T);
-  int s0 = a.psplits;
+  const bool there = r < rows;
+  const int token = (int)((uint32_t)r / (uint32_t)a.H), head = (int)((uint32_t)r % (uint32_t)a.H), e = lg * 4;   // (rows < 2^29)
+  const int all = a.psplits + a.splits;
+  f32x2 x[4];
+  f32x4 y[4];
+  // (parts of a prefix that the row does not have are read, but not added: nothing waits to know)
+  auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int s = s0 + i * W;
+      const bool ok = there && s < all;
+      x[i] = ok ? *part_sums(a, rows * s + r) : f32x2{neg_inf(), 0.0f};
+      y[i] = ok && e < a.d ? *reinterpret_cast<const f32x4*>(a.part + (rows * s + r) * a.d + e) : f32x4{};
+    }
+  };
+  load(w);
+  const bool ok = there && token >= clampi(a.cu[0], 0, a.T) && token < clampi(a.cu[a.B], 0, a.T);
+  int first = a.psplits;
   if (a.P) {
-    auto first = [&](int g) { return clampi(a.cu[clampi(a.cu_seq[g], 0, a.B)], 0, a.T); };
-    if (token >= first(0) && token < first(a.P)) s0 = 0;
+    auto at = [&](int g) { return clampi(a.cu[clampi(a.cu_seq[g], 0, a.B)], 0, a.T); };
+    if (token >= at(0) && token < at(a.P)) first = 0;
   }
   float m = neg_inf(), sum = 0.0f;
   f32x4 o = {};
@@ -1227,19 +1243,13 @@ __global__ __launch_bounds__(256) void k_prefix_join(const PrefixArgs a, int G, 
     o = o * f + y * g;
     m = up;
   };
-  if (ok) {
-    for (s0 += w; s0 < all; s0 += 4 * W) {
-      f32x2 x[4];
-      f32x4 y[4];
+  for (int s0 = w;;) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = s0 + i * W;
-        x[i] = s < all ? *part_sums(a, rows * s + r) : f32x2{neg_inf(), 0.0f};
-        y[i] = s < all && e < a.d ? *reinterpret_cast<const f32x4*>(a.part + (rows * s + r) * a.d + e) : f32x4{};
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) add(x[i], y[i]);
-    }
+    for (int i = 0; i < 4; ++i)
+      if (ok && s0 + i * W >= first && s0 + i * W < all) add(x[i], y[i]);
+    s0 += 4 * W;
+    if (s0 >= all) break;
+    load(s0);
   }
   if (W > 1) {
     so[threadIdx.x] = o;
@@ -1303,7 +1313,7 @@ hipError_t run(const PrefixArgs& a, hipStream_t s) {
     int G = 1, W = 1;
     while (G * 4 < a.d) G *= 2;
     const int64_t rows = (int64_t)a.T * a.H;
-    while (G * W < 256 && 4 * W < a.psplits + a.splits && rows * G * W < 256 * 256) W *= 2;
+    while (G * W < 256 && 4 * W < a.psplits + a.splits && rows * G * W < 1024 * 256) W *= 2;
     const int per = 256 / (G * W);
     k_prefix_join<T><<<(unsigned)((rows + per - 1) / per), 256, 0, s>>>(a, G, W);
   }
