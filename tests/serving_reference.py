@@ -63,7 +63,8 @@ class Cache:
             for b, n in enumerate(ns):
                 both = []
                 for w in range(2):
-                    x = torch.randn(max(n, 0), Hkv, d, generator=g) * torch.exp(0.3 * torch.randn(max(n, 0), Hkv, 1, generator=g))
+                    x = torch.randn(max(n, 0), Hkv, d, generator=g, dtype=torch.float32)
+                    x = x * torch.exp(0.3 * torch.randn(max(n, 0), Hkv, 1, generator=g, dtype=torch.float32))
                     x = (x * scale).to(dtype)
                     j = torch.arange(max(n, 0))
                     at = (table[b, j // page].long(), j % page)

@@ -168,15 +168,15 @@ def test_codes_are_the_type_that_torch_has():
 
 def test_rounding_is_that_of_the_type():
     g = torch.Generator().manual_seed(1)
-    x = torch.cat([torch.randn(4000, generator=g) * 2.0 ** torch.randint(-12, 7, (4000,), generator=g), torch.tensor([448.0, 0.0, 2.0 ** -10, 3 * 2.0 ** -10]),
-                   torch.tensor([17 / 16, 19 / 16, 2.0 ** -9 * 2.5])]).clamp(-448, 448)
+    x = torch.randn(4000, generator=g, dtype=torch.float32) * 2.0 ** torch.randint(-12, 7, (4000,), generator=g).float()
+    x = torch.cat([x, torch.tensor([448.0, 0.0, 2.0 ** -10, 3 * 2.0 ** -10, 17 / 16, 19 / 16, 2.0 ** -9 * 2.5], dtype=torch.float32)]).clamp(-448, 448)
     code = nearest(x.double()) + 128 * torch.signbit(x).long()
     assert torch.equal(code.to(torch.uint8), x.to(torch.float8_e4m3fn).view(torch.uint8))
 
 
 def test_a_scale_is_the_smallest_that_takes_the_largest_element():
     g = torch.Generator().manual_seed(2)
-    x = torch.randn(300, 32, generator=g) * 2.0 ** torch.randint(-140, 127, (300, 1), generator=g).float()
+    x = torch.randn(300, 32, generator=g, dtype=torch.float32) * 2.0 ** torch.randint(-140, 127, (300, 1), generator=g).float()
     x[:5] = 0
     c, s = quantise(x)
     a = x.double().abs().amax(-1)

@@ -61,9 +61,9 @@ def hard_vectors(d, dtype):
         x[i] *= 0.1
         x[i, 0] = (448.0, 446.0, 450.0, 1.75, 1.765625, 1.7421875, -448.0, 2.0, 1.0, -1.75)[i - 10]
     for i in range(20, 30):                   # ties between two numbers, and beside them
-        x[i] = torch.tensor([(2 * k + 17) / 32 * (1 + (0, 2.0 ** -7, -2.0 ** -7)[i % 3]) for k in range(d)]) * 0.25
+        x[i] = torch.tensor([(2 * k + 17) / 32 * (1 + (0, 2.0 ** -7, -2.0 ** -7)[i % 3]) for k in range(d)], dtype=F32) * 0.25
         x[i, 0] = 448.0 if i % 2 else 1.75
-    x[30] = torch.tensor([(2 * k + 1) * 2.0 ** -10 for k in range(d)])      # ties of numbers below the least normal one
+    x[30] = torch.tensor([(2 * k + 1) * 2.0 ** -10 for k in range(d)], dtype=F32)      # ties of numbers below the least normal one
     x[30, 0] = 448.0
     return x.to(dtype)
 
@@ -154,7 +154,7 @@ def test_read_of_whole_sequences_and_of_what_is_not_there():
     P.paged_read_e4m3(*c.on(DEV), table.to(DEV), i32(lens), i32(cu), cu[-1] + 2, out=out)
     for w in range(2):
         for b in range(4):
-            want = torch.cat([torch.zeros(4, Hkv, d), c.kv[b][w].transpose(0, 1).float()])
+            want = torch.cat([torch.zeros(4, Hkv, d, dtype=F32), c.kv[b][w].transpose(0, 1).float()])
             if b == 2:
                 want[4 + 16:4 + 32] = 0
             if b in (0, 3):
@@ -644,13 +644,13 @@ def test_work_on_a_given_stream_beside_the_current_one():
     junk = []
     for _ in range(4):
         s = side.cuda_stream
-        big = torch.full((1 << 22,), 3.0, device=DEV)
+        big = torch.full((1 << 22,), 3.0, dtype=F32, device=DEV)
         del big                                              # its memory is free for the current stream only
         tables = (c["table"], lens, cu)
         o = P.paged_attention_e4m3(q, *c["caches"], *tables, window=60, stream=s)
         p = P.paged_prefix_attention(q, *c["caches"][:2], c["ptable"], plen, seqs, *tables, k_scale=c["caches"][2],
                                      v_scale=c["caches"][3], sinks=2, window=200, stream=s)
-        junk.append(torch.full((1 << 20,), float("nan"), device=DEV))
+        junk.append(torch.full((1 << 20,), float("nan"), dtype=F32, device=DEV))
         k, v = P.paged_read_e4m3(*c["caches"], *tables, q.shape[0], stream=s)
         P.paged_append_e4m3(kv[0], kv[1], *c["caches"], *tables, stream=s)
         side.synchronize()
