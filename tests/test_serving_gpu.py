@@ -386,6 +386,64 @@ def test_nan_in_pages_reach_every_row_that_sees_them_and_no_other(i, codes, pref
         assert bool(torch.isnan(hit[..., cols]).all()), (own_key, at)
 
 
+# lens, new, H, Hkv, d, options
+NO_NUMBERS = [
+    ([300, 40], [1, 1], 4, 2, 64, {}),                    # 16 rows, two heads a workgroup
+    ([5000, 40], [1, 2], 4, 1, 128, {}),                  # keys in parts
+    ([5000], [1], 2, 1, 64, dict(window=3000)),
+    ([200, 90], [9, 5], 4, 2, 128, dict(window=50)),      # 32 rows
+    ([200, 150], [150, 90], 4, 2, 64, dict(window=50, sinks=2)),
+    ([9, 30], [12, 1], 2, 1, 256, {}),                    # rows that their sequence does not hold
+]
+
+
+@types
+@pytest.mark.parametrize("codes,prefix", [(True, None), (True, 75), (True, 0), (False, 75), (False, 0)],
+                         ids=["e4m3", "e4m3-prefix", "e4m3-empty-prefix", "plain-prefix", "plain-empty-prefix"])
+@pytest.mark.parametrize("i", range(len(NO_NUMBERS)))
+def test_queries_that_are_no_numbers_give_none(i, codes, prefix, dtype):
+    lens, new, H, Hkv, d, opt = NO_NUMBERS[i]
+    plen, seqs = ([], [0]) if prefix is None else ([prefix], [0, len(lens)])
+    c = Cache(lens, Hkv, d, 16, dtype, codes, 700 + i, prefixes=plen)
+    cu = offsets(new)
+    q = rnd(i, cu[-1], H, d, dtype=dtype).to(DEV)
+    print(f"[gpu] queries of nan {NO_NUMBERS[i]} {codes} {prefix} {dtype}", flush=True)
+
+    def call(q):
+        out = torch.full_like(q, 7.0)
+        if prefix is not None:
+            return prefix_call(c, q, out, plen, seqs, lens, cu, **opt)
+        return P.paged_attention_e4m3(q, *c.on(DEV), c.table.to(DEV), i32(lens), i32(cu), out=out, **opt)
+
+    base = call(q)
+    for token, head in {(0, 0), (cu[-1] - 1, H - 1), (cu[-1] // 2, H // 2)}:
+        spoilt = q.clone()
+        spoilt[token, head, d // 2] = math.nan
+        got = call(spoilt)
+        b = max(x for x in range(len(lens)) if cu[x] <= token)
+        if lens[b] - (cu[b + 1] - token) >= 0:            # a row that sees a key
+            assert bool(torch.isnan(got[token, head].float()).all()), (token, head)
+        else:
+            assert bool((got[token, head] == 0).all()), (token, head)
+        got[token, head] = base[token, head]
+        same(got, base, (token, head))
+
+
+@types
+@pytest.mark.parametrize("codes,prefix", [(True, False), (True, True), (False, True)], ids=["e4m3", "e4m3-prefix", "plain-prefix"])
+def test_a_key_of_nan_that_is_all_a_row_sees(codes, prefix, dtype):
+    plen, seqs = ([20], [0, 1]) if prefix else ([], [0])
+    c = Cache([3000, 30], 1, 64, 16, dtype, codes, 9, prefixes=plen)
+    lens, cu = [3000, 30], [0, 1, 2]
+    q = rnd(4, 2, 2, 64, dtype=dtype).to(DEV)
+    slot = c.cache[0][c.table[0, 2999 // 16], 2999 % 16]
+    slot[..., 5] = 0x7f if codes else math.nan
+    opt = dict(window=1)
+    got = (prefix_call(c, q, torch.full_like(q, 7.0), plen, seqs, lens, cu, **opt) if prefix else
+           P.paged_attention_e4m3(q, *c.on(DEV), c.table.to(DEV), i32(lens), i32(cu), **opt))
+    assert bool(torch.isnan(got[0].float()).all()) and bool(torch.isfinite(got[1].float()).all())
+
+
 @pytest.mark.parametrize("codes", [False, True], ids=["plain", "e4m3"])
 @pytest.mark.parametrize("new", [[3, 1], [90, 60]])
 def test_pages_outside_the_cache_hold_nothing(new, codes):
