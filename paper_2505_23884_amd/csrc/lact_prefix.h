@@ -1164,6 +1164,26 @@ __device__ __forceinline__ void work(const PrefixArgs& a, const Offsets& off, co
   }
 }
 
+// Job j of a role whose workgroups have HP key heads: part u of the keys of a
+// row tile, and the first head. Where a slot's heads share lines of memory (128
+// bytes), those of one part are 8 jobs apart, so that one XCD works on them at about
+// the same time and reads a line once: decoding of 64 sequences of up to 16384, 4 heads of
+// 80 in 8 bits, 131 us for 189, of 96 181 for 212; 32 x 10 tokens over up to 6001, 8 heads of 64,
+// 49 for 65. Heads of whole lines are neighbours: 64 sequences, heads of 128, 171 us for 175.
+template <class C, int HP>
+__device__ __forceinline__ void place_of_job(const PrefixArgs& a, int j, int& u, int& head) {
+  const int n = a.Hkv / HP;
+  constexpr uint32_t BYTES = HP * sizeof(typename std::conditional<std::is_same<C, Code>::value, uint8_t, C>::type);
+  if ((uint32_t)a.c.sh * BYTES & 127) {
+    const int i = j >> 3, q = i / n;
+    u = q << 3 | (j & 7);
+    head = (i - q * n) * HP;
+  } else {
+    u = j / n;
+    head = (j - u * n) * HP;
+  }
+}
+
 // PS, OS: the shapes of the rows over prefixes (or kNone) and over a sequence's own keys.
 template <typename T, class C, int DP, int PS, int OS>
 __global__ __launch_bounds__(64 * kWaves, (occupancy<T, C, DP, PS, OS>())) void k_prefix(const PrefixArgs a) {
@@ -1177,26 +1197,29 @@ __global__ __launch_bounds__(64 * kWaves, (occupancy<T, C, DP, PS, OS>())) void 
   jb.band = Band{a.win, 0, a.sinks};
   if constexpr (PS != kNone) {
     if ((int)blockIdx.x < a.pjobs) {
-      const int n = a.Hkv / P::HP, heads = n * a.psplits, t = (int)blockIdx.x / heads, y = (int)blockIdx.x - t * heads;
+      int u, head;
+      place_of_job<C, P::HP>(a, (int)blockIdx.x, u, head);
+      const int t = u / a.psplits;
       if (!find_tile<true>(a, off, t, P::R, s, jb.r0)) return;
       jb.table = a.ptable + (int64_t)s.b * a.p_pages;
       jb.t0 = s.t0;
       jb.rows = s.rows;
       jb.len = s.len;
-      jb.split = jb.part = y / n;
+      jb.split = jb.part = u - t * a.psplits;
       jb.splits = a.psplits;
-      work<T, C, DP, PS, true>(a, off, jb, 0, y % n * P::HP, smem, words);
+      work<T, C, DP, PS, true>(a, off, jb, 0, head, smem, words);
       return;
     }
   }
-  const int job = (int)blockIdx.x - (PS != kNone ? a.pjobs : 0), n = a.Hkv / O::HP, heads = n * a.splits;
-  const int t = job / heads, y = job - t * heads;
+  int u, head;
+  place_of_job<C, O::HP>(a, (int)blockIdx.x - (PS != kNone ? a.pjobs : 0), u, head);
+  const int t = u / a.splits;
   if (!find_tile<false>(a, off, t, O::R, s, jb.r0)) return;
   jb.table = a.table + (int64_t)s.b * a.max_pages;
   jb.t0 = s.t0;
   jb.rows = s.rows;
   jb.len = s.len;
-  jb.split = y / n;
+  jb.split = u - t * a.splits;
   jb.splits = a.splits;
   jb.part = PS != kNone || a.splits > 1 ? a.psplits + jb.split : -1;
   if constexpr (PS != kNone) {
@@ -1205,7 +1228,7 @@ __global__ __launch_bounds__(64 * kWaves, (occupancy<T, C, DP, PS, OS>())) void 
       if (g >= 0) jb.band.sinks = max(0, a.sinks - clampi(a.plen[g], 0, a.p_pages * a.page));
     }
   }
-  work<T, C, DP, OS, false>(a, off, jb, s.p0, y % n * O::HP, smem, words);
+  work<T, C, DP, OS, false>(a, off, jb, s.p0, head, smem, words);
 }
 
 // The parts of each (token, head), joined in a fixed order: those over its
@@ -1275,15 +1298,15 @@ __global__ __launch_bounds__(256) void k_prefix_join(const PrefixArgs a, int G, 
 }
 
 int shape_rows(int shape) { return shape == kRows128 ? 128 : shape == kRows16 || shape == kPairs16 ? 16 : 32; }
-// Workgroups of one part of the keys: row tiles of n sequences or groups, times (pairs of) key heads.
-int row_jobs(const PrefixArgs& a, int shape, int n) {
+// Workgroups: row tiles of n sequences or groups, in parts, by eights, times (pairs of) key heads.
+int row_jobs(const PrefixArgs& a, int shape, int n, int splits) {
   const int tiles = (int)((int64_t)a.T * a.G / shape_rows(shape)) + n;
-  return tiles * (shape == kPairs16 ? a.Hkv / 2 : a.Hkv);
+  return (tiles * splits + 7) / 8 * 8 * (shape == kPairs16 ? a.Hkv / 2 : a.Hkv);
 }
 
 template <typename T, class C, int DP, int PS, int OS>
 void start(const PrefixArgs& a, hipStream_t s) {
-  const unsigned jobs = (unsigned)(a.pjobs + row_jobs(a, OS, a.B) * a.splits);
+  const unsigned jobs = (unsigned)(a.pjobs + row_jobs(a, OS, a.B, a.splits));
   k_prefix<T, C, DP, PS, OS><<<jobs, 64 * kWaves, 0, s>>>(a);
 }
 

@@ -56,7 +56,7 @@ void prefix_plan(PrefixArgs& a, bool bf16, bool codes) {
   a.pshape = rows > 32 * (int64_t)a.P || a.shape == kRows128 || (a.shape == kRows32 && !fp32) ? kRows128 : kRows32;
   const int64_t shared = keys(a.p_pages);
   a.psplits = best_parts(jobs(a.pshape, a.P), shared, rate(a.pshape), (int64_t)a.T * a.H, a.d, most(shared, 64), true);
-  a.pjobs = row_jobs(a, a.pshape, a.P) * a.psplits;
+  a.pjobs = row_jobs(a, a.pshape, a.P, a.psplits);
 }
 
 hipError_t launch_prefix(const PrefixArgs& a, bool bf16, hipStream_t s) {
