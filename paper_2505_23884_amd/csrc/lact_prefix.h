@@ -230,8 +230,8 @@ template <typename T, int DP, int KT, int NT>
 struct Stage<T, Code, DP, KT, NT> {
   using L = Tile<T, DP>;
   static constexpr int CPR = DP / 16;   // 16 numbers a load
-  static constexpr int ALL = KT * CPR, N = ALL < NT ? 1 : ALL / NT, STEP = NT / CPR;
-  static_assert(ALL < NT || ALL % NT == 0, "tile split");
+  static constexpr int N = KT * CPR / NT, STEP = NT / CPR;
+  static_assert(N >= 1 && KT * CPR % NT == 0, "tile split");
   u32x4 k[N], v[N];
   int kb, vb;   // scales of the lane's key
   static __device__ __forceinline__ int row(int i) { return threadIdx.x % NT / CPR + i * STEP; }
@@ -242,28 +242,18 @@ struct Stage<T, Code, DP, KT, NT> {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int64_t o = shfl64(s.at, row(i) & 63);
-      const bool ok = o >= 0 && e < d && (ALL >= NT || row(i) < KT);
+      const bool ok = o >= 0 && e < d;
       k[i] = load16(ok, h.k + o + e);
       v[i] = load16(ok, h.v + o + e);
     }
   }
-  // a NaN among the values, or a scale that can make an infinity of one
-  __device__ __forceinline__ bool any_nonfinite() const {
-    uint32_t bad = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) bad |= (v[i][x] & 0x7f7f7f7fu) + 0x01010101u;
-    return (bad & 0x80808080u) || vb > kMaxExp + 127;
-  }
-  __device__ __forceinline__ void put(uint8_t* kt, uint8_t* vt, bool scrubbed) {
+  __device__ __forceinline__ void put(uint8_t* kt, uint8_t* vt) {
     constexpr int W = 4 * (int)sizeof(T);   // words of 16 elements
     const int c = threadIdx.x % CPR * (W / 4);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = row(i);
       const float ks = scale_of(__shfl(kb, r & 63, 64)), vs = scale_of(__shfl(vb, r & 63, 64));
-      if (ALL < NT && r >= KT) continue;
       uint32_t w[W];
 #pragma unroll
       for (int x = 0; x < 4; ++x) widen<T>(k[i][x], ks, w + x * W / 4);
@@ -272,10 +262,6 @@ struct Stage<T, Code, DP, KT, NT> {
         *reinterpret_cast<u32x4*>(kt + L::off(r, c + x / 4)) = u32x4{w[x], w[x + 1], w[x + 2], w[x + 3]};
 #pragma unroll
       for (int x = 0; x < 4; ++x) widen<T>(v[i][x], vs, w + x * W / 4);
-      if (__builtin_expect(scrubbed, 0)) {
-#pragma unroll
-        for (int x = 0; x < W; ++x) w[x] = finite_or_zero<T>(w[x]);
-      }
 #pragma unroll
       for (int x = 0; x < W; x += 4)
         *reinterpret_cast<u32x4*>(vt + L::off(r, c + x / 4)) = u32x4{w[x], w[x + 1], w[x + 2], w[x + 3]};
@@ -415,7 +401,7 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
   st.init();
   const float c = a.scale * kLog2e;
   arrived(q);
-  constexpr bool PIPED = CODES && sizeof(T) == 2 && DP <= 128;
+  constexpr bool PIPED = CODES && DP <= 128;
   // (addresses as in mma_dot_add() and mma_rows(): chunks by flipping bits of the first one's)
   typedef __attribute__((address_space(3))) const u32x4 lds_u4;
   typedef __attribute__((address_space(3))) s16x4 lds_s4;
@@ -443,7 +429,7 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
     return p;
   };
   auto tile_of = [&](int x) __attribute__((always_inline)) { return smem + ((x - x0) & 1) * 2 * BYTES; };
-  Stage<T, Code, DP, KT, NT> stage;
+  [[maybe_unused]] typename std::conditional<CODES, Stage<T, Code, DP, KT, NT>, Softmax<1>>::type stage;
   auto copy = [&](int x, const Slot<C>& s) __attribute__((always_inline)) {
     if constexpr (CODES) {
       stage.load(hd, s, a.d);
@@ -465,7 +451,7 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
     }
   };
   auto arrive = [&](int x) __attribute__((always_inline)) {
-    if constexpr (CODES) stage.put(tile_of(x), tile_of(x) + BYTES, false);
+    if constexpr (CODES) stage.put(tile_of(x), tile_of(x) + BYTES);
   };
   Slot<C> here(a, place(x0));
   Place next = place(x0 + 1);
@@ -686,7 +672,11 @@ struct Slim {
   static constexpr int ST = DP / 32, DB = DP / 16;
   static constexpr int NQ = sizeof(T) == 4 ? 3 : 1, NP = sizeof(T) == 4 ? 3 : 2;
   static constexpr int VB = 32 * PITCH, WAVE = 2 * VB + 256 * HP, SUMS = NY * (4 * DB + 2) * 256;
-  static constexpr int SMEM = kWaves * WAVE > 2 * SUMS ? kWaves * WAVE : 2 * SUMS;
+  // 32 fp32 queries of 128 in their three parts are 96 registers (67 and more spilled): they stay in LDS, behind the
+  // waves' tiles (6 chunks of 200 tokens over 4096 to 8192, 16 / 4 heads of 128: 186 us for 387).
+  static constexpr bool QLDS = NQ == 3 && NY == 2 && DP >= 128;
+  static constexpr int QUERIES = QLDS ? NY * NQ * ST * 1024 : 0;
+  static constexpr int SMEM = kWaves * WAVE + QUERIES > 2 * SUMS ? kWaves * WAVE + QUERIES : 2 * SUMS;
   static_assert(CPH >= 4, "four chunks a head at least");
 
   // The row of LDS that a key's values have, and its chunks' order: the 16
@@ -885,29 +875,35 @@ struct Slim {
     int x = x0 + wave;
     const Place at0 = place(x);
     Place next = place(x + kWaves);
-    bf16x8 q[NY][NQ][ST];
+    bf16x8 q[QLDS ? 1 : NY][NQ][QLDS ? 1 : ST];
+    u32x4* const qs = reinterpret_cast<u32x4*>(smem + kWaves * WAVE) + lane;
+    static_assert(!QLDS || ST % kWaves == 0, "steps of the queries a wave");
 #pragma unroll
     for (int y = 0; y < NY; ++y)
 #pragma unroll
-      for (int s = 0; s < ST; ++s) {
-        const int e = query_at(s);
+      for (int s0 = 0; s0 < (QLDS ? ST / kWaves : ST); ++s0) {
+        const int s = QLDS ? s0 * kWaves + wave : s0, e = query_at(s);
         const T* at = reinterpret_cast<const T*>(a.q.p) + row[y].token * a.q.st + row[y].head * a.q.sh + e;
         const bool ok = row[y].ok && e < a.d;
         if constexpr (sizeof(T) == 2) {
-          q[y][0][s] = __builtin_bit_cast(bf16x8, load16(ok, at));
+          q[y][0][s0] = __builtin_bit_cast(bf16x8, load16(ok, at));
         } else {
           const f32x4 lo = __builtin_bit_cast(f32x4, load16(ok, at)), hi = __builtin_bit_cast(f32x4, load16(ok, at + 4));
           const float f[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
           bf16x8 p[NQ];
           parts<NQ, false>(f, p);
 #pragma unroll
-          for (int k = 0; k < NQ; ++k) q[y][k][s] = p[k];
+          for (int k = 0; k < NQ; ++k) {
+            if constexpr (QLDS) qs[((y * NQ + k) * ST + s) * 64] = __builtin_bit_cast(u32x4, p[k]);
+            else q[y][k][s0] = p[k];
+          }
         }
       }
     Slot<C> here(a, at0);
     Tile32 t;
     if (x < x1) t.load(a, hd, here);
-    arrived(q);
+    if constexpr (QLDS) __syncthreads();
+    else arrived(q);
     Sums st;
 #pragma unroll
     for (int y = 0; y < NY; ++y) {
@@ -934,22 +930,43 @@ struct Slim {
       f32x4 s[NY][2];
 #pragma unroll
       for (int y = 0; y < NY; ++y) s[y][0] = s[y][1] = f32x4{};
+      if constexpr (QLDS) {
 #pragma unroll
-      for (int i = 0; i < LK * HP; ++i)
+        for (int i = 0; i < LK; ++i) {
+          u32x4 chunk[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int hp = i / LK, ih = i % LK;
-          const u32x4 chunk = *reinterpret_cast<const u32x4*>(ks + off(16 * u + n, hp * CPH + g + 4 * ih));
+          for (int u = 0; u < 2; ++u) chunk[u] = *reinterpret_cast<const u32x4*>(ks + off(16 * u + n, g + 4 * i));
 #pragma unroll
-          for (int h = 0; h < (CODES ? 2 : 1); ++h) {
-            const bf16x8 kr = rows(chunk, h);
+          for (int h = 0; h < 2; ++h) {
+            const bf16x8 kr[2] = {rows(chunk[0], h), rows(chunk[1], h)};
 #pragma unroll
-            for (int y = hp * NR; y < (hp + 1) * NR; ++y)
+            for (int y = 0; y < NY; ++y)
 #pragma unroll
-              for (int p = NQ - 1; p >= 0; --p)
-                s[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr, q[y][p][CODES ? 2 * ih + h : ih], s[y][u], 0, 0, 0);
+              for (int p = NQ - 1; p >= 0; --p) {
+                const bf16x8 part = __builtin_bit_cast(bf16x8, qs[((y * NQ + p) * ST + 2 * i + h) * 64]);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) s[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[u], part, s[y][u], 0, 0, 0);
+              }
           }
         }
+      } else {
+#pragma unroll
+        for (int i = 0; i < LK * HP; ++i)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int hp = i / LK, ih = i % LK;
+            const u32x4 chunk = *reinterpret_cast<const u32x4*>(ks + off(16 * u + n, hp * CPH + g + 4 * ih));
+#pragma unroll
+            for (int h = 0; h < (CODES ? 2 : 1); ++h) {
+              const bf16x8 kr = rows(chunk, h);
+#pragma unroll
+              for (int y = hp * NR; y < (hp + 1) * NR; ++y)
+#pragma unroll
+                for (int p = NQ - 1; p >= 0; --p)
+                  s[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr, q[y][p][CODES ? 2 * ih + h : ih], s[y][u], 0, 0, 0);
+            }
+          }
+      }
       float kf[HP][2][4], vf[HP][2][4];
 #pragma unroll
       for (int hp = 0; hp < HP; ++hp)
@@ -1316,23 +1333,26 @@ hipError_t run(const PrefixArgs& a, hipStream_t s) {
   if constexpr (FP32 && DP == 256) {                // a wave's own tile would not fit
     start<T, C, DP, kRows128, kRows128>(a, s);
   } else {
-    constexpr bool PAIRS = CODES && DP == 64;
+    constexpr bool PAIRS = CODES && DP == 64, PARTS = CODES && sizeof(T) == 4;
     constexpr int k16 = FP32 ? kRows32 : kRows16;   // (an fp32 cache has one shape of few rows)
     constexpr int p16 = PAIRS ? kPairs16 : k16;
+    // (fp32 queries over e4m3 numbers, whose bf16 products are those of the 32 rows: chunks of 200 tokens over 4096 to
+    // 8192, 16 / 4 heads of 128, 186 us, and 128 rows with fp32 products 611; 12 of 160 behind 8192 keys 322 and 1094)
+    constexpr int kMany = PARTS ? kRows32 : kRows128;
     if (!a.P) {
       if constexpr (CODES) {                        // (the other kinds have their own entry point)
-        if (a.shape == kRows128) start<T, C, DP, kNone, kRows128>(a, s);
+        if (a.shape == kRows128) start<T, C, DP, kNone, kMany>(a, s);
         else if (a.shape == kRows32) start<T, C, DP, kNone, kRows32>(a, s);
         else if (a.shape == kRows16) start<T, C, DP, kNone, kRows16>(a, s);
         else start<T, C, DP, kNone, p16>(a, s);
       }
     } else if (a.shape == kRows128) {
-      start<T, C, DP, kRows128, kRows128>(a, s);
+      start<T, C, DP, kMany, kMany>(a, s);
     } else if (a.shape == kRows32 && !FP32) {
-      start<T, C, DP, kRows128, kRows32>(a, s);
+      start<T, C, DP, kMany, kRows32>(a, s);
     } else if (a.pshape == kRows128) {
-      if (a.shape == kPairs16) start<T, C, DP, kRows128, p16>(a, s);
-      else start<T, C, DP, kRows128, k16>(a, s);
+      if (a.shape == kPairs16) start<T, C, DP, kMany, p16>(a, s);
+      else start<T, C, DP, kMany, k16>(a, s);
     } else if (a.shape == kPairs16) {
       start<T, C, DP, kRows32, p16>(a, s);
     } else {

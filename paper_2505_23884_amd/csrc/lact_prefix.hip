@@ -38,7 +38,9 @@ void prefix_plan(PrefixArgs& a, bool bf16, bool codes) {
   const bool fp32 = !bf16 && !codes, pairs = codes && a.d <= 64 && a.Hkv % 2 == 0;
   const int rows16 = fp32 ? kRows32 : pairs ? kPairs16 : kRows16;
   const int64_t rows = (int64_t)a.T * a.G;
-  a.shape = rows > 32 * (int64_t)a.B || (fp32 && a.d > 128) ? kRows128 : rows > 16 * (int64_t)a.B ? kRows32 : rows16;
+  // (fp32 queries over e4m3 numbers: 32 rows at most, as run() has it)
+  const int many = codes && !bf16 ? kRows32 : kRows128;
+  a.shape = rows > 32 * (int64_t)a.B || (fp32 && a.d > 128) ? many : rows > 16 * (int64_t)a.B ? kRows32 : rows16;
   // workgroups a part: as many as there would be if the tokens were spread evenly
   auto jobs = [&](int shape, int n) {
     const int R = shape_rows(shape);
@@ -53,7 +55,7 @@ void prefix_plan(PrefixArgs& a, bool bf16, bool codes) {
   a.splits = best_parts(jobs(a.shape, a.B) * (a.P ? 2 : 1), own, rate(a.shape), (int64_t)a.T * a.H, a.d, most(own, 32), a.P > 0);
   if (!a.P) return;
   // (32 rows of prefixes go with 16 of sequences, or 32 of an fp32 cache)
-  a.pshape = rows > 32 * (int64_t)a.P || a.shape == kRows128 || (a.shape == kRows32 && !fp32) ? kRows128 : kRows32;
+  a.pshape = rows > 32 * (int64_t)a.P || a.shape == kRows128 || (a.shape == kRows32 && !fp32) ? many : kRows32;
   const int64_t shared = keys(a.p_pages);
   a.psplits = best_parts(jobs(a.pshape, a.P), shared, rate(a.pshape), (int64_t)a.T * a.H, a.d, most(shared, 64), true);
   a.pjobs = row_jobs(a, a.pshape, a.P, a.psplits);
