@@ -264,9 +264,8 @@ __global__ __launch_bounds__(256) void k_paged_join(const PagedArgs a, int G, in
   float m = neg_inf(), sum = 0.0f;
   f32x4 o = {};
   auto add = [&](f32x2 x, f32x4 y) __attribute__((always_inline)) {
-    const float up = fmaxf(m, x[0]);
-    if (up == neg_inf()) return;
-    const float f = __builtin_amdgcn_exp2f(m - up), g = __builtin_amdgcn_exp2f(x[0] - up);
+    const float up = fmaxf(m, x[0]), top = up == neg_inf() ? 0.0f : up;   // (scores of NaN alone leave a NaN of a sum, and no maximum)
+    const float f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(x[0] - top);
     sum = sum * f + x[1] * g;
     o = o * f + y * g;
     m = up;

@@ -994,3 +994,46 @@ def test_tokens_over_pages_are_rounded_once(lens, new, H, Hkv, d, page, opt):
             x, j = q[cu[b]:cu[b + 1], h].cpu(), h // (H // Hkv)
             r = head(x, K[b][0, j], V[b][0, j], see, d ** -0.5)
             check(f"{b} {h}", o[cu[b]:cu[b + 1], h], r["o"], r["o_mag"] * (r["e"] + 2.0 ** -15 + n * 2.0 ** -24) * 1.01 + r["o"].abs() * HALF[BF])
+
+
+# lens, new, H, Hkv, d, options; the keys in parts or not, by 32 rows a workgroup or 128
+NO_NUMBERS = [
+    ([300, 40], [1, 1], 4, 2, 64, {}),
+    ([5000, 40], [1, 2], 4, 1, 128, {}),
+    ([5000], [1], 2, 1, 64, dict(window=3000)),
+    ([30], [2], 2, 2, 256, {}),
+    ([200, 150], [150, 90], 4, 2, 64, dict(window=50, sinks=2)),
+    ([1100, 700], [200, 90], 4, 2, 128, dict(sinks=70, window=400)),
+    ([1300, 3], [150, 9], 4, 1, 64, {}),                  # rows that their sequence does not hold
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("i", range(len(NO_NUMBERS)))
+def test_queries_over_pages_that_are_no_numbers_give_none(i, dtype):
+    lens, new, H, Hkv, d, opt = NO_NUMBERS[i]
+    q, kc, vc, table, ln, cu_new, _, _, cu = paged_setup(lens, new, H, Hkv, d, 16, dtype, seed=500 + i)
+    q = q[:cu[-1]].contiguous()
+    print(f"[gpu] queries of nan over pages {NO_NUMBERS[i]} {dtype}", flush=True)
+    base = P.paged_attention(q, kc, vc, table, ln, cu_new, **opt)
+    for token, h in {(0, 0), (cu[-1] - 1, H - 1), (cu[-1] // 2, H // 2)}:
+        spoilt = q.clone()
+        spoilt[token, h, d // 2] = math.nan
+        got = P.paged_attention(spoilt, kc, vc, table, ln, cu_new, **opt)
+        b = max(x for x in range(len(lens)) if cu[x] <= token)
+        if lens[b] - (cu[b + 1] - token) >= 0:            # a row that sees a key
+            assert bool(torch.isnan(got[token, h].float()).all()), (token, h)
+        else:
+            assert bool((got[token, h] == 0).all()), (token, h)
+        got[token, h] = base[token, h]
+        assert torch.equal(got, base), (token, h)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("lens", [[3000, 30], [20, 30]], ids=["parts", "whole"])
+def test_a_key_of_nan_that_is_all_a_row_sees(lens, dtype):
+    q, kc, vc, table, ln, cu_new, _, _, cu = paged_setup(lens, [1, 1], 2, 1, 64, 16, dtype, seed=9)
+    p = lens[0] - 1
+    kc[table[0, p // 16], p % 16, :, 5] = math.nan
+    o = P.paged_attention(q[:2].contiguous(), kc, vc, table, ln, cu_new, window=1)
+    assert bool(torch.isnan(o[0].float()).all()) and bool(torch.isfinite(o[1].float()).all())
