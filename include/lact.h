@@ -753,7 +753,9 @@ int lact_paged_attention_e4m3(const lact_paged_desc* desc, const lact_view* q, c
  *
  * groups >= 1 (else LACT_EINVAL); groups * Hkv <= 2^20; the pages of a
  * prefix and of a sequence together hold at most 2^29 positions; the other
- * limits of lact_paged_attention.
+ * limits of lact_paged_attention, but n_new * H <= 2^27 (up to 2^28 where
+ * the launch has fewer than 2^24 workgroups, else LACT_EUNSUPPORTED, also from
+ * the workspace's size).
  */
 typedef struct lact_prefix {
   int32_t groups, max_pages;

@@ -258,9 +258,23 @@ PrefixArgs prefix_args(const lact_paged_desc* s, const lact_prefix* p, bool code
   return a;
 }
 
+// (both roles are in one direction of one launch)
+int check_jobs(const PrefixArgs& a) { return prefix_jobs(a) * 256 < ((int64_t)1 << 32) ? LACT_OK : LACT_EUNSUPPORTED; }
+
 size_t prefix_bytes(const PrefixArgs& a) {
   const int parts = a.psplits + a.splits;
   return parts > 1 ? ws_round((size_t)parts * a.T * a.H * (a.d + 2) * 4) : 0;
+}
+
+// The workspace of a call whose descriptor was found to be `rc`.
+size_t checked_bytes(const lact_paged_desc* s, const lact_prefix* p, bool codes, int rc, int* err) {
+  PrefixArgs a{};
+  if (!rc) {
+    a = prefix_args(s, p, codes);
+    rc = check_jobs(a);
+  }
+  if (err) *err = rc;
+  return rc ? 0 : prefix_bytes(a);
 }
 
 CodeArgs code_args(const lact_paged_desc* s, const lact_view* k, const lact_view* v, const lact_view* kc,
@@ -321,6 +335,7 @@ int check_rows(const lact_paged_desc* s, const lact_view* q, const lact_view* o)
 int attend(const lact_paged_desc* s, PrefixArgs& a, const lact_view* q, const lact_view* kc, const lact_view* vc,
            const int32_t* table, const int32_t* lens, const int32_t* cu, const lact_view* o, void* workspace,
            size_t bytes, void* stream) {
+  LACT_TRY(check_jobs(a));
   LACT_TRY(check_workspace(prefix_bytes(a), workspace, bytes));
   if (s->n_new == 0) return LACT_OK;
   a.q = take(q, 1, s->H, s->n_new);
@@ -565,8 +580,7 @@ int lact_paged_read_e4m3(const lact_paged_desc* desc, const lact_view* k_cache, 
 size_t lact_paged_attention_e4m3_workspace_bytes(const lact_paged_desc* desc, int* err) {
   int rc = check_paged(desc, true);
   if (!rc && desc->d % 16) rc = LACT_EUNSUPPORTED;
-  if (err) *err = rc;
-  return rc ? 0 : prefix_bytes(prefix_args(desc, nullptr, true));
+  return checked_bytes(desc, nullptr, true, rc, err);
 }
 
 int lact_paged_attention_e4m3(const lact_paged_desc* desc, const lact_view* q, const lact_view* k_cache,
@@ -585,9 +599,7 @@ int lact_paged_attention_e4m3(const lact_paged_desc* desc, const lact_view* q, c
 
 size_t lact_paged_prefix_attention_workspace_bytes(const lact_paged_desc* desc, const lact_prefix* prefix, int e4m3,
                                                    int* err) {
-  const int rc = check_prefix(desc, prefix);
-  if (err) *err = rc;
-  return rc ? 0 : prefix_bytes(prefix_args(desc, prefix, e4m3 != 0));
+  return checked_bytes(desc, prefix, e4m3 != 0, check_prefix(desc, prefix), err);
 }
 
 int lact_paged_prefix_attention(const lact_paged_desc* desc, const lact_prefix* prefix, const lact_view* q,

@@ -588,6 +588,7 @@ struct PrefixArgs : PagedArgs {
   bool codes;                // a cache of e4m3 numbers
 };
 void prefix_plan(PrefixArgs& a, bool bf16, bool codes);
+int64_t prefix_jobs(const PrefixArgs& a);   // workgroups of 256 of its launch
 hipError_t launch_prefix(const PrefixArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_prefix_bf16(const PrefixArgs& a, hipStream_t s);
 hipError_t launch_prefix_e4m3(const PrefixArgs& a, hipStream_t s);

@@ -1316,8 +1316,8 @@ __global__ __launch_bounds__(256) void k_prefix_join(const PrefixArgs a, int G, 
 
 int shape_rows(int shape) { return shape == kRows128 ? 128 : shape == kRows16 || shape == kPairs16 ? 16 : 32; }
 // Workgroups: row tiles of n sequences or groups, in parts, by eights, times (pairs of) key heads.
-int row_jobs(const PrefixArgs& a, int shape, int n, int splits) {
-  const int tiles = (int)((int64_t)a.T * a.G / shape_rows(shape)) + n;
+int64_t row_jobs(const PrefixArgs& a, int shape, int n, int splits) {
+  const int64_t tiles = (int64_t)a.T * a.G / shape_rows(shape) + n;
   return (tiles * splits + 7) / 8 * 8 * (shape == kPairs16 ? a.Hkv / 2 : a.Hkv);
 }
 

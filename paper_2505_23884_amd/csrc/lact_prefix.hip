@@ -48,18 +48,25 @@ void prefix_plan(PrefixArgs& a, bool bf16, bool codes) {
   };
   auto keys = [&](int64_t pages) { return std::min<int64_t>(pages * a.page, (int64_t)a.win + a.sinks + rows / a.G / a.B); };
   auto rate = [&](int shape) { return (shape == kRows128 ? 0.029 : 0.018) * (a.d > 128 ? 2 : 1) * (fp32 ? 3 : 1); };
-  auto most = [&](int64_t k, int limit) { return (int)std::max<int64_t>(1, std::min<int64_t>(k / (4 * kKT), limit)); };
+  // (parts that leave each role half of the 2^24 workgroups that one launch holds, or one part)
+  auto most = [&](int64_t k, int64_t limit, int shape, int n) {
+    return (int)std::max<int64_t>(1, std::min({k / (4 * kKT), limit, (1 << 23) / row_jobs(a, shape, n, 1)}));
+  };
   a.psplits = a.pjobs = 0;
   const int64_t own = keys(a.max_pages);
   // (beside a prefix they have half the room)
-  a.splits = best_parts(jobs(a.shape, a.B) * (a.P ? 2 : 1), own, rate(a.shape), (int64_t)a.T * a.H, a.d, most(own, 32), a.P > 0);
+  a.splits = best_parts(jobs(a.shape, a.B) * (a.P ? 2 : 1), own, rate(a.shape), (int64_t)a.T * a.H, a.d,
+                        most(own, 32, a.shape, a.B), a.P > 0);
   if (!a.P) return;
   // (32 rows of prefixes go with 16 of sequences, or 32 of an fp32 cache)
   a.pshape = rows > 32 * (int64_t)a.P || a.shape == kRows128 || (a.shape == kRows32 && !fp32) ? many : kRows32;
   const int64_t shared = keys(a.p_pages);
-  a.psplits = best_parts(jobs(a.pshape, a.P), shared, rate(a.pshape), (int64_t)a.T * a.H, a.d, most(shared, 64), true);
-  a.pjobs = row_jobs(a, a.pshape, a.P, a.psplits);
+  a.psplits = best_parts(jobs(a.pshape, a.P), shared, rate(a.pshape), (int64_t)a.T * a.H, a.d,
+                         most(shared, 64, a.pshape, a.P), true);
+  a.pjobs = (int)row_jobs(a, a.pshape, a.P, a.psplits);
 }
+
+int64_t prefix_jobs(const PrefixArgs& a) { return a.pjobs + row_jobs(a, a.shape, a.B, a.splits); }
 
 hipError_t launch_prefix(const PrefixArgs& a, bool bf16, hipStream_t s) {
   if (a.codes) return bf16 ? launch_prefix_e4m3(a, s) : launch_prefix_e4m3_fp32(a, s);

@@ -212,3 +212,46 @@ def test_caches_of_the_tests_hold_what_they_say():
             pg = c.table[b, p // 4]
             got = values(c.cache[1][pg, p % 4], c.scales[1][pg, p % 4])
             assert torch.equal(got.to(torch.bfloat16), c.kv[b][1][:, p])
+
+
+# io_dtype, whether the cache is one of e4m3 numbers, heads, new tokens, sequences, groups: calls of a launch that holds
+# fewer than 2^24 workgroups of 256, and of one that does not
+@pytest.mark.parametrize("io_dtype,which,H,Hkv,d,n_new,B,groups,fits", [
+    (1, "shared", 4, 2, 32, 1 << 26, 1, 1, False),            # fp32 queries over e4m3: 32 rows a workgroup in both roles
+    (1, "shared", 4, 2, 32, (1 << 26) - 4096, 1, 1, True),
+    (1, "shared", 1, 1, 32, 1 << 28, 1, 1, False),
+    (1, "attend", 4, 2, 32, 1 << 26, 1, 0, True),
+    (0, "shared", 4, 2, 32, 1 << 26, 1, 1, True),             # 128 rows
+    (0, "plain", 4, 2, 32, 1 << 26, 1, 1, True),
+    (1, "plain", 4, 2, 32, 1 << 26, 1, 1, True),
+    (1, "shared", 1, 1, 32, (1 << 28) - (1 << 21), 1 << 20, 1 << 20, False),
+    (1, "shared", 2, 1, 16, (1 << 26) - 7, 1 << 19, 1 << 20, True)])
+def test_launches_of_too_many_workgroups_are_refused(io_dtype, which, H, Hkv, d, n_new, B, groups, fits):
+    L, err = P.lib(), ctypes.c_int(7)
+    desc = LactPagedDesc(**dict(PAGED, io_dtype=io_dtype, H=H, Hkv=Hkv, d=d, n_new=n_new, B=B))
+    if which == "attend":
+        need = L.lact_paged_attention_e4m3_workspace_bytes(desc, ctypes.byref(err))
+    else:
+        need = L.lact_paged_prefix_attention_workspace_bytes(desc, prefix(groups=groups), int(which == "shared"), ctypes.byref(err))
+    assert err.value == (0 if fits else EUNSUPPORTED)
+    if not fits:
+        assert need == 0
+        v = view(token=H * d, head=d)
+        c = view(batch=16 * Hkv * d, head=d, token=Hkv * d)
+        assert call(which, dict(io_dtype=io_dtype, H=H, Hkv=Hkv, d=d, n_new=n_new, B=B), ws=1 << 60, q=v, o=v, k_cache=c, v_cache=c,
+                    prefix=prefix(groups=groups)) == EUNSUPPORTED
+
+
+def test_parts_of_wide_tables_stay_within_a_launch():
+    # keys by the hundred million: every part is worth its sums, but the rows of one part fill half a launch
+    L, err = P.lib(), ctypes.c_int(7)
+    for d, B, n_new, io in ((16, 1, 1 << 23, 1), (64, 40, 1 << 22, 1), (16, 1, 1 << 24, 0), (32, 1 << 16, 1 << 20, 0)):
+        for which in ("attend", "shared"):
+            desc = LactPagedDesc(**dict(PAGED, H=8, Hkv=4, d=d, B=B, n_new=n_new, page=16, max_pages=1 << 24, io_dtype=io))
+            if which == "attend":
+                n = L.lact_paged_attention_e4m3_workspace_bytes(desc, ctypes.byref(err))
+            else:
+                n = L.lact_paged_prefix_attention_workspace_bytes(desc, prefix(groups=1, max_pages=1 << 24), 1, ctypes.byref(err))
+            parts = max(1, n // (n_new * 8 * (d + 2) * 4))
+            rows = 32 if io else 128          # a workgroup
+            assert err.value == 0 and parts * n_new * 8 // rows < 1 << 24, (which, d, B, parts)
