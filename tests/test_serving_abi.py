@@ -242,16 +242,15 @@ def test_launches_of_too_many_workgroups_are_refused(io_dtype, which, H, Hkv, d,
                     prefix=prefix(groups=groups)) == EUNSUPPORTED
 
 
-def test_parts_of_wide_tables_stay_within_a_launch():
-    # keys by the hundred million: every part is worth its sums, but the rows of one part fill half a launch
+@pytest.mark.parametrize("B,H,Hkv,d,n_new,page,max_pages,io_dtype", [
+    (501, 64, 8, 16, 1 << 21, 1, 74581363, 1), (30, 8, 8, 64, 1 << 24, 128, 1781422, 1), (199, 1, 1, 80, 107374182, 16, 13517319, 1),
+    (1018890, 1, 1, 16, 3056670, 1, 265423107, 0), (2110, 8, 8, 16, 1 << 24, 16, 15340556, 0)])
+def test_parts_of_wide_tables_stay_within_a_launch(B, H, Hkv, d, n_new, page, max_pages, io_dtype):
+    # keys by the hundred million: every part is worth its sums, but some of them fill a launch
     L, err = P.lib(), ctypes.c_int(7)
-    for d, B, n_new, io in ((16, 1, 1 << 23, 1), (64, 40, 1 << 22, 1), (16, 1, 1 << 24, 0), (32, 1 << 16, 1 << 20, 0)):
-        for which in ("attend", "shared"):
-            desc = LactPagedDesc(**dict(PAGED, H=8, Hkv=4, d=d, B=B, n_new=n_new, page=16, max_pages=1 << 24, io_dtype=io))
-            if which == "attend":
-                n = L.lact_paged_attention_e4m3_workspace_bytes(desc, ctypes.byref(err))
-            else:
-                n = L.lact_paged_prefix_attention_workspace_bytes(desc, prefix(groups=1, max_pages=1 << 24), 1, ctypes.byref(err))
-            parts = max(1, n // (n_new * 8 * (d + 2) * 4))
-            rows = 32 if io else 128          # a workgroup
-            assert err.value == 0 and parts * n_new * 8 // rows < 1 << 24, (which, d, B, parts)
+    desc = LactPagedDesc(**dict(PAGED, B=B, H=H, Hkv=Hkv, d=d, n_new=n_new, page=page, max_pages=max_pages, io_dtype=io_dtype))
+    n = L.lact_paged_attention_e4m3_workspace_bytes(desc, ctypes.byref(err))
+    parts = max(1, n // (n_new * H * (d + 2) * 4))
+    rows = n_new * (H // Hkv)
+    size = 32 if io_dtype else 128 if rows > 32 * B else 16       # rows a workgroup
+    assert err.value == 0 and parts * (rows // size + B) * Hkv < 1 << 24
