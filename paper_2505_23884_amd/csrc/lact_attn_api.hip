@@ -225,9 +225,11 @@ size_t paged_bytes(const PagedArgs& a) {
 // ---------------------------------------------------------------- pages of e4m3 numbers, prefixes
 // A cache of e4m3 numbers: vectors of d bytes, which the kernels move 16 at a
 // time, and a byte for each.
+int check_chunks(const lact_paged_desc* s) { return s->d % 16 ? LACT_EUNSUPPORTED : LACT_OK; }
+
 int check_codes(const lact_paged_desc* s, const lact_view* kc, const lact_view* vc, const lact_view* ks,
                 const lact_view* vs, const int32_t* table, const int32_t* lens, const int32_t* cu, bool out) {
-  if (s->d % 16) return LACT_EUNSUPPORTED;
+  LACT_TRY(check_chunks(s));
   LACT_TRY(check_cache(s, 1, kc, vc, table, lens, cu, out));
   LACT_TRY(check_view(ks, s->pages, s->Hkv, s->page, 1, 0, out));
   LACT_TRY(check_view(vs, s->pages, s->Hkv, s->page, 1, 0, out));
@@ -269,6 +271,7 @@ size_t prefix_bytes(const PrefixArgs& a) {
 // The workspace of a call whose descriptor was found to be `rc`.
 size_t checked_bytes(const lact_paged_desc* s, const lact_prefix* p, bool codes, int rc, int* err) {
   PrefixArgs a{};
+  if (!rc && codes) rc = check_chunks(s);
   if (!rc) {
     a = prefix_args(s, p, codes);
     rc = check_jobs(a);
@@ -578,9 +581,7 @@ int lact_paged_read_e4m3(const lact_paged_desc* desc, const lact_view* k_cache, 
 }
 
 size_t lact_paged_attention_e4m3_workspace_bytes(const lact_paged_desc* desc, int* err) {
-  int rc = check_paged(desc, true);
-  if (!rc && desc->d % 16) rc = LACT_EUNSUPPORTED;
-  return checked_bytes(desc, nullptr, true, rc, err);
+  return checked_bytes(desc, nullptr, true, check_paged(desc, true), err);
 }
 
 int lact_paged_attention_e4m3(const lact_paged_desc* desc, const lact_view* q, const lact_view* k_cache,

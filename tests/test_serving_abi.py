@@ -254,3 +254,10 @@ def test_parts_of_wide_tables_stay_within_a_launch(B, H, Hkv, d, n_new, page, ma
     rows = n_new * (H // Hkv)
     size = 32 if io_dtype else 128 if rows > 32 * B else 16       # rows a workgroup
     assert err.value == 0 and parts * (rows // size + B) * Hkv < 1 << 24
+
+
+def test_workspaces_of_refused_vectors():
+    L, err = P.lib(), ctypes.c_int(7)
+    f = lambda e4m3: L.lact_paged_prefix_attention_workspace_bytes(LactPagedDesc(**dict(PAGED, d=24)), prefix(), e4m3, ctypes.byref(err))
+    assert f(1) == 0 and err.value == EUNSUPPORTED       # as the call
+    assert f(0) > 0 and err.value == 0
