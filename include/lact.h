@@ -715,6 +715,8 @@ int lact_paged_attention(const lact_paged_desc* desc, const lact_view* q, const 
  * hold nothing. lact_paged_attention_e4m3 is lact_paged_attention over such a
  * cache. Values read are exact for x in [10, 246], all that the append writes;
  * with other bytes in a slot they may be zero, infinite or NaN.
+ * Few rows' scores are summed over the numbers c_i before their power of two
+ * comes in: the magnitudes of a query's elements add up to less than 2^119.
  *
  * d a multiple of 16 (else LACT_EUNSUPPORTED); the other limits and refusals of
  * lact_paged_append and lact_paged_attention.

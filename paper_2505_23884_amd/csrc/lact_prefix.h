@@ -841,7 +841,7 @@ struct Slim {
           }
         }
     }
-    __device__ __forceinline__ void put(uint8_t* kt, float c) const {
+    __device__ __forceinline__ void put(uint8_t* kt) const {
       const int lane = threadIdx.x & 63, chunk = lane % CPR;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -849,10 +849,10 @@ struct Slim {
         *reinterpret_cast<u32x4*>(kt + off(row, chunk)) = k[i];
         *reinterpret_cast<u32x4*>(kt + VB + off(row_of(row), chunk)) = v[i];
       }
-      if constexpr (CODES) {   // the factors of a key's scores and of its weights
+      if constexpr (CODES) {   // the powers of two of a key's scores and of its weights
 #pragma unroll
         for (int y = 0; y < HP; ++y)
-          reinterpret_cast<float*>(kt + 2 * VB)[64 * y + 2 * (lane & 31) + (lane >> 5)] = scale_of(scale[y]) * (lane < 32 ? c : 1.0f);
+          reinterpret_cast<float*>(kt + 2 * VB)[64 * y + 2 * (lane & 31) + (lane >> 5)] = scale_of(scale[y]);
       }
     }
   };
@@ -919,7 +919,7 @@ struct Slim {
       const bool scrubbed = what == 1 && __any(t.any_nonfinite());
       if (__builtin_expect(scrubbed, 0)) t.scrub();
       wave_fence();
-      t.put(ks, c);
+      t.put(ks);
       wave_fence();
       // the next tile
       const Slot<C> old = here;
@@ -979,7 +979,7 @@ struct Slim {
             kf[hp][u][2] = hi[0], vf[hp][u][2] = hi[1], kf[hp][u][3] = hi[2], vf[hp][u][3] = hi[3];
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) kf[hp][u][i] = c, vf[hp][u][i] = 1.0f;
+            for (int i = 0; i < 4; ++i) kf[hp][u][i] = 1.0f, vf[hp][u][i] = 1.0f;
           }
         }
       if (what) {
@@ -990,7 +990,7 @@ struct Slim {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[u][i] = s[y][u][i] * kf[y / NR][u][i];
+            for (int i = 0; i < 4; ++i) z[u][i] = s[y][u][i] * kf[y / NR][u][i] * c;   // (the score first: 2^119 c may be past fp32)
           if (what == 1) {
             const int jlo = sg[y % NR].p - jb.band.win + 1, jhi = sg[y % NR].jhi, sink = min(jb.band.sinks, jhi + 1);
             const int lo = jhi < jlo ? 1 << 30 : jlo;

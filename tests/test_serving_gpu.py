@@ -831,3 +831,27 @@ def test_outputs_and_workspaces_given_and_bindings_refuse():
     # a prefix of no pages
     same(P.paged_prefix_attention(q, *caches[:2], x["ptable"][:, :0].contiguous(), plen, seqs, *t, k_scale=caches[2], v_scale=caches[3]),
          P.paged_prefix_attention(q, *caches[:2], x["ptable"], plen * 0, seqs, *t, k_scale=caches[2], v_scale=caches[3]))
+
+
+@types
+@pytest.mark.parametrize("prefix", [False, True], ids=["own", "prefix"])
+@pytest.mark.parametrize("new,Hkv,d", [([1, 1], 2, 64), ([1, 1], 1, 128), ([5, 9], 1, 64), ([9, 7], 2, 256), ([60, 30], 2, 128)])
+def test_scores_of_zero_at_any_scale(new, Hkv, d, prefix, dtype):
+    # keys of the largest magnitudes that a cache holds, times a scale over 355: past fp32 before a score is
+    lens, plen, H = [100, 60], [40], 2 * Hkv
+    c = Cache(lens, Hkv, d, 16, dtype, True, 51, prefixes=plen)
+    c.scales[0] = torch.where(c.scales[0] == 255, c.scales[0], torch.full_like(c.scales[0], 246))
+    cu = offsets(new)
+    q = torch.zeros(cu[-1], H, d, dtype=dtype, device=DEV)
+    print(f"[gpu] scores of zero {new} {Hkv} {d} {prefix} {dtype}", flush=True)
+    for scale in (1.0, 1e3, 1e12):
+        if prefix:
+            o = prefix_call(c, q, torch.full_like(q, 7.0), plen, [0, 2], lens, cu, scale=scale)
+        else:
+            o = P.paged_attention_e4m3(q, *c.on(DEV), c.table.to(DEV), i32(lens), i32(cu), scale=scale)
+        for b in range(2):
+            k, v = (torch.cat([c.pkv[0][w], c.kv[b][w]], 1) if prefix else c.kv[b][w] for w in range(2))
+            rows = slice(cu[b], cu[b + 1])
+            want, tol = attention(q[rows].transpose(0, 1)[None].cpu(), torch.zeros_like(k)[None], v[None],
+                                  q_start=k.shape[1] - new[b])
+            check(f"{scale} {b}", o[rows].transpose(0, 1)[None], want["o"], tol["o"])
