@@ -619,7 +619,8 @@ int lact_qk_norm_rope_backward(const lact_rope_desc* desc, const lact_view* q, c
  * the second products: outputs are off by about 0.0023 of their norm, where the
  * rounding of the outputs alone makes 0.0017. dq and dk of rows that see at most
  * 128 keys, and the output of few new tokens over pages (tokens times H / Hkv up
- * to 32 a sequence on average), take what that rounding leaves too.
+ * to 32 a sequence on average, behind a shared prefix too), take what that
+ * rounding leaves too.
  * Scores (scale q . k) stay below 2^29 in magnitude, here and over pages: past
  * it the rounding of a row's maximum is larger than an exponent's range. The
  * reverse takes the weights from lse, so they are off by |lse| 2^-24 of

@@ -384,7 +384,10 @@ struct Shapes {
 // wait for, are read a stretch ahead of the products. Bound by vector and matrix work that
 // take turns (43 and 31 % of the cycles), 8 chunks of 1024 tokens over 8192 keys, 16 / 4 heads
 // of 128: e4m3 0.69 PF, bf16 0.65; 64 keys a tile, since 32 cost 20 % more.
-template <typename T, class C, int DP>
+// WHOLE: bf16 weights in two parts, for the rows of groups whose sequences have few
+// each (up to 32 on average, as the rows over their own keys then have them): 64 tokens
+// behind 16384 bf16 keys 50 us for 49, 2 x 48 behind 30011 in 8 bits 78 for 70, heads of 256 117 for 111.
+template <typename T, class C, int DP, bool WHOLE>
 __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const Row& row, const Sights& sg, int hk,
                                      uint8_t* smem, uint32_t* mask, int* found) {
   using L = Tile<T, DP>;
@@ -512,7 +515,14 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
           sum += s[i];
         }
         st.l += sum;
-        const RowsB<T> w(s);
+        // (WHOLE: the first 8 bits and what they leave; e4m3 numbers have no infinities that need both above zero)
+        f32x16 most = s;
+        if constexpr (WHOLE) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) most[i] = __uint_as_float(__float_as_uint(s[i]) & 0xffff0000u);
+          s -= most;
+        }
+        const RowsB<T> w(most), rest(s);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -520,13 +530,14 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
           for (int b = 0; b < L::DB; ++b) {
             const u32x2 lo = vf[4 * b + 2 * h], hi = vf[4 * b + 2 * h + 1];
             mma_chunk<T>(st.o[b], u32x4{lo[0], lo[1], hi[0], hi[1]}, w.v[h]);
+            if constexpr (WHOLE) mma_chunk<T>(st.o[b], u32x4{lo[0], lo[1], hi[0], hi[1]}, rest.v[h]);
           }
       }
     } else {
       auto step = [&](auto rb) __attribute__((always_inline)) {
         constexpr int RB = decltype(rb)::value;
         const int what = inner ? 2 : sees(jb.band, jb.len, sg.wa, sg.wb, k0 + RB, 32);
-        if (what) softmax_step<T, DP, RB>(st, q, ks, ks + BYTES, c, !inner, see);
+        if (what) softmax_step<T, DP, RB, WHOLE>(st, q, ks, ks + BYTES, c, !inner, see);
       };
       step(std::integral_constant<int, 0>{});
       if constexpr (KT == 64) step(std::integral_constant<int, 32>{});
@@ -1143,7 +1154,7 @@ struct Words {
   int found, sights[2 * kWaves], offsets[kOffsets + 1];
 };
 
-template <typename T, class C, int DP, int SHAPE, bool GROUP>
+template <typename T, class C, int DP, int SHAPE, bool GROUP, bool WHOLE>
 __device__ __forceinline__ void work(const PrefixArgs& a, const Offsets& off, const Job& jb, int p0, int hk, uint8_t* smem,
                                      Words& words) {
   using Ro = Role<T, C, DP, SHAPE>;
@@ -1158,7 +1169,7 @@ __device__ __forceinline__ void work(const PrefixArgs& a, const Offsets& off, co
     } else {
       sg = own_sights(a, jb, p0, row, wr, Ro::R);
     }
-    if constexpr (SHAPE == kRows128) wide<T, C, DP>(a, jb, row, sg, hk, smem, words.mask, &words.found);
+    if constexpr (SHAPE == kRows128) wide<T, C, DP, WHOLE>(a, jb, row, sg, hk, smem, words.mask, &words.found);
     else narrow<T, C, DP>(a, jb, row, sg, hk, smem);
   } else {
     constexpr int NR = Ro::NR, HP = Ro::HP;
@@ -1224,7 +1235,7 @@ __global__ __launch_bounds__(64 * kWaves, (occupancy<T, C, DP, PS, OS>())) void 
       jb.len = s.len;
       jb.split = jb.part = u - t * a.psplits;
       jb.splits = a.psplits;
-      work<T, C, DP, PS, true>(a, off, jb, 0, head, smem, words);
+      work<T, C, DP, PS, true, OS != kRows128>(a, off, jb, 0, head, smem, words);
       return;
     }
   }
@@ -1245,7 +1256,7 @@ __global__ __launch_bounds__(64 * kWaves, (occupancy<T, C, DP, PS, OS>())) void 
       if (g >= 0) jb.band.sinks = max(0, a.sinks - clampi(a.plen[g], 0, a.p_pages * a.page));
     }
   }
-  work<T, C, DP, OS, false>(a, off, jb, s.p0, head, smem, words);
+  work<T, C, DP, OS, false, false>(a, off, jb, s.p0, head, smem, words);
 }
 
 // The parts of each (token, head), joined in a fixed order: those over its

@@ -855,3 +855,44 @@ def test_scores_of_zero_at_any_scale(new, Hkv, d, prefix, dtype):
             want, tol = attention(q[rows].transpose(0, 1)[None].cpu(), torch.zeros_like(k)[None], v[None],
                                   q_start=k.shape[1] - new[b])
             check(f"{scale} {b}", o[rows].transpose(0, 1)[None], want["o"], tol["o"])
+
+
+# prefixes, sequences of each, lens, new, H, Hkv, d: up to 32 rows of a key head in a sequence, and as many
+# in a group as come together
+FEW = [
+    ([140, 90], [1, 1], [333, 90], [5, 5], 6, 1, 64),            # sequences of more than 16 rows, in groups of their own
+    ([140, 90], [1, 1], [33, 90], [3, 4], 6, 2, 128),
+    ([300], [2], [333, 90], [5, 5], 6, 1, 64),                   # more than 32 rows a group
+    ([300], [2], [20, 90], [5, 5], 6, 1, 256),
+    ([1700], [40], list(range(1, 41)), [1] * 40, 8, 2, 128),     # a decoding batch, the prefix in parts
+    ([700, 40], [30, 10], [5] * 40, [1] * 40, 4, 2, 64),
+    ([400], [20], [9] * 20, [1] * 20, 8, 1, 256),
+    ([200], [12], [6] * 12, [3] * 12, 4, 2, 80),
+]
+
+
+@pytest.mark.parametrize("dtype,codes", [(BF, True), (F32, True), (BF, False)], ids=["bf16-e4m3", "fp32-e4m3", "bf16"])
+@pytest.mark.parametrize("i", range(len(FEW)))
+def test_few_rows_behind_a_prefix_are_rounded_once(i, dtype, codes):
+    # as test_few_rows_are_rounded_once(): two or three parts of a weight, however many rows share the prefix
+    plen, counts, lens, new, H, Hkv, d = FEW[i]
+    G = H // Hkv
+    assert sum(new) * G <= 32 * len(lens)
+    c = Cache(lens, Hkv, d, 16, dtype, codes, 40 + i, prefixes=plen)
+    cu, seqs = offsets(new), offsets(counts)
+    q = rnd(2, cu[-1], H, d, dtype=dtype).to(DEV)
+    left = 2.0 ** -15 if dtype is BF else 2.0 ** -22
+    print(f"[gpu] few rows behind a prefix {FEW[i]} {dtype} {codes}", flush=True)
+    o = prefix_call(c, q, torch.full_like(q, 7.0), plen, seqs, lens, cu).cpu()
+    for g, f in enumerate(plen):
+        for b in range(seqs[g], seqs[g + 1]):
+            n, m = new[b], lens[b]
+            k, v = (torch.cat([c.pkv[g][w], c.kv[b][w]], 1) for w in range(2))
+            see = visible(n, f + m, f + m, f + m - n, None, 0, 0)
+            for h in range(H):
+                x = q[cu[b]:cu[b + 1], h].cpu()
+                r = head(x, k[h // G], v[h // G], see, d ** -0.5)
+                mag = (x.double().abs() @ k[h // G].double().abs().t()).amax(1, keepdim=True) * d ** -0.5
+                e = r["e"] + left + (left * mag if dtype is F32 else 0.0)
+                check(f"{b} {h}", o[cu[b]:cu[b + 1], h], r["o"],
+                      r["o_mag"] * (e + (f + m) * 2.0 ** -24) * 1.01 + r["o"].abs() * HALF[dtype])
