@@ -896,3 +896,44 @@ def test_few_rows_behind_a_prefix_are_rounded_once(i, dtype, codes):
                 e = r["e"] + left + (left * mag if dtype is F32 else 0.0)
                 check(f"{b} {h}", o[cu[b]:cu[b + 1], h], r["o"],
                       r["o_mag"] * (e + (f + m) * 2.0 ** -24) * 1.01 + r["o"].abs() * HALF[dtype])
+
+
+@types
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+@pytest.mark.parametrize("i", range(len(SPOILT)))
+def test_infinities_in_pages_behind_a_prefix_stay_what_they_are(i, value, dtype):
+    # as test_nan_in_pages_..., where a part of a weight that became zero, or a sign that was lost, would show
+    lens, new, H, Hkv, d, page, opt, b, where = SPOILT[i]
+    f, plen, seqs = 75, [75], [0, len(lens)]
+    c = Cache(lens, Hkv, d, page, dtype, False, 300 + i, prefixes=plen)
+    cu = offsets(new)
+    q = rnd(i, cu[-1], H, d, dtype=dtype).to(DEV)
+    print(f"[gpu] infinities behind a prefix {SPOILT[i]} {value} {dtype}", flush=True)
+
+    def call():
+        return prefix_call(c, q, torch.full_like(q, 7.0), plen, seqs, lens, cu, **opt)
+
+    base = call()
+    assert bool(torch.isfinite(base.float()).all())
+    cols = torch.arange(d) % 3 == 1
+    group = torch.repeat_interleave(torch.arange(len(lens)), torch.tensor(new))
+    pos = torch.cat([torch.arange(n - m, n) for n, m in zip(lens, new)])
+    seen = 0
+    for own_key, at in [(True, x) for x in where] + [(False, x) for x in (0, 31, 64, 74)]:
+        v, table = c.cache[1], c.table[b] if own_key else c.ptable[0]
+        saved = v.clone()
+        v[table[at // page], at % page][..., cols] = value
+        p, j = f + pos, f + at if own_key else at
+        see = j <= p
+        if "window" in opt:
+            see &= (j > p - opt["window"]) | (j < opt.get("sinks", 0))
+        if own_key:
+            see &= group == b
+        got = call()
+        c.cache[1] = saved
+        seen += int(see.sum())
+        see = see.to(DEV)
+        same(got[~see], base[~see], ("rows that do not see it", own_key, at))
+        same(got[see].cpu()[..., ~cols], base[see].cpu()[..., ~cols], ("other columns", own_key, at))
+        assert bool((got[see].cpu()[..., cols] == value).all()), (own_key, at)
+    assert seen
