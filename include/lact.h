@@ -699,9 +699,10 @@ int lact_paged_attention(const lact_paged_desc* desc, const lact_view* q, const 
  * lact_paged_append_e4m3 is lact_paged_append into such a cache: with a the
  * largest |element| of a vector, x - 127 is the smallest e with a <= 448 2^e,
  * within [-117, 119], and the elements are rounded to the nearest number, ties
- * to the even one (so they are off by 2^-4 of themselves, or by 2^(e - 10) where
- * that is more: elements below 2^-14 of the largest). Magnitudes over 448 2^119
- * become that. Infinities and NaN become NaN (0x7f) and do not count for a. Vectors
+ * to the even one (so they are off by at most 2^-4 of themselves, or by 2^(e - 10)
+ * where that is more: elements below 2^(e - 6). Those are below 2^-13.8 of the largest,
+ * but may be any, the largest too, where e is -117: in vectors below 2^-108). Magnitudes
+ * over 448 2^119 become that. Infinities and NaN become NaN (0x7f) and do not count for a. Vectors
  * of zeros have x = 10. If an append of one call writes a slot twice, any 8 numbers
  * of it, and its byte, may be of either.
  *
