@@ -14,8 +14,6 @@ namespace attn {
 // least normal fp32, and the largest, 448, times 2^119 is within bf16.
 constexpr int kMinExp = -117, kMaxExp = 119;
 
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2v;
-
 __device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 
 // The smallest e with a <= 448 2^e = 1.75 2^(e + 8), within the range, plus

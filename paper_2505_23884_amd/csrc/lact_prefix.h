@@ -213,22 +213,12 @@ struct Heads<Code> {
         ks(a.ks + hk * a.cs.sh), vs(a.vs + hk * a.cs.sh) {}
 };
 
-// A tile of KT keys and values on its way from memory to LDS through the
-// registers of NT threads; what goes to LDS is T. Each wave's lanes know where
-// the tile's keys lie (lane = key).
-template <typename T, class C, int DP, int KT, int NT>
-struct Stage : PagedStage<T, DP, NT> {
-  using Base = PagedStage<T, DP, NT>;
-  static_assert(KT == kKT, "tiles through registers");
-  __device__ __forceinline__ void load(const Heads<T>& h, const Slot<T>& s, int d) { Base::load(h.k, h.v, s.at, d); }
-  __device__ __forceinline__ void put(uint8_t* kt, uint8_t* vt, bool scrubbed) {
-    if (__builtin_expect(scrubbed, 0)) Base::scrub();
-    Base::store(kt, vt);
-  }
-};
-template <typename T, int DP, int KT, int NT>
-struct Stage<T, Code, DP, KT, NT> {
-  using L = Tile<T, DP>;
+// A tile of KT keys and values in e4m3 numbers on its way from memory to LDS,
+// as bf16, through the registers of NT threads. Each wave's lanes know where the
+// tile's keys lie (lane = key).
+template <int DP, int KT, int NT>
+struct Stage {
+  using L = Tile<__bf16, DP>;
   static constexpr int CPR = DP / 16;   // 16 numbers a load
   static constexpr int N = KT * CPR / NT, STEP = NT / CPR;
   static_assert(N >= 1 && KT * CPR % NT == 0, "tile split");
@@ -248,23 +238,20 @@ struct Stage<T, Code, DP, KT, NT> {
     }
   }
   __device__ __forceinline__ void put(uint8_t* kt, uint8_t* vt) {
-    constexpr int W = 4 * (int)sizeof(T);   // words of 16 elements
-    const int c = threadIdx.x % CPR * (W / 4);
+    const int c = threadIdx.x % CPR * 2;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = row(i);
       const float ks = scale_of(__shfl(kb, r & 63, 64)), vs = scale_of(__shfl(vb, r & 63, 64));
-      uint32_t w[W];
+      uint32_t w[8];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) widen<T>(k[i][x], ks, w + x * W / 4);
+      for (int x = 0; x < 4; ++x) widen<__bf16>(k[i][x], ks, w + 2 * x);
+      *reinterpret_cast<u32x4*>(kt + L::off(r, c)) = u32x4{w[0], w[1], w[2], w[3]};
+      *reinterpret_cast<u32x4*>(kt + L::off(r, c + 1)) = u32x4{w[4], w[5], w[6], w[7]};
 #pragma unroll
-      for (int x = 0; x < W; x += 4)
-        *reinterpret_cast<u32x4*>(kt + L::off(r, c + x / 4)) = u32x4{w[x], w[x + 1], w[x + 2], w[x + 3]};
-#pragma unroll
-      for (int x = 0; x < 4; ++x) widen<T>(v[i][x], vs, w + x * W / 4);
-#pragma unroll
-      for (int x = 0; x < W; x += 4)
-        *reinterpret_cast<u32x4*>(vt + L::off(r, c + x / 4)) = u32x4{w[x], w[x + 1], w[x + 2], w[x + 3]};
+      for (int x = 0; x < 4; ++x) widen<__bf16>(v[i][x], vs, w + 2 * x);
+      *reinterpret_cast<u32x4*>(vt + L::off(r, c)) = u32x4{w[0], w[1], w[2], w[3]};
+      *reinterpret_cast<u32x4*>(vt + L::off(r, c + 1)) = u32x4{w[4], w[5], w[6], w[7]};
     }
   }
 };
@@ -288,9 +275,9 @@ __device__ __forceinline__ void restore_key(Softmax<DP / 32>& st, const Heads<C>
       for (int i = 0; i < 16; ++i) {
         const int e = 32 * db + 8 * (i >> 2) + 4 * half + (i & 3);
         if (!see || e >= d) continue;
-        uint32_t w[sizeof(T)];
-        widen<T>(row[e], scale, w);
-        const float x = sizeof(T) == 2 ? __uint_as_float(w[0] << 16) : __uint_as_float(w[0]);
+        uint32_t w[2];
+        widen<__bf16>(row[e], scale, w);
+        const float x = __uint_as_float(w[0] << 16);
         if (!(fabsf(x) < __builtin_inff())) st.o[db][i] += x;
       }
   } else {
@@ -368,11 +355,10 @@ __device__ __forceinline__ f32x2* part_sums(const PrefixArgs& a, int64_t row) {
   return reinterpret_cast<f32x2*>(a.part + (int64_t)(a.psplits + a.splits) * a.T * a.H * a.d) + row;
 }
 
-template <typename T, class C, int DP>
+template <typename T, int DP>
 struct Shapes {
   using L = Tile<T, DP>;
   static constexpr bool H = sizeof(T) == 2 && DP <= 128;
-  static constexpr bool NARROW = !(sizeof(T) == 4 && DP == 256);   // a wave's own tile would not fit
   static constexpr int KT = H ? 64 : 32, BYTES = KT * L::PITCH, WIDE = 4 * BYTES;
   static constexpr int JOIN = 32 * (DP + 2) * 4;
   static constexpr int WAVE = ((2 * kKT * L::PITCH > JOIN ? 2 * kKT * L::PITCH : JOIN) + 1023) / 1024 * 1024;
@@ -392,7 +378,7 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
                                      uint8_t* smem, uint32_t* mask, int* found) {
   using L = Tile<T, DP>;
   constexpr bool CODES = std::is_same<C, Code>::value;
-  constexpr int KT = Shapes<T, C, DP>::KT, BYTES = KT * L::PITCH, NT = 64 * kWaves;
+  constexpr int KT = Shapes<T, DP>::KT, BYTES = KT * L::PITCH, NT = 64 * kWaves;
   using Cp = Copy<T, DP, KT, NT>;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const KeyTiles kt(jb.band, jb.len, sg.pa, sg.pb, KT);
@@ -432,7 +418,7 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
     return p;
   };
   auto tile_of = [&](int x) __attribute__((always_inline)) { return smem + ((x - x0) & 1) * 2 * BYTES; };
-  [[maybe_unused]] typename std::conditional<CODES, Stage<T, Code, DP, KT, NT>, Softmax<1>>::type stage;
+  [[maybe_unused]] typename std::conditional<CODES, Stage<DP, KT, NT>, Softmax<1>>::type stage;
   auto copy = [&](int x, const Slot<C>& s) __attribute__((always_inline)) {
     if constexpr (CODES) {
       stage.load(hd, s, a.d);
@@ -559,24 +545,24 @@ __device__ __forceinline__ void wide(const PrefixArgs& a, const Job& jb, const R
   if (row.ok && lane < 32) *part_sums(a, to) = f32x2{st.m, l};
 }
 
-// 32 rows; the waves take turns at the tiles of keys, each through LDS of its
+// 32 rows over an fp32 cache; the waves take turns at the tiles of keys, each through LDS of its
 // own, and join their sums at the end.
-template <typename T, class C, int DP>
+template <int DP>
 __device__ __forceinline__ void narrow(const PrefixArgs& a, const Job& jb, const Row& row, const Sights& sg, int hk,
                                        uint8_t* smem) {
-  using L = Tile<T, DP>;
-  constexpr int BYTES = kKT * L::PITCH, WAVE = Shapes<T, C, DP>::WAVE;
+  using L = Tile<float, DP>;
+  constexpr int BYTES = kKT * L::PITCH, WAVE = Shapes<float, DP>::WAVE;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const KeyTiles kt(jb.band, jb.len, sg.wa, sg.wb, kKT);
   const int x0 = share(kt.count(), jb.split, jb.splits), x1 = share(kt.count(), jb.split + 1, jb.splits);
-  const Heads<C> hd(a, hk);
+  const Heads<float> hd(a, hk);
   u32x4 q[L::KS];
-  load_row<T, DP>(q, reinterpret_cast<const T*>(a.q.p) + row.token * a.q.st + row.head * a.q.sh, row.ok, a.d);
+  load_row<float, DP>(q, reinterpret_cast<const float*>(a.q.p) + row.token * a.q.st + row.head * a.q.sh, row.ok, a.d);
   Softmax<DP / 32> st;
   st.init();
   const float c = a.scale * kLog2e;
   uint8_t* ks = smem + wave * WAVE;
-  Stage<T, C, DP, kKT, 64> stage;
+  PagedStage<float, DP, 64> stage;
   auto place = [&](int x) __attribute__((always_inline)) {
     Place p{};
     p.at = -1;
@@ -584,29 +570,27 @@ __device__ __forceinline__ void narrow(const PrefixArgs& a, const Job& jb, const
     return p;
   };
   int x = x0 + wave;
-  Slot<C> at(a, place(x));
+  Slot<float> at(a, place(x));
   Place next = place(x + kWaves);
-  if (x < x1) stage.load(hd, at, a.d);
+  if (x < x1) stage.load(hd.k, hd.v, at.at, a.d);
   for (; x < x1; x += kWaves) {
-    const Slot<C> here = at;
+    const Slot<float> here = at;
     const uint32_t there = (uint32_t)__ballot(here.at >= 0);
-    at = Slot<C>(a, next);
+    at = Slot<float>(a, next);
     const int k0 = kt.tile(x) * kKT;
     const int what = there == 0xffffffffu ? sees(jb.band, jb.len, sg.wa, sg.wb, k0, kKT) : 1;
     const bool scrubbed = what == 1 && __any(stage.any_nonfinite());
+    if (__builtin_expect(scrubbed, 0)) stage.scrub();
     wave_fence();
-    stage.put(ks, ks + BYTES, scrubbed);
+    stage.store(ks, ks + BYTES);
     wave_fence();
-    if (x + kWaves < x1) stage.load(hd, at, a.d);
+    if (x + kWaves < x1) stage.load(hd.k, hd.v, at.at, a.d);
     next = place(x + 2 * kWaves);
     const Sight sight(jb.band, sg.p, sg.jhi, k0);
     const uint32_t mine = there >> (4 * (lane >> 5));
     auto see = [&](int r) __attribute__((always_inline)) { return sight.see(r) && (mine >> r & 1); };
-    if (what) softmax_step<T, DP, 0, true>(st, q, ks, ks + BYTES, c, what == 1, see);
-    if (__builtin_expect(scrubbed, 0)) {
-#pragma unroll 1
-      for (int j = 0; j < kKT; ++j) restore_key<T, C, DP>(st, hd, here, j, a.d, sight);
-    }
+    if (what) softmax_step<float, DP, 0>(st, q, ks, ks + BYTES, c, what == 1, see);
+    if (__builtin_expect(scrubbed, 0)) restore_nonfinite<float, DP>(st, hd.v, here.at, a.d, sight);
   }
   // the waves' sums: each lane's [32][DP] and (m, l), added by all threads
   __syncthreads();
@@ -638,12 +622,7 @@ __device__ __forceinline__ void narrow(const PrefixArgs& a, const Job& jb, const
       o += *reinterpret_cast<const f32x4*>(of + r * DP + e) * f;
     }
     if (jb.part < 0) {
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      T* dst = out_row<T>(a, out) + e;
-      if constexpr (sizeof(T) == 2)
-        *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
-      else
-        *reinterpret_cast<f32x4*>(dst) = o * inv;
+      *reinterpret_cast<f32x4*>(out_row<float>(a, out) + e) = o * (sum == 0.0f ? 0.0f : 1.0f / sum);
     } else {
       const int64_t to = part_row(a, jb.part, out);
       *reinterpret_cast<f32x4*>(a.part + to * a.d + e) = o;
@@ -1135,8 +1114,8 @@ struct Role {
   static constexpr int HP = SHAPE == kPairs16 ? 2 : 1;   // key heads a workgroup
   static constexpr int smem() {
     if constexpr (SHAPE == kNone) return 0;
-    else if constexpr (SHAPE == kRows128) return Shapes<T, C, DP>::WIDE;
-    else if constexpr (PAGED32) return kWaves * Shapes<T, C, DP>::WAVE;
+    else if constexpr (SHAPE == kRows128) return Shapes<T, DP>::WIDE;
+    else if constexpr (PAGED32) return kWaves * Shapes<T, DP>::WAVE;
     else return Slim<T, C, DP, NR, HP>::SMEM;
   }
 };
@@ -1170,7 +1149,7 @@ __device__ __forceinline__ void work(const PrefixArgs& a, const Offsets& off, co
       sg = own_sights(a, jb, p0, row, wr, Ro::R);
     }
     if constexpr (SHAPE == kRows128) wide<T, C, DP, WHOLE>(a, jb, row, sg, hk, smem, words.mask, &words.found);
-    else narrow<T, C, DP>(a, jb, row, sg, hk, smem);
+    else narrow<DP>(a, jb, row, sg, hk, smem);
   } else {
     constexpr int NR = Ro::NR, HP = Ro::HP;
     Row row[NR * HP];
