@@ -622,7 +622,9 @@ int lact_qk_norm_rope_backward(const lact_rope_desc* desc, const lact_view* q, c
  * to 32 a sequence on average, behind a shared prefix too), take what that
  * rounding leaves too.
  * Scores (scale q . k) stay below 2^29 in magnitude, here and over pages: past
- * it the rounding of a row's maximum is larger than an exponent's range. The
+ * it the rounding of a row's maximum is larger than an exponent's range. Outputs
+ * are divided by their weights' sum at the end, and a weight is up to 2^8 until
+ * then: the magnitudes of v over a row's keys add up to less than 2^119. The
  * reverse takes the weights from lse, so they are off by |lse| 2^-24 of
  * themselves.
  */

@@ -11,7 +11,8 @@ namespace lact {
 // many: a pair takes 1.43 times one alone (12 chunks of 160 tokens behind 8192 keys,
 // the prefix in 1, 2, 3, 4 and 6 parts: 256, 180, 199, 162 and 173 us; 234, 167, 190, 142 and 151
 // by this with 0.0286 us a key, and 5 a part for the sums; 32 sequences of 5 tokens, heads of 64
-// in 8 bits, 2 to 8 parts: 52, 46, 43, 54, 52, 51 us).
+// in 8 bits, 2 to 8 parts: 52, 46, 43, 54, 52, 51 us). Where registers leave one a CU (an
+// fp32 cache, heads over 128) the rounds are twice as many as this has them.
 double span(int64_t wgs, double us) {
   const int64_t full = wgs / 512, rest = wgs % 512;
   return (full * 1.43 + (rest > 256 ? 1.43 : rest ? 1.0 : 0.0)) * us;
